@@ -359,6 +359,126 @@ rr_status rr_aux_loss_bwd(int T, int E, const float *logits, const float *f, flo
                           int accumulate, float *dlogits, void *stream);
 
 /*
+ * ---- The parts of a transformer block around the expert layer --------------------------------------------
+ * (no counterpart in the paper, whose models take them from their training framework: the dense projections, the
+ * residual connection that Section 3 leaves outside the layer, and the balance loss on padded batches).
+ *
+ * Dropout masks.  Every entry point below with a `p` and an `rng` argument takes its mask from a counter-based
+ * generator, Philox4x32-10 (Salmon et al., SC 2011), and stores none: element i of the result (row-major index
+ * without pitch) is kept iff the (i % 8)-th 16-bit piece, low half first, of the generator's four words for
+ *     key = seed (low, high word),  counter = (i / 8 low, i / 8 high, offset low, offset high)
+ * is >= D = floor(65536 p + 0.5); kept elements are multiplied by 65536 / (65536 - D).  p is in [0, 1] and
+ * takes effect in steps of 1/65536 (below 2^-17 it is no dropout at all, p = 1 drops everything).
+ *   rng   [2] u64 dev, 16-byte aligned: {seed, offset}.  It is read when the kernel runs, so a captured call takes
+ *         what stands there at each replay.  The same pair gives the same mask in every entry point; give each
+ *         call of a step its own offset.  May be NULL when p takes no effect.
+ * A dropped element is selected away: a NaN in a dropped place does not reach the result.
+ */
+
+/*
+ * rr_dropout_fwd:  y_i = residual_i + keep_i x_i / (1 - p)      (without the residual when it is NULL)
+ * rr_dropout_bwd: dx_i = keep_i dy_i / (1 - p), added to what dx holds when accumulate != 0; the gradient of the
+ *                 residual is dy itself.
+ *   n         elements, >= 0 (n == 0 does nothing)
+ *   x, dy     dev, element type x_dtype / dy_dtype;  residual, y, dx   dev, element type y_dtype / dx_dtype
+ *   y may be the same buffer as residual, and as x if the types are equal; any other overlap is not allowed.
+ * fp32 arithmetic, one rounding to the type of the result.  One kernel, no workspace.
+ */
+rr_status rr_dropout_fwd(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p,
+                         const void *rng /* dev */, void *y, void *stream);
+rr_status rr_dropout_bwd(long long n, int dy_dtype, int dx_dtype, const void *dy, float p, const void *rng /* dev */,
+                         int accumulate, void *dx, void *stream);
+
+/* activations of rr_linear_* */
+#define RR_ACT_NONE 0
+#define RR_ACT_RELU 1
+#define RR_ACT_GELU 2      /* v Phi(v), Phi the normal distribution function                */
+#define RR_ACT_GELU_TANH 3 /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2               */
+#define RR_ACT_SILU 4      /* v / (1 + e^-v)                                                */
+
+/* flags of rr_linear_shape (backward): add to the gradient instead of overwriting it */
+#define RR_ADD_DX 1u
+#define RR_ADD_DW 2u /* dW and dbias */
+
+/* Shape of one linear layer call.  Pitches count elements between rows; 0 means densely packed. */
+typedef struct rr_linear_shape {
+    int32_t M, N, K;           /* tokens, outputs, inputs; N and K are multiples of 8             */
+    int32_t act;               /* RR_ACT_*                                                        */
+    int32_t y_dtype;           /* RR_BF16 or RR_F32: type of y and residual                       */
+    int32_t dx_dtype, dw_dtype; /* RR_BF16 or RR_F32 (backward)                                   */
+    uint32_t flags;            /* RR_ADD_DX | RR_ADD_DW (backward)                                */
+    float p;                   /* dropout probability                                             */
+    int64_t ldx, ldr, ldy, ldz; /* pitches of x, residual, y, z: at least their widths, rows a    */
+    int64_t lddy, lddx;        /* multiple of 16 bytes apart; of dy and dx                        */
+} rr_linear_shape;
+
+/*
+ * rr_linear_fwd -- matrix product with everything behind it in its epilogue:
+ *     z = x W^T + bias,     y = residual + D(act(z)),     D = dropout (above) on the index row*N + column
+ *   x [M,K], W [N,K], bias [N] (or NULL)   dev bf16, 16-byte aligned, read only
+ *   residual [M,N] (or NULL), y [M,N]      dev, type y_dtype; y may be the same buffer as residual (same pitch),
+ *                                          no other overlap
+ *   z [M,N] dev bf16, or NULL: the pre-activations for rr_linear_bwd, rounded to bf16 (needed unless act is RR_ACT_NONE)
+ *   workspace dev, >= fwd_bytes, 256-byte aligned: the status word read by rr_check and nothing else
+ * Products are bf16 x bf16 on the tensor cores with fp32 accumulation (their adder truncates: the sum of n products is off by
+ * up to about n/16 * 2^-23 of the sum of their magnitudes, which shows only when y is fp32); the epilogue is fp32
+ * with one rounding to y's type.  The activations use the hardware's exponential and reciprocal (relative error
+ * about 1e-6) and for RR_ACT_GELU Abramowitz and Stegun 7.1.26 (absolute error of Phi below 1e-6).
+ * Results repeat bit for bit.  M == 0 does nothing.
+ *
+ * rr_linear_bwd, for given dy [M,N] (dev bf16, pitch lddy):
+ *     dz = D(dy) act'(z),   dx = dz W,   dW = dz^T x,   dbias = sum over the tokens of dz   (dresidual is dy itself)
+ *   z, x, W, rng, p, act as in the forward pass (z NULL with RR_ACT_NONE); x is not read when dW is NULL, nor W
+ *   when dx is NULL
+ *   dx [M,K] type dx_dtype, dW [N,K] (dense) type dw_dtype, dbias [N] fp32: each may be NULL when not wanted
+ *   workspace dev, >= bwd_bytes, 256-byte aligned
+ * dz is rounded to bf16 between the two steps (without an activation that loses nothing: the dropout factor is applied behind
+ * the products); dbias is summed from the unrounded values in a fixed order.  M == 0 sets dW and dbias to zero, or leaves them
+ * under RR_ADD_DW.
+ * Both return RR_ERR_INVALID_ARG for a shape outside the limits, a pitch below the width, a pointer that is missing or not 16-byte
+ * aligned.  Calls that share a workspace must not overlap on the GPU.
+ */
+rr_status rr_linear_workspace_bytes(int M, int N, int K, size_t *fwd_bytes, size_t *bwd_bytes);
+rr_status rr_linear_fwd(const rr_linear_shape *s /* host */, const void *x, const void *W, const void *bias,
+                        const void *residual, const void *rng /* dev */, void *y, void *z, void *workspace,
+                        size_t workspace_bytes, void *stream);
+rr_status rr_linear_bwd(const rr_linear_shape *s /* host */, const void *dy, const void *x, const void *W, const void *z,
+                        const void *rng /* dev */, void *dx, void *dW, float *dbias, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * rr_balance_fwd -- the balance loss over ALL k choices of a token, per segment of tokens (a sequence of a batch), with a
+ * token mask, the per-expert counts it is made of, and the z-loss (rr_aux_loss_fwd is the paper's form: first
+ * choices, one segment, every token).  Segment s holds the tokens [s T/S, (s+1) T/S); n_s of them are live, n is
+ * the sum of the n_s, S' the number of segments with a live token:
+ *     count_se = #{ (i, r) : i live in s, r < k, choice r of token i is e },    f_se = count_se / (k n_s)
+ *     P_se     = (1/n_s) sum over the live i of s of softmax(a_i)_e,            lse_i = log sum_e exp(a_ie)
+ *     loss[0]  = alpha E / S' sum_s sum_e f_se P_se   (alpha at uniform scores)
+ *     loss[1]  = beta / n sum over the live i of lse_i^2
+ *   logits [T,E] fp32 dev, 16-byte aligned; finite where live
+ *   topk_expert dev i32, choice r of token i at i*stride + r (pass the routing table with stride = k+1); a choice
+ *                outside 0..E-1 of a live token is not counted and latches RR_ERR_INVALID_ARG in the workspace header
+ *   live [T] u8 dev, or NULL for all tokens: 0 = not a token (padding); what its row of logits and its choices hold
+ *                does not matter
+ *   loss [2] fp32, count [S,E] i32, n_live [S] i32, P [S,E] fp32 dev, overwritten.  A segment without a live
+ *                token has zeros and no part in the mean; without any the losses are 0.
+ *   workspace dev, >= rr_balance_workspace_bytes, 256-byte aligned; its first 256 bytes are zero when first used
+ * 1 <= E <= 256, 1 <= k <= 8, k <= stride, 1 <= S, T % S == 0.  fp32 arithmetic, sums in a fixed order.  T == 0 is accepted.
+ * rr_balance_bwd, with the counts held constant:
+ *     dL/da_ij = scale live_i g_ij ( alpha E / (S' n_s) (f_sj - sum_e f_se g_ie) + 2 beta / n lse_i ),  g_i = softmax(a_i)
+ *   count, n_live as rr_balance_fwd wrote them; live, alpha, beta as there; scale a host value
+ *   dlogits [T,E] fp32 dev: overwritten (zero where not live) when accumulate == 0, else added to (rows that are not
+ *                live are left alone).  One kernel, no workspace.
+ */
+rr_status rr_balance_workspace_bytes(int T, int E, int S, size_t *bytes);
+rr_status rr_balance_fwd(int T, int E, int k, int stride, int S, const float *logits, const int32_t *topk_expert,
+                         const uint8_t *live, float alpha, float beta, float *loss, int32_t *count, int32_t *n_live,
+                         float *P, void *workspace, size_t workspace_bytes, void *stream);
+rr_status rr_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
+                         const uint8_t *live, float alpha, float beta, float scale, int accumulate, float *dlogits,
+                         void *stream);
+
+/*
  * rr_check -- synchronise `stream`, then return the status word latched in `workspace`
  * (RR_OK, RR_ERR_NONFINITE, RR_ERR_TIMEOUT) or RR_ERR_CUDA if the stream reports an error.
  * The first error latched since the last rr_check is kept; rr_check clears it after reporting.

@@ -10,7 +10,8 @@ _BINDING = ("IR", "FR", "SCORE", "FR_SOFTMAX", "LOCAL_CAP", "GRAD_EXACT", "BF16"
             "alloc_workspace", "route_workspace_bytes", "route", "route_noalloc", "check", "moe_workspace_bytes",
             "moe_fwd", "moe_bwd", "gate_workspace_bytes", "gate_fwd", "gate_bwd", "aux_workspace_bytes",
             "aux_loss_fwd", "aux_loss_bwd", "gate_route", "gate_route_workspace_bytes", "route_loss", "route_loss_workspace_bytes", "test_set_wait_limit_ns", "Trace", "status_string", "lib",
-            "LIB_PATH")
+            "LIB_PATH", "ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_GELU_TANH", "ACT_SILU", "ADD_DX", "ADD_DW", "dropout_fwd", "dropout_bwd",
+            "linear_workspace_bytes", "linear_fwd", "linear_bwd", "balance_workspace_bytes", "balance_fwd", "balance_bwd")
 
 
 def __getattr__(name):

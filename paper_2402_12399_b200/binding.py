@@ -20,6 +20,13 @@ FR_SOFTMAX = 8  # FR ranks nominees by softmax value instead of raw logit (needs
 GRAD_EXACT = 1
 BF16 = 0
 F32 = 1
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU = 2
+ACT_GELU_TANH = 3
+ACT_SILU = 4
+ADD_DX = 1
+ADD_DW = 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librr.so")
@@ -37,6 +44,12 @@ class _CShape(C.Structure):
     _fields_ = [("T", C.c_int32), ("E", C.c_int32), ("k", C.c_int32), ("capacity", C.c_int32),
                 ("G", C.c_int32), ("d", C.c_int32), ("d_ff", C.c_int32), ("dtype", C.c_int32),
                 ("mode", C.c_uint32), ("flags", C.c_uint32), ("trace", C.c_void_p)]
+
+
+class _CLinear(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "act", "y_dtype", "dx_dtype", "dw_dtype")] + \
+        [("flags", C.c_uint32), ("p", C.c_float)] + \
+        [(n, C.c_int64) for n in ("ldx", "ldr", "ldy", "ldz", "lddy", "lddx")]
 
 
 class RRError(RuntimeError):
@@ -85,6 +98,14 @@ def lib():
             [C.c_size_t, C.c_void_p]
         L.rr_aux_loss_bwd.argtypes = [C.c_int] * 2 + [C.c_void_p] * 2 + [C.c_float] * 2 + [C.c_int, C.c_void_p,
                                                                                              C.c_void_p]
+        L.rr_dropout_fwd.argtypes = [C.c_longlong, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 3
+        L.rr_dropout_bwd.argtypes = [C.c_longlong, C.c_int, C.c_int, C.c_void_p, C.c_float, C.c_void_p, C.c_int] + [C.c_void_p] * 2
+        L.rr_linear_workspace_bytes.argtypes = [C.c_int] * 3 + [C.POINTER(C.c_size_t)] * 2
+        L.rr_linear_fwd.argtypes = [C.POINTER(_CLinear)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        L.rr_linear_bwd.argtypes = [C.POINTER(_CLinear)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        L.rr_balance_workspace_bytes.argtypes = [C.c_int] * 3 + [C.POINTER(C.c_size_t)]
+        L.rr_balance_fwd.argtypes = [C.c_int] * 5 + [C.c_void_p] * 3 + [C.c_float] * 2 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        L.rr_balance_bwd.argtypes = [C.c_int] * 4 + [C.c_void_p] * 4 + [C.c_float] * 3 + [C.c_int, C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -436,4 +457,233 @@ def aux_loss_bwd(logits: torch.Tensor, f: torch.Tensor, alpha: float, scale: flo
     assert dlogits.dtype == torch.float32 and dlogits.is_contiguous() and dlogits.shape == (T, E)
     _ok(lib().rr_aux_loss_bwd(T, E, _ptr(logits), _ptr(f), alpha, scale, int(accumulate), _ptr(dlogits), _stream()),
         "rr_aux_loss_bwd")
+    return dlogits
+
+
+# ---- the parts of a block around the expert layer ------------------------------------------------------
+# Their calls are short next to the interpreter's time per call, so the checks and the marshalling below are kept lean.
+
+_TYPE_CODE = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _code(t: torch.Tensor, what: str) -> int:
+    code = _TYPE_CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+def _on_device(*tensors) -> None:
+    """Every tensor lies on the current device, whose current stream the call uses."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, but the call runs on the current device cuda:{here}")
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _check_rng(rng, p: float) -> None:
+    if rng is None:
+        if p:
+            raise ValueError("dropout needs rng: two int64 on the device, {seed, offset}")
+    elif rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous():
+        raise TypeError("rng is two contiguous int64 (or uint64), {seed, offset}")
+
+
+def _same_shape(t, shape, what):
+    if t is not None and t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def dropout_fwd(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch.Tensor | None = None,
+                out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """rr_dropout_fwd; returns residual + dropout(x) in `out` (type: out's, else out_dtype, else the residual's, else x's).
+    `rng` is {seed, offset}, two int64 on the device; the mask is a function of it and the flat element index."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
+    _on_device(x, residual, rng, out)
+    _check_rng(rng, p)
+    _same_shape(out, x.shape, "out")
+    _same_shape(residual, x.shape, "residual")
+    if not (x.is_contiguous() and out.is_contiguous() and (residual is None or residual.is_contiguous())):
+        raise ValueError("dropout takes contiguous tensors")
+    if residual is not None and residual.dtype != out.dtype:
+        raise TypeError(f"residual is {residual.dtype}, the result {out.dtype}")
+    _ok(lib().rr_dropout_fwd(x.numel(), _code(x, "x"), _code(out, "out"), x.data_ptr(), _at(residual), p, _at(rng), out.data_ptr(),
+                             _raw_stream()), "rr_dropout_fwd")
+    return out
+
+
+def dropout_bwd(dy: torch.Tensor, p: float, rng: torch.Tensor | None, out: torch.Tensor | None = None,
+                out_dtype: torch.dtype | None = None, accumulate: bool = False) -> torch.Tensor:
+    """rr_dropout_bwd; returns dropout's gradient of x (type: out's, else out_dtype, else dy's); with `accumulate` it is
+    added to `out`.  The gradient of the residual is dy."""
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty(dy.shape, dtype=out_dtype or dy.dtype, device=dy.device)
+    _on_device(dy, rng, out)
+    _check_rng(rng, p)
+    _same_shape(out, dy.shape, "out")
+    if not (dy.is_contiguous() and out.is_contiguous()):
+        raise ValueError("dropout takes contiguous tensors")
+    _ok(lib().rr_dropout_bwd(dy.numel(), _code(dy, "dy"), _code(out, "out"), dy.data_ptr(), p, _at(rng), int(accumulate), out.data_ptr(),
+                             _raw_stream()), "rr_dropout_bwd")
+    return out
+
+
+def linear_workspace_bytes(M: int, N: int, K: int):
+    """(fwd workspace bytes, bwd workspace bytes) of the linear layer."""
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _ok(lib().rr_linear_workspace_bytes(M, N, K, C.byref(a), C.byref(b)), "rr_linear_workspace_bytes")
+    return a.value, b.value
+
+
+def _pitch(t, rows: int, cols: int, what: str) -> int:
+    """Elements between the rows of a [rows, cols] matrix whose columns lie together (0: not given)."""
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    row, col = t.stride()
+    if col != 1:
+        raise ValueError(f"{what} must be row-major, its columns are {col} elements apart")
+    if rows > 1 and row < cols:
+        raise ValueError(f"the rows of {what} overlap")
+    return row if rows > 1 else 0
+
+
+def _bf16(**tensors):
+    for what, t in tensors.items():
+        if t is not None and t.dtype != torch.bfloat16:
+            raise TypeError(f"{what} must be bfloat16, got {t.dtype}")
+
+
+def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+               act: int = ACT_NONE, p: float = 0.0, rng: torch.Tensor | None = None, out: torch.Tensor | None = None,
+               z: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """rr_linear_fwd; returns y [M,N] = residual + dropout(act(x W^T + bias)) (type: out's, else out_dtype, else the residual's,
+    else bf16).  Pass `z`, a bf16 [M,N] buffer, to keep the pre-activations for linear_bwd.  x, residual, out and z may be views
+    whose rows lie apart."""
+    M, K = x.shape
+    N = W.shape[0]
+    if out is None:
+        out = torch.empty(M, N, dtype=out_dtype or (torch.bfloat16 if residual is None else residual.dtype), device=x.device)
+    if workspace is None:
+        workspace = alloc_workspace(linear_workspace_bytes(M, N, K)[0], x.device)
+    _on_device(x, W, bias, residual, rng, out, z, workspace)
+    _bf16(x=x, W=W, bias=bias, z=z)
+    _check_rng(rng, p)
+    _same_shape(W, (N, K), "W")
+    _same_shape(bias, (N,), "bias")
+    if not W.is_contiguous() or (bias is not None and not bias.is_contiguous()):
+        raise ValueError("W and bias must be contiguous")
+    if residual is not None and residual.dtype != out.dtype:
+        raise TypeError(f"residual is {residual.dtype}, the result {out.dtype}")
+    s = _CLinear(M, N, K, act, _code(out, "out"), 0, 0, 0, p, _pitch(x, M, K, "x"), _pitch(residual, M, N, "residual"),
+                 _pitch(out, M, N, "out"), _pitch(z, M, N, "z"), 0, 0)
+    _ok(lib().rr_linear_fwd(C.byref(s), x.data_ptr(), W.data_ptr(), _at(bias), _at(residual), _at(rng), out.data_ptr(), _at(z),
+                            workspace.data_ptr(), workspace.numel(), _raw_stream()), "rr_linear_fwd")
+    out._workspace = workspace
+    return out
+
+
+def linear_bwd(dy: torch.Tensor, x: torch.Tensor | None, W: torch.Tensor, z: torch.Tensor | None = None, act: int = ACT_NONE,
+               p: float = 0.0, rng: torch.Tensor | None = None, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None,
+               dbias: torch.Tensor | None = None, add_dx: bool = False, add_dw: bool = False, workspace: torch.Tensor | None = None):
+    """rr_linear_bwd; writes the gradients whose buffers are given -- dx [M,K], dw [N,K] (bf16 or fp32), dbias [N] fp32 -- and
+    returns (dx, dw, dbias).  With add_dx / add_dw (dw and dbias) they are added to what the buffers hold.  The gradient of the
+    residual is dy."""
+    M, N = dy.shape
+    K = W.shape[1]
+    if workspace is None:
+        workspace = alloc_workspace(linear_workspace_bytes(M, N, K)[1], dy.device)
+    _on_device(dy, x, W, z, rng, dx, dw, dbias, workspace)
+    _bf16(dy=dy, x=x, W=W, z=z)
+    _check_rng(rng, p)
+    _same_shape(W, (N, K), "W")
+    _same_shape(dw, (N, K), "dw")
+    _same_shape(dbias, (N,), "dbias")
+    if not W.is_contiguous() or (dw is not None and not dw.is_contiguous()) or (dbias is not None and not dbias.is_contiguous()):
+        raise ValueError("W, dw and dbias must be contiguous")
+    if dbias is not None and dbias.dtype != torch.float32:
+        raise TypeError(f"dbias must be float32, got {dbias.dtype}")
+    s = _CLinear(M, N, K, act, 0, 0 if dx is None else _code(dx, "dx"), 0 if dw is None else _code(dw, "dw"),
+                 (ADD_DX if add_dx else 0) | (ADD_DW if add_dw else 0), p, _pitch(x, M, K, "x"), 0, 0, _pitch(z, M, N, "z"),
+                 _pitch(dy, M, N, "dy"), _pitch(dx, M, K, "dx"))
+    _ok(lib().rr_linear_bwd(C.byref(s), dy.data_ptr(), _at(x), W.data_ptr(), _at(z), _at(rng), _at(dx), _at(dw), _at(dbias),
+                            workspace.data_ptr(), workspace.numel(), _raw_stream()), "rr_linear_bwd")
+    for t in (dx, dw, dbias):
+        if t is not None:
+            t._workspace = workspace
+    return dx, dw, dbias
+
+
+def balance_workspace_bytes(T: int, E: int, segments: int = 1) -> int:
+    """Workspace bytes of balance_fwd."""
+    a = C.c_size_t(0)
+    _ok(lib().rr_balance_workspace_bytes(T, E, segments, C.byref(a)), "rr_balance_workspace_bytes")
+    return a.value
+
+
+def _check_scores(logits, live):
+    if logits.dtype != torch.float32 or logits.dim() != 2 or not logits.is_contiguous():
+        raise TypeError("logits is a contiguous float32 [T,E]")
+    if live is not None and (live.dtype not in (torch.uint8, torch.bool) or live.numel() != logits.shape[0] or not live.is_contiguous()):
+        raise TypeError("live is a contiguous uint8 or bool with one element per token")
+
+
+def balance_fwd(logits: torch.Tensor, topk_expert: torch.Tensor, k: int, alpha: float, beta: float = 0.0, segments: int = 1,
+                live: torch.Tensor | None = None, workspace: torch.Tensor | None = None, out=None):
+    """rr_balance_fwd; returns (loss [2] = balance loss and z-loss, count [S,E] i32, n_live [S] i32, P [S,E]).  `topk_expert` is the
+    routing table [T,k+1] (any int32 [T,n >= k] will do); `live` marks the tokens that count."""
+    T, E = logits.shape
+    if workspace is None:
+        workspace = alloc_workspace(balance_workspace_bytes(T, E, segments), logits.device)
+    if out is None:
+        dev = logits.device
+        out = (torch.empty(2, dtype=torch.float32, device=dev), torch.empty(segments, E, dtype=torch.int32, device=dev),
+               torch.empty(segments, dtype=torch.int32, device=dev), torch.empty(segments, E, dtype=torch.float32, device=dev))
+    loss, count, n_live, P = out
+    _on_device(logits, topk_expert, live, workspace, loss, count, n_live, P)
+    _check_scores(logits, live)
+    if topk_expert.dtype != torch.int32 or topk_expert.dim() != 2 or topk_expert.shape[0] != T or not topk_expert.is_contiguous():
+        raise TypeError("topk_expert is a contiguous int32 [T,n]")
+    for t, shape, dtype in ((loss, (2,), torch.float32), (count, (segments, E), torch.int32), (n_live, (segments,), torch.int32),
+                            (P, (segments, E), torch.float32)):
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError(f"out: expected contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    _ok(lib().rr_balance_fwd(T, E, k, topk_expert.shape[1], segments, logits.data_ptr(), topk_expert.data_ptr(), _at(live), alpha, beta,
+                             loss.data_ptr(), count.data_ptr(), n_live.data_ptr(), P.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                             _raw_stream()), "rr_balance_fwd")
+    loss._workspace = workspace
+    return out
+
+
+def balance_bwd(logits: torch.Tensor, count: torch.Tensor, n_live: torch.Tensor, k: int, alpha: float, beta: float = 0.0,
+                scale: float = 1.0, live: torch.Tensor | None = None, dlogits: torch.Tensor | None = None,
+                accumulate: bool = False) -> torch.Tensor:
+    """rr_balance_bwd; writes (or, with accumulate, adds) the gradient of scale * (loss[0] + loss[1]) into `dlogits` [T,E]."""
+    T, E = logits.shape
+    if dlogits is None:
+        if accumulate:
+            raise ValueError("accumulate needs dlogits")
+        dlogits = torch.empty(T, E, dtype=torch.float32, device=logits.device)
+    _on_device(logits, count, n_live, live, dlogits)
+    _check_scores(logits, live)
+    S = n_live.numel()
+    if count.dtype != torch.int32 or count.shape != (S, E) or not count.is_contiguous() or n_live.dtype != torch.int32 or \
+            not n_live.is_contiguous():
+        raise TypeError("count and n_live are what balance_fwd returned")
+    if dlogits.dtype != torch.float32 or dlogits.shape != (T, E) or not dlogits.is_contiguous():
+        raise TypeError("dlogits is a contiguous float32 [T,E]")
+    _ok(lib().rr_balance_bwd(T, E, k, S, logits.data_ptr(), count.data_ptr(), n_live.data_ptr(), _at(live), alpha, beta, scale,
+                             int(accumulate), dlogits.data_ptr(), _raw_stream()), "rr_balance_bwd")
     return dlogits

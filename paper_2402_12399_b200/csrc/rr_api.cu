@@ -383,6 +383,174 @@ rr_status rr_aux_loss_bwd(int T, int E, const float *logits, const float *f, flo
     return rr::launch_aux_bwd(T, E, logits, f, coef, accumulate ? 1 : 0, dlogits, static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+
+bool is_dtype(int t) { return t == RR_BF16 || t == RR_F32; }
+
+// probability and generator state
+bool check_dropout(float p, const void *rng)
+{
+    if (!(p >= 0.0f && p <= 1.0f)) return false;
+    if ((double)p * 65536.0 + 0.5 < 1.0) return true;  // below half a step: no dropout, `rng` is not read
+    return rng && aligned(rng, 16);
+}
+
+rr_status check_dropout_call(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p, const void *rng,
+                             const void *y)
+{
+    if (n < 0 || !is_dtype(x_dtype) || !is_dtype(y_dtype) || !check_dropout(p, rng)) return RR_ERR_INVALID_ARG;
+    if (n == 0) return RR_OK;
+    if (!x || !y || !aligned(x, 16) || !aligned(y, 16) || !aligned(residual, 16)) return RR_ERR_INVALID_ARG;
+    if (x == y && x_dtype != y_dtype) return RR_ERR_INVALID_ARG;
+    return RR_OK;
+}
+
+}  // namespace
+
+rr_status rr_dropout_fwd(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p, const void *rng, void *y,
+                         void *stream)
+{
+    rr_status rc = check_dropout_call(n, x_dtype, y_dtype, x, residual, p, rng, y);
+    if (rc || n == 0) return rc;
+    return rr::launch_dropout(n, x_dtype, y_dtype, x, residual, p, rng, y, static_cast<cudaStream_t>(stream));
+}
+
+rr_status rr_dropout_bwd(long long n, int dy_dtype, int dx_dtype, const void *dy, float p, const void *rng, int accumulate, void *dx,
+                         void *stream)
+{
+    rr_status rc = check_dropout_call(n, dy_dtype, dx_dtype, dy, nullptr, p, rng, dx);
+    if (rc || n == 0) return rc;
+    return rr::launch_dropout(n, dy_dtype, dx_dtype, dy, accumulate ? dx : nullptr, p, rng, dx, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+
+rr_status check_linear_sizes(int M, int N, int K)
+{
+    return M < 0 || N < 8 || K < 8 || N % 8 || K % 8 ? RR_ERR_INVALID_ARG : RR_OK;
+}
+
+// a pitch of `width` elements of `size` bytes: 0 becomes the width; rows stay 16-byte aligned and addressable by TMA
+bool fill_pitch(int64_t *ld, int width, int size)
+{
+    if (*ld == 0) *ld = width;
+    return *ld >= width && *ld % (16 / size) == 0 && *ld * size < (1ll << 40);
+}
+
+rr_status check_linear(const rr_linear_shape *in, rr_linear_shape *s)
+{
+    if (!in) return RR_ERR_INVALID_ARG;
+    *s = *in;
+    rr_status rc = check_linear_sizes(s->M, s->N, s->K);
+    if (rc) return rc;
+    if (s->act < RR_ACT_NONE || s->act > RR_ACT_SILU || !is_dtype(s->y_dtype) || !is_dtype(s->dx_dtype) || !is_dtype(s->dw_dtype))
+        return RR_ERR_INVALID_ARG;
+    if (s->flags & ~(RR_ADD_DX | RR_ADD_DW)) return RR_ERR_INVALID_ARG;
+    const int ys = s->y_dtype == RR_F32 ? 4 : 2, xs = s->dx_dtype == RR_F32 ? 4 : 2;
+    if (!fill_pitch(&s->ldx, s->K, 2) || !fill_pitch(&s->ldr, s->N, ys) || !fill_pitch(&s->ldy, s->N, ys) || !fill_pitch(&s->ldz, s->N, 2) ||
+        !fill_pitch(&s->lddy, s->N, 2) || !fill_pitch(&s->lddx, s->K, xs))
+        return RR_ERR_INVALID_ARG;
+    return RR_OK;
+}
+
+}  // namespace
+
+rr_status rr_linear_workspace_bytes(int M, int N, int K, size_t *fwd_bytes, size_t *bwd_bytes)
+{
+    rr_status rc = check_linear_sizes(M, N, K);
+    if (rc) return rc;
+    if (fwd_bytes) *fwd_bytes = rr::linear_fwd_workspace();
+    if (bwd_bytes) *bwd_bytes = rr::linear_bwd_workspace(M, N);
+    return RR_OK;
+}
+
+rr_status rr_linear_fwd(const rr_linear_shape *shape, const void *x, const void *W, const void *bias, const void *residual, const void *rng,
+                        void *y, void *z, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rr_linear_shape s;
+    rr_status rc = check_linear(shape, &s);
+    if (rc) return rc;
+    if (!check_dropout(s.p, rng)) return RR_ERR_INVALID_ARG;
+    if (s.M == 0) return RR_OK;
+    if (!x || !W || !y || !workspace) return RR_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(y, 16) || !aligned(z, 16) ||
+        !aligned(workspace, 256))
+        return RR_ERR_INVALID_ARG;
+    if (residual == y && s.ldr != s.ldy) return RR_ERR_INVALID_ARG;
+    if (rr::linear_fwd_workspace() > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_linear_fwd(s, x, W, bias, residual, rng, y, z, workspace, static_cast<cudaStream_t>(stream));
+}
+
+rr_status rr_linear_bwd(const rr_linear_shape *shape, const void *dy, const void *x, const void *W, const void *z, const void *rng, void *dx,
+                        void *dW, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rr_linear_shape s;
+    rr_status rc = check_linear(shape, &s);
+    if (rc) return rc;
+    if (!check_dropout(s.p, rng)) return RR_ERR_INVALID_ARG;
+    if (!aligned(dx, 16) || !aligned(dW, 16) || !aligned(dbias, 16)) return RR_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.M == 0) {  // no tokens: the gradients of the parameters are zero
+        const size_t wbytes = (size_t)s.N * s.K * (s.dw_dtype == RR_F32 ? 4 : 2);
+        if (!(s.flags & RR_ADD_DW) && ((dW && cudaMemsetAsync(dW, 0, wbytes, st) != cudaSuccess) ||
+                                       (dbias && cudaMemsetAsync(dbias, 0, (size_t)s.N * 4, st) != cudaSuccess)))
+            return RR_ERR_CUDA;
+        return RR_OK;
+    }
+    if (!dy || !workspace || (dW && !x) || (dx && !W) || (s.act != RR_ACT_NONE && !z)) return RR_ERR_INVALID_ARG;
+    if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(W, 16) || !aligned(z, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    if (rr::linear_bwd_workspace(s.M, s.N) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_linear_bwd(s, dy, x, W, z, rng, dx, dW, dbias, workspace, st);
+}
+
+namespace {
+
+rr_status check_balance(int T, int E, int k, int S)
+{
+    return T < 0 || E < 1 || E > rr::kMaxE || k < 1 || k > rr::kMaxK || S < 1 || T % S ? RR_ERR_INVALID_ARG : RR_OK;
+}
+
+}  // namespace
+
+rr_status rr_balance_workspace_bytes(int T, int E, int S, size_t *bytes)
+{
+    rr_status rc = check_balance(T, E, 1, S);
+    if (rc || !bytes) return RR_ERR_INVALID_ARG;
+    *bytes = rr::balance_workspace(T, E, S);
+    return RR_OK;
+}
+
+rr_status rr_balance_fwd(int T, int E, int k, int stride, int S, const float *logits, const int32_t *topk_expert, const uint8_t *live,
+                         float alpha, float beta, float *loss, int32_t *count, int32_t *n_live, float *P, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    rr_status rc = check_balance(T, E, k, S);
+    if (rc) return rc;
+    if (stride < k || !loss || !count || !n_live || !P) return RR_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        const size_t n = (size_t)S * E * 4;
+        if (cudaMemsetAsync(loss, 0, 8, st) != cudaSuccess || cudaMemsetAsync(count, 0, n, st) != cudaSuccess ||
+            cudaMemsetAsync(n_live, 0, (size_t)S * 4, st) != cudaSuccess || cudaMemsetAsync(P, 0, n, st) != cudaSuccess)
+            return RR_ERR_CUDA;
+        return RR_OK;
+    }
+    if (!logits || !topk_expert || !workspace || !aligned(logits, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    if (rr::balance_workspace(T, E, S) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_balance_fwd(T, E, k, stride, S, logits, topk_expert, live, alpha, beta, loss, count, n_live, P, workspace, st);
+}
+
+rr_status rr_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live, const uint8_t *live,
+                         float alpha, float beta, float scale, int accumulate, float *dlogits, void *stream)
+{
+    rr_status rc = check_balance(T, E, k, S);
+    if (rc || T == 0) return rc;
+    if (!logits || !count || !n_live || !dlogits || !aligned(logits, 16) || !aligned(dlogits, 16)) return RR_ERR_INVALID_ARG;
+    const float coef_b = (float)((double)scale * alpha * E), coef_z = (float)(2.0 * scale * beta);
+    return rr::launch_balance_bwd(T, E, k, S, logits, count, n_live, live, coef_b, coef_z, accumulate ? 1 : 0, dlogits,
+                                  static_cast<cudaStream_t>(stream));
+}
+
 rr_status rr_check(const void *workspace, void *stream)
 {
     if (!workspace) return RR_ERR_INVALID_ARG;

@@ -8,6 +8,7 @@
 // Column sums are carried per lane over a contiguous slab of tokens, then added over the groups of a
 // warp, the warps of a block and the blocks in a fixed order: the result repeats bit for bit.
 #include "rr_ffn.cuh"
+#include "rr_rows.cuh"
 
 namespace rr {
 
@@ -18,30 +19,6 @@ constexpr int kAuxWarps = kAuxThreads / 32;
 constexpr int kAuxMaxBlocks = 1184;  // 8 per SM
 constexpr int kFwdMaxBlocks = 592;   // forward: 4 per SM (the second kernel's one block reads a row per block)
 constexpr int kFinalThreads = 1024;
-
-template <int GS>
-__device__ __forceinline__ float group_max(float v)
-{
-#pragma unroll
-    for (int o = GS / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
-template <int GS>
-__device__ __forceinline__ float group_sum(float v)
-{
-#pragma unroll
-    for (int o = GS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-// Which columns a lane keeps.  Vector layout (E a multiple of 4): float4 pieces, piece q of lane gl
-// covers columns q*4*GS + 4*gl .. + 3, so one load instruction of a group reads 16*GS contiguous bytes.
-// Scalar layout (any E): element c is column c*GS + gl.
-template <int GS, bool VEC>
-__device__ __forceinline__ int column_of(int c, int gl)
-{
-    return VEC ? (c >> 2) * (4 * GS) + 4 * gl + (c & 3) : c * GS + gl;
-}
 
 // softmax of one token over the group's lanes; a lane without a token (ok == false) takes part in
 // the shuffles and gets zeros
@@ -248,24 +225,6 @@ __global__ void __launch_bounds__(kAuxThreads) k_aux_bwd(const float *__restrict
     }
 }
 
-// Lane layout for E experts: with E a multiple of 4 a lane keeps up to eight columns as float4 pieces
-// and the group is as small as that allows (few shuffle steps: the reductions over the group, not the
-// loads, bound these kernels otherwise); any other E takes scalar columns over up to 32 lanes.
-struct Layout {
-    bool vec;
-    int gs, cpl;
-};
-Layout layout_of(int E)
-{
-    int epad = 1;
-    while (epad < E) epad <<= 1;
-    if (E % 4 == 0) {
-        const int cpl = epad < 8 ? 4 : 8;
-        return {true, epad / cpl, cpl};
-    }
-    return {false, epad < 32 ? epad : 32, epad <= 32 ? 1 : epad / 32};
-}
-
 int aux_blocks(int T, int E)
 {
     const int per_pass = 2 * kAuxWarps * (32 / layout_of(E).gs);  // tokens a block takes per loop pass
@@ -329,34 +288,6 @@ rr_status run_bwd(int T, int E, const float *logits, const float *f, float coef,
     return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 
-// calls F<GS, CPL, VEC>::run(args...) for the layout of E
-#define RR_AUX_DISPATCH(FN, ...)                                                   \
-    do {                                                                           \
-        const Layout l = layout_of(E);                                             \
-        if (l.vec) {                                                               \
-            if (l.cpl == 4) return FN<1, 4, true>(__VA_ARGS__);                    \
-            switch (l.gs) {                                                        \
-            case 1: return FN<1, 8, true>(__VA_ARGS__);                            \
-            case 2: return FN<2, 8, true>(__VA_ARGS__);                            \
-            case 4: return FN<4, 8, true>(__VA_ARGS__);                            \
-            case 8: return FN<8, 8, true>(__VA_ARGS__);                            \
-            case 16: return FN<16, 8, true>(__VA_ARGS__);                          \
-            default: return FN<32, 8, true>(__VA_ARGS__);                          \
-            }                                                                      \
-        }                                                                          \
-        if (l.cpl == 2) return FN<32, 2, false>(__VA_ARGS__);                      \
-        if (l.cpl == 4) return FN<32, 4, false>(__VA_ARGS__);                      \
-        if (l.cpl == 8) return FN<32, 8, false>(__VA_ARGS__);                      \
-        switch (l.gs) {                                                            \
-        case 1: return FN<1, 1, false>(__VA_ARGS__);                               \
-        case 2: return FN<2, 1, false>(__VA_ARGS__);                               \
-        case 4: return FN<4, 1, false>(__VA_ARGS__);                               \
-        case 8: return FN<8, 1, false>(__VA_ARGS__);                               \
-        case 16: return FN<16, 1, false>(__VA_ARGS__);                             \
-        default: return FN<32, 1, false>(__VA_ARGS__);                             \
-        }                                                                          \
-    } while (0)
-
 }  // namespace
 
 size_t aux_workspace(int T, int E) { return aux_layout(nullptr, T, E, nullptr); }
@@ -366,13 +297,17 @@ rr_status launch_aux_fwd(int T, int E, int stride, const float *logits, const in
 {
     AuxScratch a;
     aux_layout(workspace, T, E, &a);
-    RR_AUX_DISPATCH(run_fwd, T, E, stride, logits, first, alpha, loss, f, P, a, st);
+    rr_status rc = RR_OK;
+    RR_ROWS_DISPATCH(rc = run_fwd, E, T, E, stride, logits, first, alpha, loss, f, P, a, st);
+    return rc;
 }
 
 rr_status launch_aux_bwd(int T, int E, const float *logits, const float *f, float coef, int accumulate,
                          float *dlogits, cudaStream_t st)
 {
-    RR_AUX_DISPATCH(run_bwd, T, E, logits, f, coef, accumulate, dlogits, st);
+    rr_status rc = RR_OK;
+    RR_ROWS_DISPATCH(rc = run_bwd, E, T, E, logits, f, coef, accumulate, dlogits, st);
+    return rc;
 }
 
 }  // namespace rr

@@ -1,0 +1,409 @@
+// Balance loss over all k choices of a router, per segment of tokens, with a token mask; per-expert counts;
+// the z-loss on the log of the softmax's denominator; and the gradient of both.  Segment s holds the tokens
+// [s L, (s+1) L); n_s of them are live (mask non-zero), n is the sum of the n_s, S' the number of segments with
+// a live token.
+//     count_se = #{ (i, r) : i live in s, r < k, choice r of i is e },   f_se = count_se / (k n_s)
+//     P_se     = (1/n_s) sum_{i live in s} g_ie,    g_i = softmax(a_i),   lse_i = log sum_e exp(a_ie)
+//     L_b = alpha E / S' sum_s sum_e f_se P_se,     L_z = beta / n sum_{i live} lse_i^2
+//     dL/da_ij = live_i g_ij ( alpha E / (S' n_s) (f_sj - sum_e f_se g_ie) + 2 beta / n lse_i )    (f constant)
+// One read of the scores forward, one read and one write (or read-modify-write) backward: HBM at sizes above L2,
+// launch latency below.  The row of a dead token is read and selected away (its load does not wait for the
+// mask), so what it holds -- NaN, infinities -- reaches no sum.  All sums are fp32 in a fixed order (counts are
+// integers), so the results repeat bit for bit.
+#include "rr_ffn.cuh"
+#include "rr_rows.cuh"
+
+namespace rr {
+
+namespace {
+
+constexpr int kBalThreads = 256;
+constexpr int kBalWarps = kBalThreads / 32;
+constexpr int kBalBlocks = 592;     // forward: blocks wanted, 4 per SM
+constexpr int kBalFinal = 512;      // threads of the second forward kernel
+constexpr int kBalBwdBlocks = 1184; // backward: 8 per SM
+
+// softmax of one row over the group's lanes and its log-sum-exp; a token that is not live takes part in the
+// shuffles with zeros
+template <int GS, int CPL, bool VEC>
+__device__ __forceinline__ void load_row(const float *__restrict__ a, bool in, int E, int gl, float (&g)[CPL])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int q = 0; q < CPL / 4; ++q) {
+            const int j = column_of<GS, true>(4 * q, gl);
+            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (in && j < E) v = __ldg(reinterpret_cast<const float4 *>(a + j));
+            g[4 * q] = v.x; g[4 * q + 1] = v.y; g[4 * q + 2] = v.z; g[4 * q + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            const int j = column_of<GS, false>(c, gl);
+            g[c] = (in && j < E) ? __ldg(a + j) : -INFINITY;
+        }
+    }
+}
+template <int GS, int CPL>
+__device__ __forceinline__ float softmax_lse(bool live, float (&g)[CPL])
+{
+    float m = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) m = fmaxf(m, g[c]);
+    m = group_max<GS>(m);
+    float z = 0.f;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) {
+        g[c] = live ? expf(g[c] - m) : 0.f;  // exp(-inf) = 0 for the columns past E
+        z += g[c];
+    }
+    z = group_sum<GS>(z);
+    const float inv = live ? 1.0f / z : 0.f;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) g[c] *= inv;
+    return live ? m + logf(z) : 0.f;
+}
+
+__device__ __forceinline__ bool is_live(const uint8_t *__restrict__ live, bool in, long long t)
+{
+    return in && (!live || __ldg(live + t) != 0);
+}
+
+struct BalShape {
+    int E, k, stride;
+    long long L;   // tokens of a segment
+    int S;         // segments
+    int cps;       // blocks per segment (forward)
+    int slab;      // tokens of a block (forward)
+};
+
+struct BalScratch {
+    Header *hdr;
+    float *partial;  // [S*cps][E] softmax sums
+    int *pcount;     // [S*cps][E] choices
+    float *plse;     // [S*cps] sums of lse^2
+    int *pn;         // [S*cps] live tokens
+    float *dot;      // [S] sum_e f P of each segment
+    float *slse;     // [S]
+    int *sn;         // [S]
+};
+
+// Forward, first kernel: block (s, c) adds up the tokens of its slab of segment s.
+template <int GS, int CPL, bool VEC>
+__global__ void __launch_bounds__(kBalThreads)
+k_balance_partial(const BalShape b, const float *__restrict__ logits, const int32_t *__restrict__ topk,
+                  const uint8_t *__restrict__ live, const BalScratch w)
+{
+    constexpr int TPW = 32 / GS;
+    __shared__ float red[kBalWarps][kMaxE];
+    __shared__ int cnt[kMaxE];
+    __shared__ float red_lse[kBalWarps];
+    __shared__ int red_n[kBalWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
+    for (int j = threadIdx.x; j < E; j += kBalThreads) cnt[j] = 0;
+    __syncthreads();
+    const int s = blockIdx.x / b.cps, c0 = blockIdx.x - s * b.cps;
+    const long long seg0 = s * b.L, t0 = seg0 + (long long)c0 * b.slab;
+    const long long t1 = min(seg0 + b.L, t0 + b.slab);
+    float acc[CPL] = {}, lse2 = 0.f;
+    int n = 0;
+    auto choices = [&](long long t) {
+        for (int r = gl; r < b.k; r += GS) {
+            const int e = __ldg(topk + t * b.stride + r);
+            if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+            else latch_status(&w.hdr->status, RR_ERR_INVALID_ARG);
+        }
+    };
+    for (long long base = t0 + warp * TPW; base < t1; base += 2 * kBalWarps * TPW) {  // two tokens in flight per group
+        const long long ta = base + grp, tb = ta + kBalWarps * TPW;
+        const bool ina = ta < t1, inb = tb < t1;
+        float ga[CPL], gb[CPL];
+        load_row<GS, CPL, VEC>(logits + (ina ? ta : 0) * E, ina, E, gl, ga);
+        load_row<GS, CPL, VEC>(logits + (inb ? tb : 0) * E, inb, E, gl, gb);
+        const bool la = is_live(live, ina, ta), lb = is_live(live, inb, tb);
+        if (la) choices(ta);
+        if (lb) choices(tb);
+        const float za = softmax_lse<GS, CPL>(la, ga), zb = softmax_lse<GS, CPL>(lb, gb);
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) acc[c] += la ? ga[c] : 0.f;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) acc[c] += lb ? gb[c] : 0.f;
+        lse2 += za * za;
+        lse2 += zb * zb;
+        n += (la ? 1 : 0) + (lb ? 1 : 0);
+    }
+    // groups of the warp, then warps of the block, in a fixed order
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) {
+#pragma unroll
+        for (int o = GS; o < 32; o <<= 1) acc[c] += __shfl_xor_sync(0xffffffffu, acc[c], o);
+        const int j = column_of<GS, VEC>(c, gl);
+        if (grp == 0 && j < E) red[warp][j] = acc[c];
+    }
+#pragma unroll
+    for (int o = GS; o < 32; o <<= 1) {
+        lse2 += __shfl_xor_sync(0xffffffffu, lse2, o);
+        n += __shfl_xor_sync(0xffffffffu, n, o);
+    }
+    if (lane == 0) { red_lse[warp] = lse2; red_n[warp] = n; }
+    __syncthreads();
+    for (int j = threadIdx.x; j < E; j += kBalThreads) {
+        float sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < kBalWarps; ++q) sum += red[q][j];
+        w.partial[(size_t)blockIdx.x * E + j] = sum;
+        w.pcount[(size_t)blockIdx.x * E + j] = cnt[j];
+    }
+    if (threadIdx.x == 0) {
+        float sum = 0.f;
+        int m = 0;
+        for (int q = 0; q < kBalWarps; ++q) { sum += red_lse[q]; m += red_n[q]; }
+        w.plse[blockIdx.x] = sum;
+        w.pn[blockIdx.x] = m;
+    }
+}
+
+// sums over the block in a fixed order; every thread gets the result
+template <class T>
+__device__ __forceinline__ T block_sum(T v, T *buf)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();  // (buf may still be read from the call before)
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    T sum = 0;
+    for (int q = 0; q < (int)(blockDim.x >> 5); ++q) sum += buf[q];
+    return sum;
+}
+
+// Forward, second kernel: block s adds up the blocks of segment s; the block that finishes last adds up the segments.
+__global__ void __launch_bounds__(kBalFinal)
+k_balance_final(const BalShape b, float alpha, float beta, const BalScratch w, float *loss, int *count, int *n_live, float *P)
+{
+    __shared__ float sp[kBalFinal];
+    __shared__ int sc[kBalFinal];
+    __shared__ float fbuf[32];
+    __shared__ int ibuf[32];
+    __shared__ int last;
+    const int s = blockIdx.x, E = b.E, tid = threadIdx.x;
+    int epad = 1;
+    while (epad < E) epad <<= 1;
+    const int R = kBalFinal / epad, r = tid / epad, j = tid % epad;
+    const size_t row0 = (size_t)s * b.cps;
+    float sum = 0.f;
+    int cnt = 0;
+    if (j < E) {
+#pragma unroll 4
+        for (int c = r; c < b.cps; c += R) {
+            sum += w.partial[(row0 + c) * E + j];
+            cnt += w.pcount[(row0 + c) * E + j];
+        }
+    }
+    float lse2 = 0.f;
+    int n = 0;
+    for (int c = tid; c < b.cps; c += kBalFinal) { lse2 += w.plse[row0 + c]; n += w.pn[row0 + c]; }
+    sp[tid] = sum;
+    sc[tid] = cnt;
+    n = block_sum(n, ibuf);  // (its barriers also order the writes to sp and sc)
+    lse2 = block_sum(lse2, fbuf);
+    float prod = 0.f;
+    if (tid < E) {
+        float tot = 0.f;
+        int m = 0;
+        for (int q = 0; q < R; ++q) { tot += sp[q * epad + tid]; m += sc[q * epad + tid]; }
+        const float p = n > 0 ? tot / (float)n : 0.f;
+        count[(size_t)s * E + tid] = m;
+        P[(size_t)s * E + tid] = p;
+        if (n > 0) prod = (float)m / ((float)b.k * (float)n) * p;
+    }
+    prod = block_sum(prod, fbuf);
+    if (tid == 0) {
+        n_live[s] = n;
+        w.dot[s] = prod;
+        w.slse[s] = lse2;
+        w.sn[s] = n;
+        __threadfence();
+        last = atomicAdd(&w.hdr->sync[8], 1) == b.S - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    float dots = 0.f, z = 0.f;
+    int segs = 0;
+    unsigned long long tokens = 0;  // (T is an int, so this fits; the sum of floats follows the same order every time)
+    for (int q = tid; q < b.S; q += kBalFinal) {
+        dots += __ldcg(w.dot + q);
+        z += __ldcg(w.slse + q);
+        const int m = __ldcg(w.sn + q);
+        tokens += m;
+        segs += m > 0 ? 1 : 0;
+    }
+    dots = block_sum(dots, fbuf);
+    z = block_sum(z, fbuf);
+    segs = block_sum(segs, ibuf);
+    const int live = block_sum((int)tokens, ibuf);
+    if (tid == 0) {
+        loss[0] = segs > 0 ? alpha * (float)E / (float)segs * dots : 0.f;
+        loss[1] = live > 0 ? beta / (float)live * z : 0.f;
+        w.hdr->sync[8] = 0;
+    }
+}
+
+// Backward: items of up to `slab` tokens of one segment, dealt to the blocks in turn.
+template <int GS, int CPL, bool VEC>
+__global__ void __launch_bounds__(kBalThreads)
+k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__restrict__ count, const int *__restrict__ n_live,
+              const uint8_t *__restrict__ live, float coef_b, float coef_z, int accumulate, float *dlogits)
+{
+    constexpr int TPW = 32 / GS;
+    __shared__ int ibuf[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
+    int segs = 0, tokens = 0;
+    for (int q = threadIdx.x; q < b.S; q += kBalThreads) {
+        const int m = __ldg(n_live + q);
+        tokens += m;
+        segs += m > 0 ? 1 : 0;
+    }
+    segs = block_sum(segs, ibuf);
+    tokens = block_sum(tokens, ibuf);
+    const float cz = tokens > 0 ? coef_z / (float)tokens : 0.f;
+    for (long long item = blockIdx.x; item < (long long)b.S * b.cps; item += gridDim.x) {
+        const int s = (int)(item / b.cps);
+        const long long seg0 = s * b.L, t0 = seg0 + (item - (long long)s * b.cps) * b.slab, t1 = min(seg0 + b.L, t0 + b.slab);
+        const int ns = __ldg(n_live + s);
+        const float inv = ns > 0 ? 1.0f / ((float)b.k * (float)ns) : 0.f;
+        const float cb = ns > 0 ? coef_b / ((float)segs * (float)ns) : 0.f;
+        float fj[CPL];
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            const int j = column_of<GS, VEC>(c, gl);
+            fj[c] = j < E ? (float)__ldg(count + (size_t)s * E + j) * inv : 0.f;
+        }
+        for (long long base = t0 + warp * TPW; base < t1; base += kBalWarps * TPW) {
+            const long long t = base + grp;
+            const bool in = t < t1;
+            float g[CPL];
+            load_row<GS, CPL, VEC>(logits + (in ? t : 0) * E, in, E, gl, g);
+            const bool l = is_live(live, in, t);
+            const float lse = softmax_lse<GS, CPL>(l, g);
+            float dot = 0.f;
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) dot += l ? fj[c] * g[c] : 0.f;
+            dot = group_sum<GS>(dot);
+            if (!in || (!l && accumulate)) continue;
+            float *o = dlogits + t * E;
+            const float zz = cz * lse;
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) g[c] = l ? g[c] * fmaf(cb, fj[c] - dot, zz) : 0.f;
+            if constexpr (VEC) {
+#pragma unroll
+                for (int q = 0; q < CPL / 4; ++q) {
+                    const int j = column_of<GS, true>(4 * q, gl);
+                    if (j >= E) continue;
+                    float4 *dst = reinterpret_cast<float4 *>(o + j);
+                    float4 v = make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
+                    if (accumulate) {
+                        const float4 old = *dst;
+                        v = make_float4(__fadd_rn(old.x, v.x), __fadd_rn(old.y, v.y), __fadd_rn(old.z, v.z), __fadd_rn(old.w, v.w));
+                    }
+                    *dst = v;
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) {
+                    const int j = column_of<GS, false>(c, gl);
+                    if (j < E) o[j] = accumulate ? __fadd_rn(o[j], g[c]) : g[c];
+                }
+            }
+        }
+    }
+}
+
+// Blocks per segment and tokens per block, for about `want` blocks in all and no fewer than `pass` tokens in one.
+BalShape balance_shape(int T, int E, int k, int stride, int S, int want, int pass)
+{
+    BalShape b;
+    b.E = E;
+    b.k = k;
+    b.stride = stride;
+    b.S = S;
+    b.L = T / S;
+    long long cps = want / S, most = (b.L + pass - 1) / pass;
+    if (cps > most) cps = most;
+    if (cps < 1) cps = 1;
+    b.slab = (int)((b.L + cps - 1) / cps);
+    if (b.slab < 1) b.slab = 1;
+    b.cps = (int)((b.L + b.slab - 1) / b.slab);
+    if (b.cps < 1) b.cps = 1;
+    return b;
+}
+BalShape forward_shape(int T, int E, int k, int stride, int S)
+{
+    return balance_shape(T, E, k, stride, S, kBalBlocks, 4 * kBalWarps * (32 / layout_of(E).gs));
+}
+
+size_t balance_layout(void *ws, int T, int E, int S, BalScratch *out)
+{
+    const BalShape b = forward_shape(T, E, 1, 1, S);
+    const size_t rows = (size_t)b.S * b.cps;
+    Carver c(ws);
+    BalScratch w;
+    w.hdr = c.take<Header>(1);
+    w.partial = c.take<float>(rows * E);
+    w.pcount = c.take<int>(rows * E);
+    w.plse = c.take<float>(rows);
+    w.pn = c.take<int>(rows);
+    w.dot = c.take<float>(S);
+    w.slse = c.take<float>(S);
+    w.sn = c.take<int>(S);
+    if (out) *out = w;
+    return align_up(c.off, 256);
+}
+
+template <int GS, int CPL, bool VEC>
+rr_status run_fwd(const BalShape &b, const float *logits, const int32_t *topk, const uint8_t *live, const BalScratch &w,
+                  cudaStream_t st)
+{
+    k_balance_partial<GS, CPL, VEC><<<b.S * b.cps, kBalThreads, 0, st>>>(b, logits, topk, live, w);
+    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+}
+
+template <int GS, int CPL, bool VEC>
+rr_status run_bwd(const BalShape &b, const float *logits, const int *count, const int *n, const uint8_t *live, float coef_b,
+                  float coef_z, int accumulate, float *dlogits, cudaStream_t st)
+{
+    const long long items = (long long)b.S * b.cps;
+    const int grid = (int)(items < kBalBwdBlocks ? items : kBalBwdBlocks);
+    k_balance_bwd<GS, CPL, VEC><<<grid, kBalThreads, 0, st>>>(b, logits, count, n, live, coef_b, coef_z, accumulate, dlogits);
+    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t balance_workspace(int T, int E, int S) { return balance_layout(nullptr, T, E, S, nullptr); }
+
+rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float *logits, const int32_t *topk,
+                             const uint8_t *live, float alpha, float beta, float *loss, int32_t *count, int32_t *n_live, float *P,
+                             void *workspace, cudaStream_t st)
+{
+    const BalShape b = forward_shape(T, E, k, stride, S);
+    BalScratch w;
+    balance_layout(workspace, T, E, S, &w);
+    rr_status rc = RR_OK;
+    RR_ROWS_DISPATCH(rc = run_fwd, E, b, logits, topk, live, w, st);
+    if (rc) return rc;
+    k_balance_final<<<S, kBalFinal, 0, st>>>(b, alpha, beta, w, loss, count, n_live, P);
+    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+}
+
+rr_status launch_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
+                             const uint8_t *live, float coef_b, float coef_z, int accumulate, float *dlogits, cudaStream_t st)
+{
+    const BalShape b = balance_shape(T, E, k, 1, S, kBalBwdBlocks, kBalWarps * (32 / layout_of(E).gs));
+    rr_status rc = RR_OK;
+    RR_ROWS_DISPATCH(rc = run_bwd, E, b, logits, count, n_live, live, coef_b, coef_z, accumulate, dlogits, st);
+    return rc;
+}
+
+}  // namespace rr

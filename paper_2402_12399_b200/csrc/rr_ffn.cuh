@@ -64,4 +64,21 @@ rr_status launch_aux_fwd(int T, int E, int stride, const float *logits, const in
 rr_status launch_aux_bwd(int T, int E, const float *logits, const float *f, float coef, int accumulate,
                          float *dlogits, cudaStream_t st);
 
+// Dropout with residual (rr_dropout.cu), linear layer (rr_linear.cu), balance loss (rr_balance.cu)
+rr_status launch_dropout(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p, const void *rng,
+                         void *y, cudaStream_t st);
+size_t linear_fwd_workspace();
+size_t linear_bwd_workspace(int M, int N);
+// (the shape's pitches are filled in)
+rr_status launch_linear_fwd(const rr_linear_shape &s, const void *x, const void *w, const void *bias, const void *residual,
+                            const void *rng, void *y, void *z, void *workspace, cudaStream_t st);
+rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void *x, const void *w, const void *z, const void *rng,
+                            void *dx, void *dw, float *dbias, void *workspace, cudaStream_t st);
+size_t balance_workspace(int T, int E, int S);
+rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float *logits, const int32_t *topk, const uint8_t *live,
+                             float alpha, float beta, float *loss, int32_t *count, int32_t *n_live, float *P, void *workspace,
+                             cudaStream_t st);
+rr_status launch_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
+                             const uint8_t *live, float coef_b, float coef_z, int accumulate, float *dlogits, cudaStream_t st);
+
 }  // namespace rr
