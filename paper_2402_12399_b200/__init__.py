@@ -18,5 +18,7 @@ def __getattr__(name):
     if name in _BINDING or name == "binding":
         import importlib
         binding = importlib.import_module(__name__ + ".binding")
-        return binding if name == "binding" else getattr(binding, name)
+        value = binding if name == "binding" else getattr(binding, name)
+        globals()[name] = value   # found at once from the next time on
+        return value
     raise AttributeError(name)

@@ -486,7 +486,8 @@ def _at(t):
 
 
 def _raw_stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # (the stream's handle without a Stream object around it: 0.1 us instead of 3)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _check_rng(rng, p: float) -> None:

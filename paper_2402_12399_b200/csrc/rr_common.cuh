@@ -34,6 +34,14 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // epilogue -- instead of the 2 s of production.  Host-side; launches copy it into their parameters.
 unsigned long long test_wait_limit_ns();
 
+// streaming multiprocessors of the current device, 0 if that cannot be told
+inline int device_sms()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n;
+}
+
 // Carves aligned sub-buffers out of one workspace allocation (base may be null to size only).
 struct Carver {
     char *base;

@@ -12,24 +12,39 @@ namespace rr {
 
 namespace {
 
-constexpr int kDropThreads = 256;
+constexpr int kDropThreads = 256, kDropBlocks = 3;  // blocks per SM
 
-// eight consecutive elements at 16-byte aligned addresses; plain (coherent) loads, because y may be x or residual
-__device__ __forceinline__ void read8(const float *p, float (&v)[8])
-{
-    const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void read8(const __nv_bfloat16 *p, float (&v)[8])
-{
-    const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// Eight consecutive elements at a 16-byte aligned address as they lie in memory, and as fp32.  Plain (coherent) loads, because y
+// may be x or residual.
+template <class T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void read(const float *p)
+    {
+        a = __ldcs(reinterpret_cast<const float4 *>(p));
+        b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
     }
-}
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void read(const __nv_bfloat16 *p) { u = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
 __device__ __forceinline__ void write8(float *p, const float (&v)[8])
 {
     __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
@@ -50,28 +65,55 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-template <class TX, class TY>
-__global__ void __launch_bounds__(kDropThreads) k_dropout(long long n, const TX *x, const TY *residual, DropoutParams d, TY *y)
+template <class TX, class TY, bool kResidual>
+__global__ void __launch_bounds__(kDropThreads, kDropBlocks) k_dropout(long long n, const TX *x, const TY *residual, DropoutParams d, TY *y)
 {
     PhiloxKey key = {};
     if (d.rng) key = philox_key(d.rng);
-    const long long groups = (n + 7) >> 3, step = (long long)gridDim.x * kDropThreads;
-    for (long long g = (long long)blockIdx.x * kDropThreads + threadIdx.x; g < groups; g += step) {
-        const long long i = g * 8;
-        if (i + 8 <= n) {
-            float v[8], r[8] = {};
-            read8(x + i, v);
-            if (residual) read8(residual + i, r);
-            const uint32_t keep = d.rng ? philox_keep8(key, (unsigned long long)g, d.drop) : 0xffu;
+    const uint32_t bound = keep_bound(d.drop);
+    const long long groups = (n + 7) >> 3, whole = n >> 3, step = (long long)gridDim.x * kDropThreads;
+    const long long g0 = (long long)blockIdx.x * kDropThreads + threadIdx.x;
+    auto one = [&](long long g, const Raw8<TX> &rx, const Raw8<TY> &rr, const uint32_t (&w)[4]) {
+        float v[8], r[8] = {};
+        rx.get(v);
+        if (kResidual) rr.get(r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? fmaf(v[j], d.factor, r[j]) : r[j];
-            write8(y + i, v);
-        } else {  // the last, partial group
-            const uint32_t keep = d.rng ? philox_keep8(key, (unsigned long long)g, d.drop) : 0xffu;
-            for (int j = 0; i + j < n; ++j) {
-                const float r = residual ? as_float(residual[i + j]) : 0.0f;
-                put(y + i + j, (keep >> j) & 1u ? fmaf(as_float(x[i + j]), d.factor, r) : r);
-            }
+        for (int j = 0; j < 8; ++j) v[j] = !d.rng || keep(w, j, bound) ? fmaf(v[j], d.factor, r[j]) : r[j];
+        write8(y + g * 8, v);
+    };
+    long long g = g0;
+    for (; g + step < whole; g += 2 * step) {  // two groups at once: loads in flight together, one key schedule
+        Raw8<TX> xa, xb;
+        Raw8<TY> ra, rb;
+        xa.read(x + g * 8);
+        xb.read(x + (g + step) * 8);
+        if (kResidual) {
+            ra.read(residual + g * 8);
+            rb.read(residual + (g + step) * 8);
+        }
+        uint32_t w[2][4];
+        if (d.rng) philox_words<2>(key, (unsigned long long)g, d.drop, w, (unsigned long long)step);
+        one(g, xa, ra, w[0]);
+        one(g + step, xb, rb, w[1]);
+    }
+    if (g < whole) {
+        Raw8<TX> xa;
+        Raw8<TY> ra;
+        xa.read(x + g * 8);
+        if (kResidual) ra.read(residual + g * 8);
+        uint32_t w[1][4];
+        if (d.rng) philox_words<1>(key, (unsigned long long)g, d.drop, w);
+        one(g, xa, ra, w[0]);
+    }
+    if (whole < groups && whole % step == g0) {  // the last, partial group
+        uint32_t w[1][4];
+        if (d.rng) philox_words<1>(key, (unsigned long long)whole, d.drop, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const long long i = whole * 8 + j;
+            if (i >= n) break;
+            const float r = kResidual ? as_float(residual[i]) : 0.0f;
+            put(y + i, !d.rng || keep(w[0], j, bound) ? fmaf(as_float(x[i]), d.factor, r) : r);
         }
     }
 }
@@ -80,9 +122,13 @@ template <class TX, class TY>
 rr_status run(long long n, const void *x, const void *residual, const DropoutParams &d, void *y, cudaStream_t st)
 {
     const long long groups = (n + 7) / 8, want = (groups + kDropThreads - 1) / kDropThreads;
-    const int grid = (int)(want < 148 * 8 ? want : 148 * 8);
-    k_dropout<TX, TY><<<grid, kDropThreads, 0, st>>>(n, static_cast<const TX *>(x), static_cast<const TY *>(residual), d,
-                                                     static_cast<TY *>(y));
+    const int sms = device_sms();
+    if (sms < 1) return RR_ERR_CUDA;
+    const int grid = (int)(want < sms * kDropBlocks ? want : sms * kDropBlocks);  // resident all at once: no partial wave
+    const TX *px = static_cast<const TX *>(x);
+    const TY *pr = static_cast<const TY *>(residual);
+    if (residual) k_dropout<TX, TY, true><<<grid, kDropThreads, 0, st>>>(n, px, pr, d, static_cast<TY *>(y));
+    else k_dropout<TX, TY, false><<<grid, kDropThreads, 0, st>>>(n, px, pr, d, static_cast<TY *>(y));
     return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 

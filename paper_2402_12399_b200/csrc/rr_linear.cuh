@@ -2,6 +2,7 @@
 // activations' derivatives for its backward pass.
 #pragma once
 #include <cuda_bf16.h>
+#include <float.h>
 
 #include "rr_common.cuh"
 #include "rr_philox.cuh"
@@ -55,23 +56,7 @@ __device__ __forceinline__ void normal_cdf_pdf(float v, float &cdf, float &pdf)
 constexpr float kTanhA = 1.5957691216f;  // 2 sqrt(2 / pi)
 constexpr float kTanhB = 0.044715f;
 
-// A NaN stays a NaN; at +-infinity the limits: v or 0 (v sigmoid(v) is -inf * 0 there, so the product is guarded).
-template <int kAct>
-__device__ __forceinline__ float act_value(float v)
-{
-    if constexpr (kAct == RR_ACT_RELU) return v > 0.0f ? v : (v != v ? v : 0.0f);
-    if constexpr (kAct == RR_ACT_SILU || kAct == RR_ACT_GELU_TANH) {
-        // both are v sigmoid(w): w = v, or (0.5 v (1 + tanh(w / 2)))  w = 2 sqrt(2/pi) (v + 0.044715 v^3)
-        const float s = sigmoid(kAct == RR_ACT_SILU ? v : kTanhA * v * fmaf(kTanhB * v, v, 1.0f));
-        return s == 0.0f ? 0.0f : v * s;
-    }
-    if constexpr (kAct == RR_ACT_GELU) {
-        float cdf, pdf;
-        normal_cdf_pdf(v, cdf, pdf);
-        return cdf == 0.0f ? 0.0f : v * cdf;
-    }
-    return v;
-}
+// act'(v); a NaN stays a NaN, at +-infinity the limits
 template <int kAct>
 __device__ __forceinline__ float act_slope(float v)
 {
@@ -112,129 +97,232 @@ __device__ __forceinline__ uint4 pack8(const float *v)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The activation of eight values, in packed fp32 pairs where the operation exists for pairs (the epilogue is bound by the
+// instructions it issues).  A NaN stays a NaN; at -infinity the factor is 0, and the maximum keeps the product from being a NaN.
 template <int kAct>
 __device__ __forceinline__ void act8(float *v)
 {
+    using namespace tc;
+    if constexpr (kAct == RR_ACT_RELU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = act_value<kAct>(v[j]);
+        for (int j = 0; j < 8; ++j) v[j] = v[j] <= 0.0f ? 0.0f : v[j];
+    }
+    if constexpr (kAct == RR_ACT_SILU || kAct == RR_ACT_GELU_TANH) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const f32x2 x = pack2(v[j], v[j + 1]);
+            f32x2 w;  // -log2(e) times the argument of the sigmoid
+            if (kAct == RR_ACT_SILU) w = mul2(x, pack2(-kLog2e, -kLog2e));
+            else w = mul2(x, fma2(mul2(x, x), pack2(-kLog2e * kTanhA * kTanhB, -kLog2e * kTanhA * kTanhB), pack2(-kLog2e * kTanhA, -kLog2e * kTanhA)));
+            float w0, w1;
+            unpack2(w, w0, w1);
+            unpack2(add2(pack2(ex2(w0), ex2(w1)), pack2(1.0f, 1.0f)), w0, w1);
+            unpack2(mul2(pack2(fmaxf(v[j], -FLT_MAX), fmaxf(v[j + 1], -FLT_MAX)), pack2(rcp(w0), rcp(w1))), v[j], v[j + 1]);
+        }
+    }
+    if constexpr (kAct == RR_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            // normal_cdf_pdf on a pair; Phi = 1/2 +- (1/2 - tail / 2), the sign that of v
+            const f32x2 x = pack2(v[j], v[j + 1]);
+            const f32x2 t2 = mul2(mul2(x, x), pack2(-0.5f * kLog2e, -0.5f * kLog2e));
+            const f32x2 d = fma2(pack2(fabsf(v[j]), fabsf(v[j + 1])), pack2(0.3275911f * 0.70710678f, 0.3275911f * 0.70710678f), pack2(1.0f, 1.0f));
+            float a, b;
+            unpack2(d, a, b);
+            const f32x2 u = pack2(rcp(a), rcp(b));
+            unpack2(t2, a, b);
+            const f32x2 e = pack2(ex2(a), ex2(b));
+            f32x2 q = fma2(pack2(0.5f * 1.061405429f, 0.5f * 1.061405429f), u, pack2(0.5f * -1.453152027f, 0.5f * -1.453152027f));
+            q = fma2(q, u, pack2(0.5f * 1.421413741f, 0.5f * 1.421413741f));
+            q = fma2(q, u, pack2(0.5f * -0.284496736f, 0.5f * -0.284496736f));
+            q = fma2(q, u, pack2(0.5f * 0.254829592f, 0.5f * 0.254829592f));
+            float h0, h1;  // 1/2 - half the tail
+            unpack2(fma2(mul2(q, u), mul2(e, pack2(-1.0f, -1.0f)), pack2(0.5f, 0.5f)), h0, h1);
+            unpack2(mul2(pack2(fmaxf(v[j], -FLT_MAX), fmaxf(v[j + 1], -FLT_MAX)), add2(pack2(copysignf(h0, v[j]), copysignf(h1, v[j + 1])), pack2(0.5f, 0.5f))),
+                    v[j], v[j + 1]);
+        }
+    }
 }
 
-// One epilogue warp: 32 rows (lane = row) x 32 columns at a time.  Results leave through the warp's 4 KB staging tile
-// by TMA stores, which clip at the matrix's edges: lane r writes its row in 16-byte pieces, piece j at
-// j ^ (r & 7) of 128-byte rows (fp32) or j ^ ((r >> 1) & 3) of 64-byte rows (bf16: two tiles of 2 KB in turn).
+__device__ __forceinline__ void add_pair(float *v, float a, float b)
+{
+    tc::unpack2(tc::add2(tc::pack2(v[0], v[1]), tc::pack2(a, b)), v[0], v[1]);
+}
+
+template <int kAct>
+__device__ __forceinline__ void act32(float *v)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) act8<kAct>(v + 8 * j);
+}
+// the activation of eight values
+__device__ __forceinline__ void activate8(int act, float *v)
+{
+    switch (act) {
+    case RR_ACT_RELU: act8<RR_ACT_RELU>(v); break;
+    case RR_ACT_GELU: act8<RR_ACT_GELU>(v); break;
+    case RR_ACT_GELU_TANH: act8<RR_ACT_GELU_TANH>(v); break;
+    case RR_ACT_SILU: act8<RR_ACT_SILU>(v); break;
+    default: break;
+    }
+}
+// dropout of eight consecutive elements whose generator words are w
+__device__ __forceinline__ void drop8(const uint32_t (&w)[4], uint32_t bound, float factor, float *v)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float a, b;
+        tc::unpack2(tc::mul2(tc::pack2(v[i], v[i + 1]), tc::pack2(factor, factor)), a, b);
+        v[i] = keep(w, i, bound) ? a : 0.0f;
+        v[i + 1] = keep(w, i + 1, bound) ? b : 0.0f;
+    }
+}
+
+// The whole epilogue of eight consecutive columns [col, col+8) of one row, results written straight to memory.
+__device__ __forceinline__ void finish8(const Epilogue &e, const PhiloxKey &key, float (&v)[8], long long row, int col, int N, void *y,
+                                        long long ldy, __nv_bfloat16 *z, long long ldz)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= e.alpha;
+    if (e.bias) {
+        float b[8];
+        unpack8(__ldg(reinterpret_cast<const uint4 *>(e.bias + col)), b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    if (z) *reinterpret_cast<uint4 *>(z + row * ldz + col) = pack8(v);
+    activate8(e.act, v);
+    if (e.drop.rng) {
+        uint32_t w[1][4];
+        philox_words<1>(key, ((unsigned long long)row * (unsigned)N + (unsigned)col) >> 3, e.drop.drop, w);
+        drop8(w[0], keep_bound(e.drop.drop), e.drop.factor, v);
+    }
+    if (e.y_f32) {
+        float4 *out = reinterpret_cast<float4 *>(static_cast<float *>(y) + row * ldy + col);
+        if (e.residual) {
+            const float4 *r = reinterpret_cast<const float4 *>(static_cast<const float *>(e.residual) + row * e.ldr + col);
+            const float4 a = r[0], b = r[1];
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
+        out[0] = make_float4(v[0], v[1], v[2], v[3]);
+        out[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        if (e.residual) {
+            float a[8];
+            unpack8(*reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(e.residual) + row * e.ldr + col), a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += a[i];
+        }
+        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(y) + row * ldy + col) = pack8(v);
+    }
+}
+
+// One epilogue warp of the tiled kernel: 32 rows (lane = row) x 32 columns at a time.  Results leave through the warp's
+// 2 KB staging tile by TMA stores, which clip at the matrix's edges: 64-byte rows, lane r writes its row in 16-byte
+// pieces, piece j at j ^ ((r >> 1) & 3); bf16 in one piece of 32 columns, fp32 in two of 16.
 struct EpilogueWarp {
     PhiloxKey key;
-    uint32_t stores;
+    uint4 ahead[4];  // bf16 residual of the next chunk: requested before the accumulator is waited for
 
-    __device__ __forceinline__ explicit EpilogueWarp(const Epilogue &e) : key{}, stores(0)
+    __device__ __forceinline__ void fetch(const Epilogue &e, int row, int col0, int M, int N)
     {
-        if (e.drop.rng) key = philox_key(e.drop.rng);
+        if (!e.residual || e.y_f32) return;
+        const __nv_bfloat16 *r = static_cast<const __nv_bfloat16 *>(e.residual) + row * e.ldr + col0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ahead[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < M && col0 + 8 * j < N) ahead[j] = *reinterpret_cast<const uint4 *>(r + 8 * j);
+        }
     }
 
-    // sends 32 x 32 bf16 through the next 2 KB tile
-    __device__ __forceinline__ void send_bf16(const float *v, uint8_t *st, const CUtensorMap *map, int col0, int row0, int lane)
+    __device__ __forceinline__ static void reuse_tile(int lane)  // the store before has read the staging tile
     {
-        uint8_t *bt = st + (stores & 1u) * 2048;
-        if (stores >= 2) {  // the store before the last one has read this tile
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            __syncwarp();
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4 *>(bt + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = pack8(v + 8 * j);
-        finish(bt, map, col0, row0, lane);
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
     }
-    __device__ __forceinline__ void send_f32(const float *v, uint8_t *st, const CUtensorMap *map, int col0, int row0, int lane)
-    {
-        if (stores >= 1) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            __syncwarp();
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<float4 *>(st + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        finish(st, map, col0, row0, lane);
-    }
-    __device__ __forceinline__ void finish(uint8_t *bt, const CUtensorMap *map, int col0, int row0, int lane)
+    __device__ __forceinline__ static void send(const uint8_t *st, const CUtensorMap *map, int col0, int row0, int lane)
     {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
-            tc::tma_store_2d(map, bt, col0, row0);
+            tc::tma_store_2d(map, st, col0, row0);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
-        ++stores;
+    }
+    __device__ __forceinline__ static void send_bf16(const float *v, uint8_t *st, const CUtensorMap *map, int col0, int row0, int lane)
+    {
+        reuse_tile(lane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4 *>(st + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = pack8(v + 8 * j);
+        send(st, map, col0, row0, lane);
     }
 
-    // accumulator columns [col0, col0+32) of rows [row0, row0+32), lane = row; N is a multiple of 8
-    __device__ __forceinline__ void chunk(const Epilogue &e, float (&v)[32], int row0, int col0, int M, int N, int lane, uint8_t *st,
-                                          const CUtensorMap *mapY, const CUtensorMap *mapZ)
+    // accumulator columns [col0, col0+32) of rows [row0, row0+32); N is a multiple of 8; `next` < 0: no chunk follows
+    // `bias`: of the chunk's 32 columns, fp32 in shared memory (forward)
+    template <bool kForward>
+    __device__ __forceinline__ void chunk(const Epilogue &e, float (&v)[32], const float *bias, int row0, int col0, int next, int M, int N,
+                                          int lane, uint8_t *st, const CUtensorMap *mapY, const CUtensorMap *mapZ)
     {
         const int row = row0 + lane;
-        const bool live = row < M;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= e.alpha;
-        if (e.bias) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (col0 + 8 * j < N) {
-                    float b[8];
-                    unpack8(__ldg(reinterpret_cast<const uint4 *>(e.bias + col0 + 8 * j)), b);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[8 * j + i] += b[i];
-                }
-            }
-        }
-        if (e.save_z) {
-            if (e.y_f32 && stores >= 1) {  // (the fp32 tile of the store before lies over both bf16 tiles)
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                __syncwarp();
-            }
-            send_bf16(v, st, mapZ, col0, row0, lane);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            switch (e.act) {
-            case RR_ACT_RELU: act8<RR_ACT_RELU>(v + 8 * j); break;
-            case RR_ACT_GELU: act8<RR_ACT_GELU>(v + 8 * j); break;
-            case RR_ACT_GELU_TANH: act8<RR_ACT_GELU_TANH>(v + 8 * j); break;
-            case RR_ACT_SILU: act8<RR_ACT_SILU>(v + 8 * j); break;
-            default: break;
-            }
-        }
-        if (e.drop.rng) {
-            const unsigned long long g0 = ((unsigned long long)row * (unsigned)N + (unsigned)col0) >> 3;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t keep = philox_keep8(key, g0 + j, e.drop.drop);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[8 * j + i] = (keep >> i) & 1u ? v[8 * j + i] * e.drop.factor : 0.0f;
-            }
-        }
-        if (e.residual && live) {
-            if (e.y_f32) {
-                const float *r = static_cast<const float *>(e.residual) + row * e.ldr + col0;
+        if constexpr (kForward) {
+            if (e.bias) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (col0 + 4 * j < N) {
-                        const float4 a = *reinterpret_cast<const float4 *>(r + 4 * j);
-                        v[4 * j] += a.x; v[4 * j + 1] += a.y; v[4 * j + 2] += a.z; v[4 * j + 3] += a.w;
-                    }
-                }
-            } else {
-                const __nv_bfloat16 *r = static_cast<const __nv_bfloat16 *>(e.residual) + row * e.ldr + col0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (col0 + 8 * j < N) {
-                        float a[8];
-                        unpack8(*reinterpret_cast<const uint4 *>(r + 8 * j), a);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[8 * j + i] += a[i];
-                    }
+                    const float4 b = *reinterpret_cast<const float4 *>(bias + 4 * j);
+                    add_pair(v + 4 * j, b.x, b.y);
+                    add_pair(v + 4 * j + 2, b.z, b.w);
                 }
             }
+            if (e.save_z) send_bf16(v, st, mapZ, col0, row0, lane);
+            switch (e.act) {
+            case RR_ACT_RELU: act32<RR_ACT_RELU>(v); break;
+            case RR_ACT_GELU: act32<RR_ACT_GELU>(v); break;
+            case RR_ACT_GELU_TANH: act32<RR_ACT_GELU_TANH>(v); break;
+            case RR_ACT_SILU: act32<RR_ACT_SILU>(v); break;
+            default: break;
+            }
+            if (e.drop.rng) {
+                uint32_t w[4][4];
+                philox_words<4>(key, ((unsigned long long)row * (unsigned)N + (unsigned)col0) >> 3, e.drop.drop, w);
+                const uint32_t bound = keep_bound(e.drop.drop);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) drop8(w[j], bound, e.drop.factor, v + 8 * j);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= e.alpha;
         }
-        if (e.y_f32) send_f32(v, st, mapY, col0, row0, lane);
-        else send_bf16(v, st, mapY, col0, row0, lane);
+        if (!e.y_f32) {
+            if (e.residual) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float a[8];
+                    unpack8(ahead[j], a);
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) add_pair(v + 8 * j + i, a[i], a[i + 1]);
+                }
+                if (next >= 0) fetch(e, row, next, M, N);
+            }
+            send_bf16(v, st, mapY, col0, row0, lane);
+        } else {
+            const float *r = static_cast<const float *>(e.residual) + row * e.ldr + col0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (col0 + 16 * h >= N) break;
+                reuse_tile(lane);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = 16 * h + 4 * j;
+                    float4 a = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                    if (e.residual && row < M && col0 + c < N) {
+                        const float4 b = *reinterpret_cast<const float4 *>(r + c);
+                        a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+                    }
+                    *reinterpret_cast<float4 *>(st + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = a;
+                }
+                send(st, mapY, col0 + 16 * h, row0, lane);
+            }
+        }
     }
 };
 

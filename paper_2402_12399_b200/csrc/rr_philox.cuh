@@ -37,28 +37,45 @@ __device__ __forceinline__ PhiloxKey philox_key(const unsigned long long *rng)
     return {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)offset, (uint32_t)(offset >> 32)};
 }
 
-// bit j of the result: element 8*group + j is kept
-__device__ __forceinline__ uint32_t philox_keep8(const PhiloxKey &key, unsigned long long group, uint32_t drop)
+// The generator's words for G groups of eight elements, `group`, `group` + stride, ..., in lockstep: the groups share the key
+// schedule and hide each other's latency.  They are set so that keep() below is false for every piece when all is dropped.
+template <int G>
+__device__ __forceinline__ void philox_words(const PhiloxKey &key, unsigned long long group, uint32_t drop, uint32_t (&w)[G][4],
+                                             unsigned long long stride = 1)
 {
-    uint32_t c0 = (uint32_t)group, c1 = (uint32_t)(group >> 32), c2 = key.o0, c3 = key.o1, k0 = key.k0, k1 = key.k1;
+    uint32_t k0 = key.k0, k1 = key.k1;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const unsigned long long c = group + g * stride;
+        w[g][0] = (uint32_t)c;
+        w[g][1] = (uint32_t)(c >> 32);
+        w[g][2] = key.o0;
+        w[g][3] = key.o1;
+    }
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
-        const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-        c1 = (uint32_t)p1;
-        c3 = (uint32_t)p0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const uint64_t p0 = (uint64_t)w[g][0] * 0xD2511F53u, p1 = (uint64_t)w[g][2] * 0xCD9E8D57u;
+            w[g][0] = (uint32_t)(p1 >> 32) ^ w[g][1] ^ k0;
+            w[g][2] = (uint32_t)(p0 >> 32) ^ w[g][3] ^ k1;
+            w[g][1] = (uint32_t)p1;
+            w[g][3] = (uint32_t)p0;
+        }
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    const uint32_t w[4] = {c0, c1, c2, c3};
-    uint32_t keep = 0;
+    if (drop > 65535u) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        keep |= (w[q] & 0xffffu) >= drop ? 1u << (2 * q) : 0u;
-        keep |= (w[q] >> 16) >= drop ? 2u << (2 * q) : 0u;
+        for (int g = 0; g < G; ++g) w[g][0] = w[g][1] = w[g][2] = w[g][3] = 0u;
     }
-    return keep;
+}
+// `drop` as the bound of keep(): the pieces are compared in the upper halves of words, one comparison each
+__device__ __forceinline__ uint32_t keep_bound(uint32_t drop) { return drop > 65535u ? 0xffffffffu : drop << 16; }
+// is element j of the group kept?
+__device__ __forceinline__ bool keep(const uint32_t (&w)[4], int j, uint32_t bound)
+{
+    return ((j & 1) ? w[j >> 1] : w[j >> 1] << 16) >= bound;
 }
 
 }  // namespace rr

@@ -70,6 +70,40 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     return true;
 }
 
+// As mbar_try_wait, but the thread may sleep in the instruction for up to about a millisecond: a waiting thread then takes no
+// issue slots from the warps that work.
+__device__ __forceinline__ bool mbar_try_sleep(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u)
+        : "memory");
+    return ok != 0;
+}
+
+// mbar_wait for loops that wait once per k-block: sleeping tries, and the clock is read only every sixteenth time one fails.
+__device__ __forceinline__ bool mbar_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status)
+{
+    unsigned long long t0 = 0;
+    for (uint32_t it = 1; !mbar_try_sleep(bar, parity); ++it) {
+        if ((it & 15u) == 0) {
+            if (*abort_flag) return false;
+            const unsigned long long now = globaltimer();
+            if (t0 == 0) t0 = now;
+            if (now - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                latch_status(status, RR_ERR_TIMEOUT);
+                return false;
+            }
+        }
+    }
+    return true;
+}
+
 // Lane 0 waits, the whole warp learns the outcome.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status,
                                           unsigned long long limit_ns = kWaitLimitNs)
@@ -221,6 +255,30 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d_tmem, uint64_t adesc, uin
             ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
             : "memory");
     }
+}
+
+// ---- single CTAs (cta_group::1) -----------------------------------------------------------
+__device__ __forceinline__ void tmem_alloc_one(uint32_t *smem_result, uint32_t ncols)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_result)), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish_one() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_dealloc_one(uint32_t taddr, uint32_t ncols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+// arrive on this CTA's mbarrier once every MMA issued so far by this thread has completed
+__device__ __forceinline__ void mma_commit_one(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mma_ss_one(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
 
 // 32 consecutive fp32 columns of this thread's TMEM lane; returns once the values have landed
