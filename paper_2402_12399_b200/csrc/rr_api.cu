@@ -460,7 +460,7 @@ rr_status rr_linear_workspace_bytes(int M, int N, int K, size_t *fwd_bytes, size
     rr_status rc = check_linear_sizes(M, N, K);
     if (rc) return rc;
     if (fwd_bytes) *fwd_bytes = rr::linear_fwd_workspace();
-    if (bwd_bytes) *bwd_bytes = rr::linear_bwd_workspace(M, N);
+    if (bwd_bytes) *bwd_bytes = rr::linear_bwd_workspace(M, N, K);
     return RR_OK;
 }
 
@@ -499,7 +499,7 @@ rr_status rr_linear_bwd(const rr_linear_shape *shape, const void *dy, const void
     }
     if (!dy || !workspace || (dW && !x) || (dx && !W) || (s.act != RR_ACT_NONE && !z)) return RR_ERR_INVALID_ARG;
     if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(W, 16) || !aligned(z, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
-    if (rr::linear_bwd_workspace(s.M, s.N) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    if (rr::linear_bwd_workspace(s.M, s.N, s.K) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
     return rr::launch_linear_bwd(s, dy, x, W, z, rng, dx, dW, dbias, workspace, st);
 }
 

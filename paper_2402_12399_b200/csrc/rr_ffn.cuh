@@ -68,7 +68,7 @@ rr_status launch_aux_bwd(int T, int E, const float *logits, const float *f, floa
 rr_status launch_dropout(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p, const void *rng,
                          void *y, cudaStream_t st);
 size_t linear_fwd_workspace();
-size_t linear_bwd_workspace(int M, int N);
+size_t linear_bwd_workspace(int M, int N, int K);
 // (the shape's pitches are filled in)
 rr_status launch_linear_fwd(const rr_linear_shape &s, const void *x, const void *w, const void *bias, const void *residual,
                             const void *rng, void *y, void *z, void *workspace, cudaStream_t st);

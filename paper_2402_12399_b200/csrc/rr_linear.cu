@@ -7,7 +7,6 @@
 // of the next.  Operands are read as they lie in memory (K-major or MN-major), nothing is transposed.
 #include <cuda.h>
 #include <cuda_bf16.h>
-#include <stdlib.h>
 
 #include "rr_ffn.cuh"
 #include "rr_linear.cuh"
@@ -29,61 +28,87 @@ constexpr int kDenseThreads = 32 * (kDenseEpi0 + kDenseEpiWarps);
 constexpr int kEpiBytes = 2048;          // staging of one epilogue warp
 
 struct DenseShared {
-    alignas(16) float bias[2][256];  // of the tile's columns, one buffer per accumulator
+    alignas(16) float bias[kDenseEpiWarps][32];  // of the columns that an epilogue warp is working on
     uint64_t full[12], empty[12], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort_flag;
 };
 
-template <int TN>
-__host__ __device__ constexpr int dense_stage_bytes() { return kStageA + TN / 2 * 128; }
-template <int TN>
-__host__ __device__ constexpr int dense_stages() { return TN == 256 ? 6 : 8; }
-template <int TN>
-constexpr size_t dense_smem() { return (size_t)dense_stages<TN>() * dense_stage_bytes<TN>() + kDenseEpiWarps * kEpiBytes + sizeof(DenseShared); }
+constexpr int kTN = 256;                                    // columns of a tile
+constexpr int kDenseStage = kStageA + kTN / 2 * 128;        // bytes of one k-block in one CTA
+constexpr int kDenseStages = 6;
+constexpr size_t kDenseSmem = (size_t)kDenseStages * kDenseStage + kDenseEpiWarps * kEpiBytes + sizeof(DenseShared);
 
-// One product of a launch: C[M,N] = A B, tiles of 256 x TN.  *_mn: the operand is MN-major, its rows are the contraction.
+// One product of a launch: C[M,N] = A B in tiles of 256 x 256.  *_mn: the operand is MN-major, its rows are the contraction.
+// With split > 1 the contraction of every tile is cut into that many items, whose results go to consecutive matrices
+// of part_rows rows (fp32) for k_combine to add up.
 struct DenseJob {
     CUtensorMap mapA, mapB, mapY, mapZ;
-    int M, N, m_tiles, n_tiles, kblocks, tiles;
+    int M, N, m_tiles, n_tiles, kblocks, items;
+    int split, part_rows;
     int a_mn, b_mn;
     Epilogue e;
 };
-// Up to two products share a launch (dx and dW), the one with the longer contraction first.
+// db[c] (+)= factor * sum over the slabs of k_dz, in their order
+struct BiasGrad {
+    const float *partial;  // [slabs][n], null: none
+    float *db;
+    int n, slabs, add;
+    float factor;
+};
+__device__ __forceinline__ void bias_grad(const BiasGrad &b, int c)
+{
+    if (c >= b.n) return;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < b.slabs; ++i) s += b.partial[(size_t)i * b.n + c];
+    b.db[c] = b.add ? __fadd_rn(b.db[c], b.factor * s) : b.factor * s;
+}
+
+// Up to two products share a launch (dx and dW), the one with the longer items first.
 struct DenseParams {
     DenseJob job[2];
-    int total;
+    int items[2];  // of each job
+    int head;      // rounds of the second job's items that only pairs with fewer items of the first take part in
+    BiasGrad bias; // (backward)
     int *status;
 };
 
-// Tile `t` of a job: bands of eight row tiles, inside a band column after column, so that the pairs running together share few
-// A and B tiles (74 pairs: 8 x 9) and find them in L2.
-struct Tile {
-    int job, m, n;
+// The it-th item of this pair (job, index), index -1: no more.  The first job's items are dealt out in rounds; `more` pairs got
+// one more than the others.  Of the second job's shorter items the others take `head` rounds alone (about the length
+// of a longer one), then all pairs take part.
+struct Item {
+    int job, at;
 };
-// The it-th tile of this pair.  Pairs take every npairs-th item, every second band of npairs items walked backwards, so
-// that the pairs which got the longer items of one band get the shorter end of the next.  -1: no more.
-__device__ __forceinline__ int item_of(const DenseParams &p, int it, int pair, int npairs)
+__device__ __forceinline__ Item item_of(const DenseParams &p, int it, int pair, int npairs)
 {
-    const int first = it * npairs, n = min(npairs, p.total - first);
-    if (n <= 0) return -1;
-    const int at = (it & 1) ? npairs - 1 - pair : pair;  // (a last, partial band goes to those it reaches first)
-    return at < n ? first + at : -1;
+    const int more = p.items[0] % npairs, mine = p.items[0] / npairs + (pair < more ? 1 : 0);
+    if (it < mine) return {0, it * npairs + pair};
+    const int k = it - mine, others = npairs - more;
+    int at;
+    if (pair < more) at = p.head * others + k * npairs + others + pair;
+    else if (k < p.head) at = k * others + pair - more;
+    else at = p.head * others + (k - p.head) * npairs + pair - more;
+    return {1, at < p.items[1] ? at : -1};
 }
-__device__ __forceinline__ Tile tile_of(const DenseParams &p, int t)
+// Tile and share of the contraction of an item.  Bands of eight row tiles, inside a band column after column, so that the pairs
+// running together share few A and B tiles (74 pairs: 8 x 9) and find them in L2.
+struct Work {
+    int m, n, part, kb0, kb1;
+};
+__device__ __forceinline__ Work work_of(const DenseJob &j, int at)
 {
-    const int j = t >= p.job[0].tiles ? 1 : 0;
-    if (j) t -= p.job[0].tiles;
-    const int nt = p.job[j].n_tiles, band = 8 * nt, b = t / band, first = 8 * b, high = min(8, p.job[j].m_tiles - first), r = t - b * band;
-    return {j, first + r % high, r / high};
+    const int t = at / j.split, part = at - t * j.split;
+    const int band = 8 * j.n_tiles, b = t / band, first = 8 * b, high = min(8, j.m_tiles - first), r = t - b * band;
+    return {first + r % high, r / high, part, (int)((long long)j.kblocks * part / j.split), (int)((long long)j.kblocks * (part + 1) / j.split)};
 }
 
-template <int TN, bool kForward>
+template <bool kForward>
 __global__ void __launch_bounds__(kDenseThreads, 1)
 k_dense(const __grid_constant__ DenseParams p)
 {
     extern __shared__ __align__(1024) uint8_t tiles[];  // (128-byte swizzled tiles start at multiples of 1024)
-    constexpr int kNS = dense_stages<TN>(), kStage = dense_stage_bytes<TN>(), kBRows = TN / 2;
+    constexpr int TN = kTN, kNS = kDenseStages, kStage = kDenseStage, kBRows = TN / 2;
     uint8_t *staging = tiles + (size_t)kNS * kStage;
     DenseShared *sh = reinterpret_cast<DenseShared *>(staging + kDenseEpiWarps * kEpiBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -117,13 +142,16 @@ k_dense(const __grid_constant__ DenseParams p)
         // TMA producers: producer j takes the k-blocks j, j + 3, ... of this CTA's stream
         if (lane == 0) {
             uint32_t s = warp % kNS, ph = 0;
-            int kb = warp, t;
+            int ahead = warp;  // k-blocks from the item's first one to this producer's next
             bool ok = true;
-            for (int it = 0; ok && (t = item_of(p, it, pair, npairs)) >= 0; ++it) {
-                const Tile w = tile_of(p, t);
-                const DenseJob &j = p.job[w.job];
+            for (int it = 0; ok; ++it) {
+                const Item i = item_of(p, it, pair, npairs);
+                if (i.at < 0) break;
+                const DenseJob &j = p.job[i.job];
+                const Work w = work_of(j, i.at);
                 const int row = w.m * 256 + 128 * rank, col = w.n * TN + kBRows * rank;  // this CTA's rows of A and of B
-                for (; kb < j.kblocks; kb += kDenseProducers) {
+                int kb = w.kb0 + ahead;
+                for (; kb < w.kb1; kb += kDenseProducers) {
                     if (!mbar_wait_brisk(&sh->empty[s], ph ^ 1u, abort_flag, p.status)) { ok = false; break; }
                     uint8_t *a = tiles + (size_t)s * kStage, *b = a + kStageA;
                     const uint32_t bar = lead_full + 8u * s;
@@ -143,32 +171,33 @@ k_dense(const __grid_constant__ DenseParams p)
                     s += kDenseProducers;
                     if (s >= (uint32_t)kNS) { s -= kNS; ph ^= 1u; }
                 }
-                kb -= j.kblocks;
+                ahead = kb - w.kb1;
             }
         }
     } else if (warp == kDenseMma) {
         if (rank == 0 && lane == 0) {
             const uint32_t a0 = smem_u32(tiles);
             uint32_t s = 0, ph = 0;
-            int t;
             bool ok = true;
-            for (int it = 0; ok && (t = item_of(p, it, pair, npairs)) >= 0; ++it) {
-                const DenseJob &j = p.job[tile_of(p, t).job];
+            for (int it = 0; ok; ++it) {
+                const Item i = item_of(p, it, pair, npairs);
+                if (i.at < 0) break;
+                const DenseJob &j = p.job[i.job];
+                const Work w = work_of(j, i.at);
                 const bool amn = !kForward && j.a_mn, bmn = !kForward && j.b_mn;
                 const uint32_t idesc = instr_desc(1u, amn ? 1u : 0u, bmn ? 1u : 0u, 256, TN);
                 const uint64_t adesc0 = smem_desc(a0, amn ? kPanel : 16, 1024), bdesc0 = smem_desc(a0 + kStageA, bmn ? kPanel : 16, 1024);
                 const uint32_t a_step = amn ? 128u : 2u, b_step = bmn ? 128u : 2u;
-                const int kblocks = j.kblocks;
                 const uint32_t buf = it & 1u;
                 if (!mbar_wait_brisk(&sh->tempty[buf], ((it >> 1) & 1u) ^ 1u, abort_flag, p.status)) break;
                 fence_after_sync();
-                for (int kb = 0; kb < kblocks; ++kb) {
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
                     if (!mbar_wait_brisk(&sh->full[s], ph, abort_flag, p.status)) { ok = false; break; }
                     fence_after_sync();
                     const uint32_t off = s * (uint32_t)(kStage >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        mma_ss_pair<false>(tmem_base + buf * TN, adesc0 + off + a_step * kk, bdesc0 + off + b_step * kk, idesc, (kb | kk) != 0);
+                        mma_ss_pair<false>(tmem_base + buf * TN, adesc0 + off + a_step * kk, bdesc0 + off + b_step * kk, idesc, kb != w.kb0 || kk != 0);
                     mma_commit_pair(&sh->empty[s]);
                     if (++s == (uint32_t)kNS) { s = 0; ph ^= 1u; }
                 }
@@ -180,27 +209,25 @@ k_dense(const __grid_constant__ DenseParams p)
         const int eg = (warp - kDenseEpi0) >> 2, q = warp & 3;
         uint8_t *st = staging + (size_t)(eg * 4 + q) * kEpiBytes;
         EpilogueWarp ew;
+        if (!kForward && p.bias.partial)  // before the first tile there is nothing else to do: 32 columns a warp, over all blocks
+            for (int c = (warp - kDenseEpi0) * (int)gridDim.x + (int)blockIdx.x; c * 32 < p.bias.n; c += kDenseEpiWarps * (int)gridDim.x)
+                bias_grad(p.bias, c * 32 + lane);
         if (kForward && p.job[0].e.drop.rng) ew.key = philox_key(p.job[0].e.drop.rng);
-        int t;
-        for (int it = 0; (t = item_of(p, it, pair, npairs)) >= 0; ++it) {
-            const Tile w = tile_of(p, t);
-            const DenseJob &j = p.job[w.job];
+        for (int it = 0;; ++it) {
+            const Item i = item_of(p, it, pair, npairs);
+            if (i.at < 0) break;
+            const DenseJob &j = p.job[i.job];
+            const Work w = work_of(j, i.at);
             const uint32_t buf = it & 1u;
             const int row0 = w.m * 256 + 128 * rank + q * 32;  // first of this warp's 32 rows
             const int col00 = w.n * TN;
             const bool mine = row0 < j.M;
-            if (mine) ew.fetch(j.e, row0 + lane, col00 + eg * 32, j.M, j.N);
-            // one thread polls, the others sleep at a named barrier: sixteen polling warps would take issue slots from the
-            // producers and the MMA issuer (K = 4096, one tile a pair: 41 us instead of 34)
-            if (kForward && j.e.bias) {
-                // (the barrier below also says that everyone has finished the tile before, whose buffer the next one takes)
-                const int c = threadIdx.x - 32 * kDenseEpi0;
-                if (c < TN) sh->bias[buf][c] = col00 + c < j.N ? __bfloat162float(j.e.bias[col00 + c]) : 0.0f;
-            }
-            if (warp == kDenseEpi0 && lane == 0) mbar_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status);
-            __syncwarp();
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kDenseEpiWarps) : "memory");
-            if (*abort_flag) break;
+            if (mine) ew.template fetch<kForward>(j.e, row0 + lane, col00 + eg * 32, j.M, j.N, lane);
+            // Every warp waits for itself, asleep: sixteen warps that poll would take issue slots from the producers and the MMA
+            // issuer, and a barrier in front of the tile would hold the early ones back.
+            int ok = 1;
+            if (lane == 0) ok = mbar_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status) ? 1 : 0;
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
             fence_after_sync();
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * TN;
             if (mine) {
@@ -208,7 +235,8 @@ k_dense(const __grid_constant__ DenseParams p)
                 for (int c = eg * 32; c < TN && col00 + c < j.N; c += 128) {
                     float v[32];
                     tmem_ld32(taddr + c, v);
-                    ew.template chunk<kForward>(j.e, v, sh->bias[buf] + c, row0, col00 + c, c + 128 < TN ? col00 + c + 128 : -1, j.M, j.N, lane, st, &j.mapY, &j.mapZ);
+                    ew.template chunk<kForward>(j.e, v, sh->bias[eg * 4 + q], row0, w.part * j.part_rows, col00 + c, c + 128 < TN ? col00 + c + 128 : -1, j.M,
+                                                 j.N, lane, st, &j.mapY, &j.mapZ);
                 }
             }
             fence_before_sync();
@@ -235,6 +263,7 @@ k_dense(const __grid_constant__ DenseParams p)
 // tiles meet in shared memory: each CTA of the cluster adds up its share of the features, in the order of the
 // ranks (the result repeats bit for bit), and finishes them.  About 110 KB of shared memory a CTA: two share an SM.
 //   kWmn: the weights are MN-major (dx = dz W: the features are the columns of W, the contraction runs over its rows).
+constexpr int kSlimTokens = 128;   // up to here always
 constexpr int kSlimThreads = 320;  // warp 0: TMA, warp 1: MMA, warps 2-9: TMEM; all of them finish
 template <int BN>
 __host__ __device__ constexpr int slim_stage_bytes() { return kStageA + BN * 128; }
@@ -403,6 +432,28 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
     }
 }
 
+// ---- the parts of a split contraction ------------------------------------------------------------------
+// y = finish(sum of `split` fp32 matrices [M,N], part_rows rows apart, in their order)
+__global__ void __launch_bounds__(256) k_combine(int M, int N, const float *__restrict__ parts, int split, int part_rows, Epilogue e, void *y, long long ldy)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int groups = N >> 3;
+    const long long n = (long long)M * groups, step = (long long)part_rows * N;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const long long row = i / groups;
+        const int col = (int)(i - row * groups) * 8;
+        const float *src = parts + row * N + col;
+        float v[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < split; ++s, src += step) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(src)), b = __ldg(reinterpret_cast<const float4 *>(src) + 1);
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
+        finish8(e, PhiloxKey{}, v, row, col, N, y, ldy, nullptr, 0);
+    }
+}
+
 // ---- dz and its column sums ---------------------------------------------------------------------------
 constexpr int kDzThreads = 256, kDzCols = 256;  // 32 threads x 8 columns, 8 rows at a time
 
@@ -436,6 +487,8 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
                     if (kAct != RR_ACT_NONE) a4[u] = __ldg(reinterpret_cast<const uint4 *>(z + row * ldz + col));
                 }
             }
+            uint32_t w[kU][4];
+            if (d.rng) philox_words<kU>(key, ((unsigned long long)r * N + col) >> 3, d.drop, w, (unsigned long long)kRows * N >> 3);
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
                 const int row = r + u * kRows;
@@ -448,10 +501,8 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
                     for (int j = 0; j < 8; ++j) g[j] *= act_slope<kAct>(a[j]);
                 }
                 if (d.rng) {
-                    uint32_t w[1][4];
-                    philox_words<1>(key, ((unsigned long long)row * N + col) >> 3, d.drop, w);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] = keep(w[0], j, bound) ? g[j] : 0.0f;
+                    for (int j = 0; j < 8; ++j) g[j] = keep(w[u], j, bound) ? g[j] : 0.0f;
                 }
                 if (dz) *reinterpret_cast<uint4 *>(dz + (size_t)row * N + col) = pack8(g);
 #pragma unroll
@@ -472,16 +523,7 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
     }
 }
 
-// db[c] (+)= factor * sum over the slabs, in their order
-__global__ void k_dbias(int N, int slabs, const float *__restrict__ partial, float factor, int add, float *db)
-{
-    const int c = blockIdx.x * blockDim.x + threadIdx.x;
-    if (c >= N) return;
-    float s = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < slabs; ++i) s += partial[(size_t)i * N + c];
-    db[c] = add ? __fadd_rn(db[c], factor * s) : factor * s;
-}
+__global__ void __launch_bounds__(256) k_dbias(const BiasGrad b) { bias_grad(b, blockIdx.x * 256 + threadIdx.x); }
 
 int dz_slabs(int M, int N)
 {
@@ -491,19 +533,54 @@ int dz_slabs(int M, int N)
     return want < 1 ? 1 : want;
 }
 
+// How the backward products are cut into items: parts of dx's and dW's contractions (0: not on this kernel).
+struct Plan {
+    int dx, dw;
+};
+constexpr int kPlanPairs = 74;  // CTA pairs of a B200; fixed, because the workspace depends on it
+long long tiles_of(int rows, int cols) { return ((long long)rows + 255) / 256 * ((cols + 255) / 256); }
+int kblocks_of(int n) { return (n + 63) / 64; }
+// A product with few tiles and a long contraction (dW of many tokens) would keep a few pairs busy long after the others have
+// finished: its contraction is cut so that an item takes no longer than an even share of the whole launch (twelve k-blocks at
+// least), where that saves more than the sixteen k-blocks' time (5 us) that writing and adding up the parts costs.
+Plan plan_bwd(int M, int N, int K, bool dx, bool dw)
+{
+    const long long tx = dx ? tiles_of(M, K) : 0, tw = dw ? tiles_of(N, K) : 0;
+    const int kx = kblocks_of(N), kw = kblocks_of(M);
+    long long even = (tx * kx + tw * kw + kPlanPairs - 1) / kPlanPairs;
+    if (even < 12) even = 12;
+    auto parts = [&](long long tiles, int kb) {
+        if (tiles == 0) return 0;
+        if (kb <= even + 16) return 1;
+        return (int)((kb + even - 1) / even);
+    };
+    return {parts(tx, kx), parts(tw, kw)};
+}
+int part_rows(int rows) { return (rows + 255) / 256 * 256; }  // (the last tile's rows may not run into the next part)
+
 struct LinearScratch {
     Header *hdr;
     __nv_bfloat16 *dz;  // [M,N]
     float *partial;     // [slabs][N]
+    float *parts_dx, *parts_dw;  // [parts][rows][K]
 };
 
-size_t linear_layout(void *ws, int M, int N, LinearScratch *out)
+size_t linear_layout(void *ws, int M, int N, int K, LinearScratch *out)
 {
+    size_t px = 0, pw = 0;
+    for (int want = 1; want < 4; ++want) {  // room for whichever gradients a call asks for
+        const Plan p = plan_bwd(M, N, K, want & 1, want & 2);
+        const size_t x = p.dx > 1 ? (size_t)p.dx * part_rows(M) * K : 0, w = p.dw > 1 ? (size_t)p.dw * part_rows(N) * K : 0;
+        if (x > px) px = x;
+        if (w > pw) pw = w;
+    }
     Carver c(ws);
     LinearScratch s;
     s.hdr = c.take<Header>(1);
     s.dz = c.take<__nv_bfloat16>((size_t)M * N);
     s.partial = c.take<float>((size_t)dz_slabs(M, N) * N);
+    s.parts_dx = c.take<float>(px);
+    s.parts_dw = c.take<float>(pw);
     if (out) *out = s;
     return align_up(c.off, 256);
 }
@@ -534,25 +611,36 @@ struct Matrix {
     bool mn;
 };
 
-bool make_job(DenseJob *j, int TN, Matrix a, Matrix b, int M, int N, int K, void *y, long long ldy, void *z, long long ldz, const Epilogue &e)
+// With split > 1, `parts` takes the results instead of y.
+bool make_job(DenseJob *j, Matrix a, Matrix b, int M, int N, int K, void *y, long long ldy, void *z, long long ldz, const Epilogue &e, int split = 1,
+              float *parts = nullptr)
 {
     // K-major: [rows, K], box 64 of K x the CTA's rows; MN-major: [K, rows], box 64 of the rows x 64 of K
     if (!(a.mn ? map_2d(&j->mapA, a.p, K, M, a.pitch, false, 64, 64) : map_2d(&j->mapA, a.p, M, K, a.pitch, false, 64, 128))) return false;
-    if (!(b.mn ? map_2d(&j->mapB, b.p, K, N, b.pitch, false, 64, 64) : map_2d(&j->mapB, b.p, N, K, b.pitch, false, 64, TN / 2))) return false;
-    if (!map_2d(&j->mapY, y, M, N, ldy, e.y_f32, e.y_f32 ? 16 : 32, 32)) return false;
-    j->mapZ = j->mapY;
-    if (z && !map_2d(&j->mapZ, z, M, N, ldz, false, 32, 32)) return false;
+    if (!(b.mn ? map_2d(&j->mapB, b.p, K, N, b.pitch, false, 64, 64) : map_2d(&j->mapB, b.p, N, K, b.pitch, false, 64, kTN / 2))) return false;
     j->M = M;
     j->N = N;
     j->m_tiles = (M + 255) / 256;
-    j->n_tiles = (N + TN - 1) / TN;
-    j->kblocks = (K + 63) / 64;
+    j->n_tiles = (N + kTN - 1) / kTN;
+    j->kblocks = kblocks_of(K);
     j->a_mn = a.mn;
     j->b_mn = b.mn;
     j->e = e;
-    const long long tiles = (long long)j->m_tiles * j->n_tiles;
-    if (tiles >= (1ll << 29)) return false;
-    j->tiles = (int)tiles;
+    j->split = split;
+    j->part_rows = part_rows(M);
+    if (split > 1) {
+        j->e = Epilogue{};
+        j->e.alpha = 1.0f;
+        j->e.y_f32 = 1;
+        if (!map_2d(&j->mapY, parts, (long long)split * j->part_rows, N, N, true, 16, 32)) return false;
+    } else {
+        if (!map_2d(&j->mapY, y, M, N, ldy, e.y_f32, e.y_f32 ? 16 : 32, 32)) return false;
+    }
+    j->mapZ = j->mapY;
+    if (z && !map_2d(&j->mapZ, z, M, N, ldz, false, 32, 32)) return false;
+    const long long items = (long long)j->m_tiles * j->n_tiles * split;
+    if (items >= (1ll << 29)) return false;
+    j->items = (int)items;
     return true;
 }
 
@@ -576,15 +664,30 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int TN, bool kForward>
-rr_status launch_dense(const DenseParams &p, cudaStream_t st)
+// `n` jobs of p, the one with the longer items first
+template <bool kForward>
+rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
 {
     const int pairs = device_sms() / 2;
     if (pairs < 1) return RR_ERR_CUDA;
-    if (cudaFuncSetAttribute(k_dense<TN, kForward>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dense_smem<TN>()) != cudaSuccess)
-        return RR_ERR_CUDA;
-    return launch_dependent(k_dense<TN, kForward>, dim3(2 * (unsigned)(p.total < pairs ? p.total : pairs)), kDenseThreads, dense_smem<TN>(), 2,
-                            st, p) == cudaSuccess
+    p.items[0] = p.job[0].items;
+    p.items[1] = n > 1 ? p.job[1].items : 0;
+    p.head = 0;
+    if (n > 1) {  // (an item's epilogue and start count as three k-blocks)
+        const int a = p.job[0].kblocks / p.job[0].split + 3, b = p.job[1].kblocks / p.job[1].split + 3;
+        p.head = (a + b / 2) / b;
+    }
+    const long long total = (long long)p.items[0] + p.items[1];
+    if (cudaFuncSetAttribute(k_dense<kForward>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseSmem) != cudaSuccess) return RR_ERR_CUDA;
+    return launch_dependent(k_dense<kForward>, dim3(2 * (unsigned)(total < pairs ? total : pairs)), kDenseThreads, kDenseSmem, 2, st, p) == cudaSuccess
+               ? RR_OK : RR_ERR_CUDA;
+}
+
+rr_status launch_combine(int M, int N, const float *parts, int split, const Epilogue &e, void *y, long long ldy, cudaStream_t st)
+{
+    const long long blocks = ((long long)M * (N / 8) + 255) / 256;
+    return launch_dependent(k_combine, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8)), 256, 0, 1, st, M, N, parts, split, part_rows(M), e, y,
+                            ldy) == cudaSuccess
                ? RR_OK : RR_ERR_CUDA;
 }
 
@@ -598,7 +701,6 @@ rr_status run_slim(const CUtensorMap &mW, const CUtensorMap &mX, const SlimParam
                ? RR_OK : RR_ERR_CUDA;
 }
 
-int env_int(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
 // y [tokens, features] = x [tokens, K] . W; W is [features, K], or [K, features] with kWmn.
 template <bool kWmn>
 rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, void *y, long long ldy, void *z, long long ldz, const Epilogue &e,
@@ -620,9 +722,10 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
     p.ldz = ldz;
     p.status = status;
     const int f_tiles = (features + 127) / 128;
-    const int maxc = env_int("SLIM_CTAS", 296), minkb = env_int("SLIM_KB", 2);
+    // two CTAs on every SM, if each is left four k-blocks (1 x 4096 x 4096: 9.5 us with 256 CTAs, 10.0 with 128; 64 x 4096 x 1024: 6.9 us with
+    // 128 CTAs of four k-blocks, 8.1 with 256 of two)
     p.split = 1;
-    while (p.split < 8 && (long long)f_tiles * p.t_tiles * p.split * 2 <= maxc && p.kblocks >= 2 * minkb * p.split) p.split *= 2;
+    while (p.split < 8 && (long long)f_tiles * p.t_tiles * p.split * 2 <= 2 * 148 && p.kblocks >= 8 * p.split) p.split *= 2;
     switch (BN) {
     case 16: return run_slim<16, kWmn>(mW, mX, p, f_tiles, st);
     case 32: return run_slim<32, kWmn>(mW, mX, p, f_tiles, st);
@@ -642,7 +745,7 @@ void launch_dz(dim3 grid, cudaStream_t st, int M, int N, const void *dy, long lo
 }  // namespace
 
 size_t linear_fwd_workspace() { return kHeaderBytes; }
-size_t linear_bwd_workspace(int M, int N) { return linear_layout(nullptr, M, N, nullptr); }
+size_t linear_bwd_workspace(int M, int N, int K) { return linear_layout(nullptr, M, N, K, nullptr); }
 
 rr_status launch_linear_fwd(const rr_linear_shape &s, const void *x, const void *w, const void *bias, const void *residual, const void *rng,
                             void *y, void *z, void *workspace, cudaStream_t st)
@@ -656,21 +759,24 @@ rr_status launch_linear_fwd(const rr_linear_shape &s, const void *x, const void 
     e.save_z = z != nullptr;
     e.drop = dropout_params(s.p, rng);
     e.alpha = 1.0f;
-    if (s.M <= env_int("SLIM_M", 128))
+    // Few tokens, or tiles for no more than half of the SMs and a long contraction to split (measured, 256 x 256 tiles against the
+    // split kernel: 512 x 4096 x 4096 28.5 against 21.3 us, 1024 x 1024 x 4096 20.9 against 15.4, 512 x 1024 x 1024 11.5 against 8.9; with more tiles or a
+    // short contraction the larger tiles win: 768 x 4096 x 4096 28.5 against 35.6, 2048 x 1024 x 1024 10.1 against 10.7).
+    const long long tiles = tiles_of(s.M, s.N);
+    if (s.M <= kSlimTokens || tiles <= 16 || (tiles <= kPlanPairs / 2 && kblocks_of(s.K) >= 32))
         return launch_slim<false>({w, s.K}, {x, s.ldx}, s.M, s.N, s.K, y, s.ldy, z, s.ldz, e, &static_cast<Header *>(workspace)->status, st);
     DenseParams p;
     p.status = &static_cast<Header *>(workspace)->status;
-    const int TN = env_int("TN", 256);
-    if (!make_job(&p.job[0], TN, {x, s.ldx, false}, {w, s.K, false}, s.M, s.N, s.K, y, s.ldy, z, s.ldz, e)) return RR_ERR_CUDA;
-    p.total = p.job[0].tiles;
-    return TN == 256 ? launch_dense<256, true>(p, st) : launch_dense<128, true>(p, st);
+    p.bias = {};
+    if (!make_job(&p.job[0], {x, s.ldx, false}, {w, s.K, false}, s.M, s.N, s.K, y, s.ldy, z, s.ldz, e)) return RR_ERR_CUDA;
+    return launch_dense<true>(p, 1, st);
 }
 
 rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void *x, const void *w, const void *z, const void *rng, void *dx,
                             void *dw, float *dbias, void *workspace, cudaStream_t st)
 {
     LinearScratch ws;
-    linear_layout(workspace, s.M, s.N, &ws);
+    linear_layout(workspace, s.M, s.N, s.K, &ws);
     const DropoutParams d = dropout_params(s.p, rng);
     const bool plain = s.act == RR_ACT_NONE && !d.rng;  // dz is dy itself
     const bool want_dz = !plain && (dx || dw);
@@ -687,11 +793,9 @@ rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void
         default: launch_dz<RR_ACT_SILU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
         }
         if (cudaGetLastError() != cudaSuccess) return RR_ERR_CUDA;
-        if (dbias) {
-            k_dbias<<<(s.N + 255) / 256, 256, 0, st>>>(s.N, slabs, ws.partial, d.rng ? d.factor : 1.0f, (s.flags & RR_ADD_DW) ? 1 : 0, dbias);
-            if (cudaGetLastError() != cudaSuccess) return RR_ERR_CUDA;
-        }
     }
+    BiasGrad bias = {};
+    if (dbias) bias = {ws.partial, dbias, s.N, dz_slabs(s.M, s.N), (s.flags & RR_ADD_DW) ? 1 : 0, d.rng ? d.factor : 1.0f};
     const Operand g = plain ? Operand{dy, s.lddy} : Operand{ws.dz, s.N};
     Epilogue e = {};
     e.alpha = d.rng ? d.factor : 1.0f;
@@ -705,26 +809,32 @@ rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void
     ew.y_f32 = s.dw_dtype == RR_F32;
     ew.residual = (s.flags & RR_ADD_DW) ? dw : nullptr;
     ew.ldr = s.K;
-    if (dx && s.M <= env_int("SLIM_M", 128)) {
+    if (dx && s.M <= kSlimTokens) {
         const rr_status rc = launch_slim<true>({w, s.K}, {g.p, g.pitch}, s.M, s.K, s.N, dx, s.lddx, nullptr, 0, e, &ws.hdr->status, st);
         if (rc) return rc;
         dx = nullptr;
     }
-    if (!dx && !dw) return RR_OK;
+    if (!dx && !dw) {
+        if (dbias) k_dbias<<<(s.N + 255) / 256, 256, 0, st>>>(bias);
+        return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    }
+    const Plan plan = plan_bwd(s.M, s.N, s.K, dx, dw);
     DenseParams p;
     p.status = &ws.hdr->status;
-    p.total = 0;
+    p.bias = bias;
     int n = 0;
-    const int TN = env_int("TN", 256);
-    for (int first = 0; first < 2; ++first) {  // the longer contraction first
-        const bool is_dx = (s.N >= s.M) == (first == 0);
+    for (int turn = 0; turn < 2; ++turn) {
+        const bool is_dx = ((long long)kblocks_of(s.N) * (plan.dw ? plan.dw : 1) >= (long long)kblocks_of(s.M) * (plan.dx ? plan.dx : 1)) == (turn == 0);
         if (is_dx ? !dx : !dw) continue;
-        const bool ok = is_dx ? make_job(&p.job[n], TN, {g.p, g.pitch, false}, {w, s.K, true}, s.M, s.K, s.N, dx, s.lddx, nullptr, 0, e)
-                              : make_job(&p.job[n], TN, {g.p, g.pitch, true}, {x, s.ldx, true}, s.N, s.K, s.M, dw, s.K, nullptr, 0, ew);
+        const bool ok = is_dx ? make_job(&p.job[n], {g.p, g.pitch, false}, {w, s.K, true}, s.M, s.K, s.N, dx, s.lddx, nullptr, 0, e, plan.dx, ws.parts_dx)
+                              : make_job(&p.job[n], {g.p, g.pitch, true}, {x, s.ldx, true}, s.N, s.K, s.M, dw, s.K, nullptr, 0, ew, plan.dw, ws.parts_dw);
         if (!ok) return RR_ERR_CUDA;
-        p.total += p.job[n++].tiles;
+        ++n;
     }
-    return TN == 256 ? launch_dense<256, false>(p, st) : launch_dense<128, false>(p, st);
+    rr_status rc = launch_dense<false>(p, n, st);
+    if (!rc && plan.dx > 1) rc = launch_combine(s.M, s.K, ws.parts_dx, plan.dx, e, dx, s.lddx, st);
+    if (!rc && plan.dw > 1) rc = launch_combine(s.N, s.K, ws.parts_dw, plan.dw, ew, dw, s.K, st);
+    return rc;
 }
 
 }  // namespace rr

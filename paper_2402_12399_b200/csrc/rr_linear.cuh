@@ -224,8 +224,12 @@ struct EpilogueWarp {
     PhiloxKey key;
     uint4 ahead[4];  // bf16 residual of the next chunk: requested before the accumulator is waited for
 
-    __device__ __forceinline__ void fetch(const Epilogue &e, int row, int col0, int M, int N)
+    float ahead_bias;  // and its bias, of column col0 + lane
+
+    template <bool kForward>
+    __device__ __forceinline__ void fetch(const Epilogue &e, int row, int col0, int M, int N, int lane)
     {
+        if (kForward && e.bias) ahead_bias = col0 + lane < N ? __bfloat162float(e.bias[col0 + lane]) : 0.0f;
         if (!e.residual || e.y_f32) return;
         const __nv_bfloat16 *r = static_cast<const __nv_bfloat16 *>(e.residual) + row * e.ldr + col0;
 #pragma unroll
@@ -258,14 +262,17 @@ struct EpilogueWarp {
     }
 
     // accumulator columns [col0, col0+32) of rows [row0, row0+32); N is a multiple of 8; `next` < 0: no chunk follows
-    // `bias`: of the chunk's 32 columns, fp32 in shared memory (forward)
+    // `bias`: 32 floats of shared memory of this warp; `shift`: rows between these and their place behind mapY
     template <bool kForward>
-    __device__ __forceinline__ void chunk(const Epilogue &e, float (&v)[32], const float *bias, int row0, int col0, int next, int M, int N,
+    __device__ __forceinline__ void chunk(const Epilogue &e, float (&v)[32], float *bias, int row0, int shift, int col0, int next, int M, int N,
                                           int lane, uint8_t *st, const CUtensorMap *mapY, const CUtensorMap *mapZ)
     {
         const int row = row0 + lane;
         if constexpr (kForward) {
             if (e.bias) {
+                __syncwarp();
+                bias[lane] = ahead_bias;
+                __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float4 b = *reinterpret_cast<const float4 *>(bias + 4 * j);
@@ -301,10 +308,11 @@ struct EpilogueWarp {
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) add_pair(v + 8 * j + i, a[i], a[i + 1]);
                 }
-                if (next >= 0) fetch(e, row, next, M, N);
             }
-            send_bf16(v, st, mapY, col0, row0, lane);
+            if (next >= 0) fetch<kForward>(e, row, next, M, N, lane);
+            send_bf16(v, st, mapY, col0, row0 + shift, lane);
         } else {
+            if (next >= 0) fetch<kForward>(e, row, next, M, N, lane);
             const float *r = static_cast<const float *>(e.residual) + row * e.ldr + col0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -320,7 +328,7 @@ struct EpilogueWarp {
                     }
                     *reinterpret_cast<float4 *>(st + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = a;
                 }
-                send(st, mapY, col0 + 16 * h, row0, lane);
+                send(st, mapY, col0 + 16 * h, row0 + shift, lane);
             }
         }
     }

@@ -15,6 +15,8 @@ import block_ref as ref
 
 pytestmark = pytest.mark.gpu
 HALF = 2.0 ** -8       # half a step of bf16, relative
+# (the long ones: few tiles and a long contraction, which the backward pass splits)
+LONG = [(4099, 136, 264), (9001, 264, 520), (300, 4104, 264), (20011, 24, 8)]
 SIZES = [(1, 8, 8), (2, 64, 64), (31, 136, 72), (33, 72, 136), (64, 1032, 8), (127, 8, 520), (129, 264, 520), (255, 520, 264), (257, 512, 1032), (700, 648, 392)]
 
 
@@ -42,7 +44,7 @@ def _assert_within(got, want, tol, what=""):
     assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
 
 
-@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("M,N,K", SIZES + LONG)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_whole_numbers_are_exact(M, N, K, dtype):
     import paper_2402_12399_b200 as rr
@@ -99,7 +101,7 @@ def test_forward(M, N, K, act):
         _assert_within(y, want, tol, "y")
 
 
-@pytest.mark.parametrize("M,N,K", SIZES + [(3, 1032, 2056), (300, 2048, 1032), (1111, 1416, 968), (4099, 136, 264)])
+@pytest.mark.parametrize("M,N,K", SIZES + [(3, 1032, 2056), (300, 2048, 1032), (1111, 1416, 968)] + LONG)
 @pytest.mark.parametrize("act", range(5))
 def test_gradients(M, N, K, act):
     import paper_2402_12399_b200 as rr
