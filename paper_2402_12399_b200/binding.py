@@ -652,15 +652,17 @@ def balance_fwd(logits: torch.Tensor, topk_expert: torch.Tensor, k: int, alpha: 
         dev = logits.device
         out = (torch.empty(2, dtype=torch.float32, device=dev), torch.empty(segments, E, dtype=torch.int32, device=dev),
                torch.empty(segments, dtype=torch.int32, device=dev), torch.empty(segments, E, dtype=torch.float32, device=dev))
+    else:
+        for t, shape, dtype in zip(out, ((2,), (segments, E), (segments,), (segments, E)),
+                                   (torch.float32, torch.int32, torch.int32, torch.float32)):
+            if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError(f"out: expected contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+        _on_device(*out)
     loss, count, n_live, P = out
-    _on_device(logits, topk_expert, live, workspace, loss, count, n_live, P)
+    _on_device(logits, topk_expert, live, workspace)
     _check_scores(logits, live)
     if topk_expert.dtype != torch.int32 or topk_expert.dim() != 2 or topk_expert.shape[0] != T or not topk_expert.is_contiguous():
         raise TypeError("topk_expert is a contiguous int32 [T,n]")
-    for t, shape, dtype in ((loss, (2,), torch.float32), (count, (segments, E), torch.int32), (n_live, (segments,), torch.int32),
-                            (P, (segments, E), torch.float32)):
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-            raise ValueError(f"out: expected contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     _ok(lib().rr_balance_fwd(T, E, k, topk_expert.shape[1], segments, logits.data_ptr(), topk_expert.data_ptr(), _at(live), alpha, beta,
                              loss.data_ptr(), count.data_ptr(), n_live.data_ptr(), P.data_ptr(), workspace.data_ptr(), workspace.numel(),
                              _raw_stream()), "rr_balance_fwd")

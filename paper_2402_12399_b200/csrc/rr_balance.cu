@@ -10,18 +10,20 @@
 // launch latency below.  The row of a dead token is read and selected away (its load does not wait for the
 // mask), so what it holds -- NaN, infinities -- reaches no sum.  All sums are fp32 in a fixed order (counts are
 // integers), so the results repeat bit for bit.
+#include <type_traits>
+
 #include "rr_ffn.cuh"
 #include "rr_rows.cuh"
+#include "rr_tc.cuh"
 
 namespace rr {
 
 namespace {
 
-constexpr int kBalThreads = 256;
+constexpr int kBalThreads = 512;
 constexpr int kBalWarps = kBalThreads / 32;
-constexpr int kBalBlocks = 592;     // forward: blocks wanted, 4 per SM
-constexpr int kBalFinal = 512;      // threads of the second forward kernel
-constexpr int kBalBwdBlocks = 1184; // backward: 8 per SM
+constexpr int kBalBlocks = 296;     // blocks wanted: two per SM, all resident at once
+constexpr int kBalFinal = 1024;     // threads of the second forward kernel
 
 // softmax of one row over the group's lanes and its log-sum-exp; a token that is not live takes part in the
 // shuffles with zeros
@@ -44,24 +46,55 @@ __device__ __forceinline__ void load_row(const float *__restrict__ a, bool in, i
         }
     }
 }
+// g becomes exp(a - m), m the row's maximum; returns log sum_e exp(a_e) and, in inv, the factor that makes g the softmax.  These
+// kernels are bound by the instructions they issue, so: one fused multiply-add per pair of columns, the hardware's exponential,
+// logarithm and reciprocal (relative errors of about 2^-22).  The shift is the rounded product m log2(e) itself, which
+// the logarithm adds back, so its rounding cancels.  The row of a dead token gives garbage that its group keeps to itself.
 template <int GS, int CPL>
-__device__ __forceinline__ float softmax_lse(bool live, float (&g)[CPL])
+__device__ __forceinline__ float softmax_lse(float (&g)[CPL], float &inv)
 {
+    using namespace tc;
     float m = -INFINITY;
 #pragma unroll
     for (int c = 0; c < CPL; ++c) m = fmaxf(m, g[c]);
-    m = group_max<GS>(m);
+    const float shift = group_max<GS>(m) * kLog2e;
     float z = 0.f;
+    if constexpr (CPL % 2 == 0) {
+        f32x2 sum = pack2(0.f, 0.f);
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) {
-        g[c] = live ? expf(g[c] - m) : 0.f;  // exp(-inf) = 0 for the columns past E
-        z += g[c];
+        for (int c = 0; c < CPL; c += 2) {
+            unpack2(fma2(pack2(g[c], g[c + 1]), pack2(kLog2e, kLog2e), pack2(-shift, -shift)), g[c], g[c + 1]);
+            g[c] = ex2(g[c]);  // (exp(-inf) = 0 for the columns past E)
+            g[c + 1] = ex2(g[c + 1]);
+            sum = add2(sum, pack2(g[c], g[c + 1]));
+        }
+        float a, b;
+        unpack2(sum, a, b);
+        z = a + b;
+    } else {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            g[c] = ex2(fmaf(g[c], kLog2e, -shift));
+            z += g[c];
+        }
     }
     z = group_sum<GS>(z);
-    const float inv = live ? 1.0f / z : 0.f;
+    inv = rcp(z);
+    return (shift + lg2(z)) * 0.693147180559945f;
+}
+// acc += inv * g
+template <int CPL>
+__device__ __forceinline__ void add_scaled(float (&acc)[CPL], const float (&g)[CPL], float inv)
+{
+    using namespace tc;
+    if constexpr (CPL % 2 == 0) {
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) g[c] *= inv;
-    return live ? m + logf(z) : 0.f;
+        for (int c = 0; c < CPL; c += 2)
+            unpack2(fma2(pack2(g[c], g[c + 1]), pack2(inv, inv), pack2(acc[c], acc[c + 1])), acc[c], acc[c + 1]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) acc[c] = fmaf(g[c], inv, acc[c]);
+    }
 }
 
 __device__ __forceinline__ bool is_live(const uint8_t *__restrict__ live, bool in, long long t)
@@ -99,6 +132,9 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
     __shared__ int cnt[kMaxE];
     __shared__ float red_lse[kBalWarps];
     __shared__ int red_n[kBalWarps];
+    // the second kernel is launched as a programmatic dependent: it may be made ready at once (it waits for the whole of this
+    // grid before it reads the partial sums)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
     for (int j = threadIdx.x; j < E; j += kBalThreads) cnt[j] = 0;
     __syncthreads();
@@ -107,29 +143,37 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
     const long long t1 = min(seg0 + b.L, t0 + b.slab);
     float acc[CPL] = {}, lse2 = 0.f;
     int n = 0;
-    auto choices = [&](long long t) {
-        for (int r = gl; r < b.k; r += GS) {
-            const int e = __ldg(topk + t * b.stride + r);
-            if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
-            else latch_status(&w.hdr->status, RR_ERR_INVALID_ARG);
-        }
+    auto count_choice = [&](int e) {
+        if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+        else latch_status(&w.hdr->status, RR_ERR_INVALID_ARG);
     };
     for (long long base = t0 + warp * TPW; base < t1; base += 2 * kBalWarps * TPW) {  // two tokens in flight per group
         const long long ta = base + grp, tb = ta + kBalWarps * TPW;
         const bool ina = ta < t1, inb = tb < t1;
+        // rows, marks and choices are requested together, whatever the marks will say
         float ga[CPL], gb[CPL];
         load_row<GS, CPL, VEC>(logits + (ina ? ta : 0) * E, ina, E, gl, ga);
         load_row<GS, CPL, VEC>(logits + (inb ? tb : 0) * E, inb, E, gl, gb);
         const bool la = is_live(live, ina, ta), lb = is_live(live, inb, tb);
-        if (la) choices(ta);
-        if (lb) choices(tb);
-        const float za = softmax_lse<GS, CPL>(la, ga), zb = softmax_lse<GS, CPL>(lb, gb);
-#pragma unroll
-        for (int c = 0; c < CPL; ++c) acc[c] += la ? ga[c] : 0.f;
-#pragma unroll
-        for (int c = 0; c < CPL; ++c) acc[c] += lb ? gb[c] : 0.f;
-        lse2 += za * za;
-        lse2 += zb * zb;
+        const int ea = ina && gl < b.k ? __ldg(topk + ta * b.stride + gl) : 0, eb = inb && gl < b.k ? __ldg(topk + tb * b.stride + gl) : 0;
+        if (la && gl < b.k) count_choice(ea);
+        if (lb && gl < b.k) count_choice(eb);
+        if (GS < kMaxK) {  // (a group smaller than k)
+            for (int r = gl + GS; r < b.k; r += GS) {
+                if (la) count_choice(__ldg(topk + ta * b.stride + r));
+                if (lb) count_choice(__ldg(topk + tb * b.stride + r));
+            }
+        }
+        float ia, ib;
+        const float za = softmax_lse<GS, CPL>(ga, ia), zb = softmax_lse<GS, CPL>(gb, ib);
+        if (la) {
+            add_scaled<CPL>(acc, ga, ia);
+            lse2 = fmaf(za, za, lse2);
+        }
+        if (lb) {
+            add_scaled<CPL>(acc, gb, ib);
+            lse2 = fmaf(zb, zb, lse2);
+        }
         n += (la ? 1 : 0) + (lb ? 1 : 0);
     }
     // groups of the warp, then warps of the block, in a fixed order
@@ -163,91 +207,137 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
     }
 }
 
-// sums over the block in a fixed order; every thread gets the result
+// sums over the warp, the same in every lane, and over the block (any number of warps up to 32), in a fixed order
 template <class T>
-__device__ __forceinline__ T block_sum(T v, T *buf)
+__device__ __forceinline__ T warp_sum(T v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <class... T>
+__device__ __forceinline__ void block_sums(uint32_t (*buf)[32], T &...v)
+{
+    const int lane = threadIdx.x & 31, warps = (int)(blockDim.x >> 5);
+    int k = 0;
+    auto store = [&](auto &x) {
+        x = warp_sum(x);
+        if (lane == 0) buf[k][threadIdx.x >> 5] = *reinterpret_cast<const uint32_t *>(&x);
+        ++k;
+    };
     __syncthreads();  // (buf may still be read from the call before)
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    (store(v), ...);
     __syncthreads();
-    T sum = 0;
-    for (int q = 0; q < (int)(blockDim.x >> 5); ++q) sum += buf[q];
-    return sum;
+    k = 0;
+    auto load = [&](auto &x) {
+        const uint32_t u = lane < warps ? buf[k][lane] : 0u;  // (the bits of a zero of either type)
+        x = warp_sum(*reinterpret_cast<const typename std::remove_reference<decltype(x)>::type *>(&u));
+        ++k;
+    };
+    (load(v), ...);
 }
 
 // Forward, second kernel: block s adds up the blocks of segment s; the block that finishes last adds up the segments.
+// Thread (r, j) takes the rows r, r + R, ... of column j (of the four columns from j on when VEC); the R sums of a column are then
+// added in two steps.
+template <bool VEC>
 __global__ void __launch_bounds__(kBalFinal)
 k_balance_final(const BalShape b, float alpha, float beta, const BalScratch w, float *loss, int *count, int *n_live, float *P)
 {
-    __shared__ float sp[kBalFinal];
-    __shared__ int sc[kBalFinal];
-    __shared__ float fbuf[32];
-    __shared__ int ibuf[32];
+    constexpr int V = VEC ? 4 : 1, kParts = kBalFinal / kMaxE;
+    __shared__ float sp[kBalFinal * V];
+    __shared__ int sc[kBalFinal * V];
+    __shared__ float tp[kParts][kMaxE];
+    __shared__ int tc[kParts][kMaxE];
+    __shared__ uint32_t buf[4][32];
     __shared__ int last;
-    const int s = blockIdx.x, E = b.E, tid = threadIdx.x;
-    int epad = 1;
+    const int s = blockIdx.x, E = b.E, tid = threadIdx.x, lane = tid & 31;
+    int epad = V;
     while (epad < E) epad <<= 1;
-    const int R = kBalFinal / epad, r = tid / epad, j = tid % epad;
+    const int cols = epad / V, R = kBalFinal / cols, r = tid / cols, j = (tid % cols) * V;
     const size_t row0 = (size_t)s * b.cps;
-    float sum = 0.f;
-    int cnt = 0;
+    float sum[V] = {}, lse2 = 0.f;
+    int cnt[V] = {}, n = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the first kernel has completed and its sums are visible
+    for (int c = lane; c < b.cps; c += 32) { lse2 += w.plse[row0 + c]; n += w.pn[row0 + c]; }  // (every warp for itself: no barrier)
     if (j < E) {
 #pragma unroll 4
         for (int c = r; c < b.cps; c += R) {
-            sum += w.partial[(row0 + c) * E + j];
-            cnt += w.pcount[(row0 + c) * E + j];
+            if constexpr (VEC) {
+                const float4 x = *reinterpret_cast<const float4 *>(w.partial + (row0 + c) * E + j);
+                const int4 y = *reinterpret_cast<const int4 *>(w.pcount + (row0 + c) * E + j);
+                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+                cnt[0] += y.x; cnt[1] += y.y; cnt[2] += y.z; cnt[3] += y.w;
+            } else {
+                sum[0] += w.partial[(row0 + c) * E + j];
+                cnt[0] += w.pcount[(row0 + c) * E + j];
+            }
         }
     }
-    float lse2 = 0.f;
-    int n = 0;
-    for (int c = tid; c < b.cps; c += kBalFinal) { lse2 += w.plse[row0 + c]; n += w.pn[row0 + c]; }
-    sp[tid] = sum;
-    sc[tid] = cnt;
-    n = block_sum(n, ibuf);  // (its barriers also order the writes to sp and sc)
-    lse2 = block_sum(lse2, fbuf);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        sp[r * epad + j + v] = sum[v];
+        sc[r * epad + j + v] = cnt[v];
+    }
+    n = warp_sum(n);
+    lse2 = warp_sum(lse2);
+    __syncthreads();
+    {
+        const int c = tid % kMaxE, part = tid / kMaxE, rows = min(R, b.cps);  // (the other rows are zero)
+        float t = 0.f;
+        int m = 0;
+        if (c < E)
+            for (int q = part; q < rows; q += kParts) { t += sp[q * epad + c]; m += sc[q * epad + c]; }
+        tp[part][c] = t;
+        tc[part][c] = m;
+    }
+    __syncthreads();
     float prod = 0.f;
     if (tid < E) {
         float tot = 0.f;
         int m = 0;
-        for (int q = 0; q < R; ++q) { tot += sp[q * epad + tid]; m += sc[q * epad + tid]; }
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) { tot += tp[q][tid]; m += tc[q][tid]; }
         const float p = n > 0 ? tot / (float)n : 0.f;
         count[(size_t)s * E + tid] = m;
         P[(size_t)s * E + tid] = p;
         if (n > 0) prod = (float)m / ((float)b.k * (float)n) * p;
     }
-    prod = block_sum(prod, fbuf);
-    if (tid == 0) {
-        n_live[s] = n;
-        w.dot[s] = prod;
-        w.slse[s] = lse2;
-        w.sn[s] = n;
-        __threadfence();
-        last = atomicAdd(&w.hdr->sync[8], 1) == b.S - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
+    block_sums(buf, prod);
     float dots = 0.f, z = 0.f;
-    int segs = 0;
-    unsigned long long tokens = 0;  // (T is an int, so this fits; the sum of floats follows the same order every time)
-    for (int q = tid; q < b.S; q += kBalFinal) {
-        dots += __ldcg(w.dot + q);
-        z += __ldcg(w.slse + q);
-        const int m = __ldcg(w.sn + q);
-        tokens += m;
-        segs += m > 0 ? 1 : 0;
-    }
-    dots = block_sum(dots, fbuf);
-    z = block_sum(z, fbuf);
-    segs = block_sum(segs, ibuf);
-    const int live = block_sum((int)tokens, ibuf);
-    if (tid == 0) {
-        loss[0] = segs > 0 ? alpha * (float)E / (float)segs * dots : 0.f;
-        loss[1] = live > 0 ? beta / (float)live * z : 0.f;
+    int segs = 0, live = 0;
+    if (b.S == 1) {
+        if (tid) return;
+        n_live[0] = n;
+        dots = prod;
+        z = lse2;
+        segs = n > 0 ? 1 : 0;
+        live = n;
+    } else {
+        if (tid == 0) {
+            n_live[s] = n;
+            w.dot[s] = prod;
+            w.slse[s] = lse2;
+            w.sn[s] = n;
+            __threadfence();
+            last = atomicAdd(&w.hdr->sync[8], 1) == b.S - 1;
+        }
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        for (int q = tid; q < b.S; q += kBalFinal) {
+            dots += __ldcg(w.dot + q);
+            z += __ldcg(w.slse + q);
+            const int m = __ldcg(w.sn + q);
+            live += m;
+            segs += m > 0 ? 1 : 0;
+        }
+        block_sums(buf, dots, z, segs, live);
+        if (tid) return;
         w.hdr->sync[8] = 0;
     }
+    loss[0] = segs > 0 ? alpha * (float)E / (float)segs * dots : 0.f;
+    loss[1] = live > 0 ? beta / (float)live * z : 0.f;
 }
 
 // Backward: items of up to `slab` tokens of one segment, dealt to the blocks in turn.
@@ -257,7 +347,7 @@ k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__r
               const uint8_t *__restrict__ live, float coef_b, float coef_z, int accumulate, float *dlogits)
 {
     constexpr int TPW = 32 / GS;
-    __shared__ int ibuf[32];
+    __shared__ uint32_t buf[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
     int segs = 0, tokens = 0;
     for (int q = threadIdx.x; q < b.S; q += kBalThreads) {
@@ -265,8 +355,7 @@ k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__r
         tokens += m;
         segs += m > 0 ? 1 : 0;
     }
-    segs = block_sum(segs, ibuf);
-    tokens = block_sum(tokens, ibuf);
+    block_sums(buf, segs, tokens);
     const float cz = tokens > 0 ? coef_z / (float)tokens : 0.f;
     for (long long item = blockIdx.x; item < (long long)b.S * b.cps; item += gridDim.x) {
         const int s = (int)(item / b.cps);
@@ -286,16 +375,16 @@ k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__r
             float g[CPL];
             load_row<GS, CPL, VEC>(logits + (in ? t : 0) * E, in, E, gl, g);
             const bool l = is_live(live, in, t);
-            const float lse = softmax_lse<GS, CPL>(l, g);
-            float dot = 0.f;
+            float inv, dot = 0.f;
+            const float lse = softmax_lse<GS, CPL>(g, inv);
 #pragma unroll
-            for (int c = 0; c < CPL; ++c) dot += l ? fj[c] * g[c] : 0.f;
-            dot = group_sum<GS>(dot);
+            for (int c = 0; c < CPL; ++c) dot = fmaf(fj[c], g[c], dot);
+            dot = group_sum<GS>(dot) * inv;
             if (!in || (!l && accumulate)) continue;
             float *o = dlogits + t * E;
             const float zz = cz * lse;
 #pragma unroll
-            for (int c = 0; c < CPL; ++c) g[c] = l ? g[c] * fmaf(cb, fj[c] - dot, zz) : 0.f;
+            for (int c = 0; c < CPL; ++c) g[c] = l ? g[c] * inv * fmaf(cb, fj[c] - dot, zz) : 0.f;
             if constexpr (VEC) {
 #pragma unroll
                 for (int q = 0; q < CPL / 4; ++q) {
@@ -340,7 +429,7 @@ BalShape balance_shape(int T, int E, int k, int stride, int S, int want, int pas
 }
 BalShape forward_shape(int T, int E, int k, int stride, int S)
 {
-    return balance_shape(T, E, k, stride, S, kBalBlocks, 4 * kBalWarps * (32 / layout_of(E).gs));
+    return balance_shape(T, E, k, stride, S, kBalBlocks, 2 * kBalWarps * (32 / layout_of(E).gs));
 }
 
 size_t balance_layout(void *ws, int T, int E, int S, BalScratch *out)
@@ -374,7 +463,7 @@ rr_status run_bwd(const BalShape &b, const float *logits, const int *count, cons
                   float coef_z, int accumulate, float *dlogits, cudaStream_t st)
 {
     const long long items = (long long)b.S * b.cps;
-    const int grid = (int)(items < kBalBwdBlocks ? items : kBalBwdBlocks);
+    const int grid = (int)(items < kBalBlocks ? items : kBalBlocks);
     k_balance_bwd<GS, CPL, VEC><<<grid, kBalThreads, 0, st>>>(b, logits, count, n, live, coef_b, coef_z, accumulate, dlogits);
     return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
@@ -393,14 +482,26 @@ rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float
     rr_status rc = RR_OK;
     RR_ROWS_DISPATCH(rc = run_fwd, E, b, logits, topk, live, w, st);
     if (rc) return rc;
-    k_balance_final<<<S, kBalFinal, 0, st>>>(b, alpha, beta, w, loss, count, n_live, P);
-    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    // as a programmatic dependent of the first kernel: its launch overlaps the first one's run
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S);
+    cfg.blockDim = dim3(kBalFinal);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t err = E % 4 == 0 ? cudaLaunchKernelEx(&cfg, k_balance_final<true>, b, alpha, beta, w, loss, count, n_live, P)
+                                       : cudaLaunchKernelEx(&cfg, k_balance_final<false>, b, alpha, beta, w, loss, count, n_live, P);
+    return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 
 rr_status launch_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
                              const uint8_t *live, float coef_b, float coef_z, int accumulate, float *dlogits, cudaStream_t st)
 {
-    const BalShape b = balance_shape(T, E, k, 1, S, kBalBwdBlocks, kBalWarps * (32 / layout_of(E).gs));
+    // (with few segments one item per block; with many, smaller items even out their lengths)
+    const BalShape b = balance_shape(T, E, k, 1, S, (S > kBalBlocks / 4 ? 4 : 1) * kBalBlocks, kBalWarps * (32 / layout_of(E).gs));
     rr_status rc = RR_OK;
     RR_ROWS_DISPATCH(rc = run_bwd, E, b, logits, count, n_live, live, coef_b, coef_z, accumulate, dlogits, st);
     return rc;

@@ -21,19 +21,9 @@ struct Epilogue {
     float alpha;                // factor of the accumulator
 };
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLog2e = 1.4426950408889634f;
+using tc::ex2;
+using tc::kLog2e;
+using tc::rcp;
 __device__ __forceinline__ float sigmoid(float v) { return rcp(1.0f + ex2(-kLog2e * v)); }
 
 // The normal distribution function and density.  Phi(v) = erfc(|v| / sqrt 2) / 2 mirrored, with
