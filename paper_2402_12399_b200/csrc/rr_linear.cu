@@ -497,8 +497,9 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
                 unpack8(g4[u], g);
                 if constexpr (kAct != RR_ACT_NONE) {
                     unpack8(a4[u], a);
+                    act_slope8<kAct>(a);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] *= act_slope<kAct>(a[j]);
+                    for (int j = 0; j < 8; j += 2) unpack2(mul2(pack2(g[j], g[j + 1]), pack2(a[j], a[j + 1])), g[j], g[j + 1]);
                 }
                 if (d.rng) {
 #pragma unroll
@@ -506,7 +507,7 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
                 }
                 if (dz) *reinterpret_cast<uint4 *>(dz + (size_t)row * N + col) = pack8(g);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += g[j];
+                for (int j = 0; j < 8; j += 2) add_pair(acc + j, g[j], g[j + 1]);
             }
         }
     }

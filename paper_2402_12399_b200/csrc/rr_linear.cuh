@@ -24,47 +24,76 @@ struct Epilogue {
 using tc::ex2;
 using tc::kLog2e;
 using tc::rcp;
-__device__ __forceinline__ float sigmoid(float v) { return rcp(1.0f + ex2(-kLog2e * v)); }
 
-// The normal distribution function and density.  Phi(v) = erfc(|v| / sqrt 2) / 2 mirrored, with
-// erfc(t) = (a1 u + a2 u^2 + .. + a5 u^5) e^{-t^2}, u = 1 / (1 + 0.3275911 t)   (Abramowitz and Stegun 7.1.26,
-// absolute error below 1.5e-7): the exponential is the density's, so the derivative costs nothing more.
-__device__ __forceinline__ void normal_cdf_pdf(float v, float &cdf, float &pdf)
+// The normal distribution function of a pair as copysign(h, v) + 1/2, and e^(-v^2/2), 2.5 times the density:
+// Phi(v) = erfc(|v| / sqrt 2) / 2 mirrored, with erfc(t) = (a1 u + a2 u^2 + .. + a5 u^5) e^{-t^2}, u = 1 / (1 + 0.3275911 t)
+// (Abramowitz and Stegun 7.1.26, absolute error below 1.5e-7); h = 1/2 - half of that.
+__device__ __forceinline__ void normal_pair(float v0, float v1, float &h0, float &h1, tc::f32x2 &e)
 {
-    const float t = fabsf(v) * 0.70710678f;
-    const float e = ex2(-kLog2e * t * t);
-    const float u = rcp(fmaf(0.3275911f, t, 1.0f));
-    float q = fmaf(1.061405429f, u, -1.453152027f);
-    q = fmaf(q, u, 1.421413741f);
-    q = fmaf(q, u, -0.284496736f);
-    q = fmaf(q, u, 0.254829592f);
-    const float half_tail = 0.5f * q * u * e;
-    cdf = v < 0.0f ? half_tail : 1.0f - half_tail;
-    pdf = 0.39894228f * e;
+    using namespace tc;
+    const f32x2 x = pack2(v0, v1);
+    float a, b;
+    unpack2(mul2(mul2(x, x), pack2(-0.5f * kLog2e, -0.5f * kLog2e)), a, b);
+    e = pack2(ex2(a), ex2(b));
+    constexpr float p = 0.3275911f * 0.70710678f;
+    const f32x2 u = pack2(rcp(fmaf(fabsf(v0), p, 1.0f)), rcp(fmaf(fabsf(v1), p, 1.0f)));
+    f32x2 q = fma2(pack2(-0.5f * 1.061405429f, -0.5f * 1.061405429f), u, pack2(0.5f * 1.453152027f, 0.5f * 1.453152027f));
+    q = fma2(q, u, pack2(-0.5f * 1.421413741f, -0.5f * 1.421413741f));
+    q = fma2(q, u, pack2(0.5f * 0.284496736f, 0.5f * 0.284496736f));
+    q = fma2(q, u, pack2(-0.5f * 0.254829592f, -0.5f * 0.254829592f));
+    unpack2(fma2(mul2(q, u), e, pack2(0.5f, 0.5f)), h0, h1);
 }
 
 constexpr float kTanhA = 1.5957691216f;  // 2 sqrt(2 / pi)
 constexpr float kTanhB = 0.044715f;
 
-// act'(v); a NaN stays a NaN, at +-infinity the limits
+// -log2(e) times the argument of the sigmoid that SiLU and the tanh form of GELU multiply v by
 template <int kAct>
-__device__ __forceinline__ float act_slope(float v)
+__device__ __forceinline__ tc::f32x2 sigmoid_argument(tc::f32x2 x)
 {
-    if constexpr (kAct == RR_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
-    if constexpr (kAct == RR_ACT_SILU) {
-        const float s = sigmoid(v);
-        return s == 0.0f ? 0.0f : s == 1.0f ? 1.0f : s * fmaf(v, 1.0f - s, 1.0f);
+    using namespace tc;
+    if (kAct == RR_ACT_SILU) return mul2(x, pack2(-kLog2e, -kLog2e));
+    constexpr float b = -kLog2e * kTanhA * kTanhB, a = -kLog2e * kTanhA;
+    return mul2(x, fma2(mul2(x, x), pack2(b, b), pack2(a, a)));
+}
+__device__ __forceinline__ float finite(float v) { return fminf(fmaxf(v, -FLT_MAX), FLT_MAX); }  // (a NaN becomes a number)
+
+// act'(v) of eight values, in packed fp32 pairs where the operation exists for pairs.  A NaN stays a NaN (through the exponential);
+// at +-infinity, where the other factor is 0, the bounded v keeps the product from being a NaN.
+template <int kAct>
+__device__ __forceinline__ void act_slope8(float *v)
+{
+    using namespace tc;
+    const f32x2 one = pack2(1.0f, 1.0f);
+    if constexpr (kAct == RR_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = v[j] > 0.0f ? 1.0f : 0.0f;
     }
-    if constexpr (kAct == RR_ACT_GELU_TANH) {
-        const float s = sigmoid(kTanhA * v * fmaf(kTanhB * v, v, 1.0f));
-        return s == 0.0f ? 0.0f : s == 1.0f ? 1.0f : fmaf(v * s * (1.0f - s), kTanhA * fmaf(3.0f * kTanhB * v, v, 1.0f), s);
+    if constexpr (kAct == RR_ACT_SILU || kAct == RR_ACT_GELU_TANH) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            float a, b;
+            unpack2(sigmoid_argument<kAct>(pack2(v[j], v[j + 1])), a, b);
+            unpack2(add2(pack2(ex2(a), ex2(b)), one), a, b);
+            const f32x2 s = pack2(rcp(a), rcp(b)), minus = pack2(-1.0f, -1.0f);
+            // s + x dw/dv s (1 - s);   (1 - s as -(s - 1)); where v is large enough for v^3 to overflow, s (1 - s) is 0 and v bounded
+            const f32x2 x = pack2(fminf(fmaxf(v[j], -1e4f), 1e4f), fminf(fmaxf(v[j + 1], -1e4f), 1e4f));
+            f32x2 xw = x;
+            if (kAct == RR_ACT_GELU_TANH)
+                xw = mul2(x, fma2(mul2(x, x), pack2(3.0f * kTanhA * kTanhB, 3.0f * kTanhA * kTanhB), pack2(kTanhA, kTanhA)));
+            unpack2(fma2(mul2(xw, s), fma2(s, minus, one), s), v[j], v[j + 1]);
+        }
     }
     if constexpr (kAct == RR_ACT_GELU) {
-        float cdf, pdf;
-        normal_cdf_pdf(v, cdf, pdf);
-        return pdf == 0.0f ? cdf : fmaf(v, pdf, cdf);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            float h0, h1;
+            f32x2 e;
+            normal_pair(v[j], v[j + 1], h0, h1, e);
+            const f32x2 cdf = add2(pack2(copysignf(h0, v[j]), copysignf(h1, v[j + 1])), pack2(0.5f, 0.5f));
+            unpack2(fma2(pack2(finite(v[j]), finite(v[j + 1])), mul2(e, pack2(0.39894228f, 0.39894228f)), cdf), v[j], v[j + 1]);
+        }
     }
-    return 1.0f;
 }
 
 __device__ __forceinline__ void unpack8(const uint4 &u, float (&v)[8])
@@ -87,8 +116,7 @@ __device__ __forceinline__ uint4 pack8(const float *v)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The activation of eight values, in packed fp32 pairs where the operation exists for pairs (the epilogue is bound by the
-// instructions it issues).  A NaN stays a NaN; at -infinity the factor is 0, and the maximum keeps the product from being a NaN.
+// The activation of eight values, likewise.
 template <int kAct>
 __device__ __forceinline__ void act8(float *v)
 {
@@ -100,34 +128,18 @@ __device__ __forceinline__ void act8(float *v)
     if constexpr (kAct == RR_ACT_SILU || kAct == RR_ACT_GELU_TANH) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-            const f32x2 x = pack2(v[j], v[j + 1]);
-            f32x2 w;  // -log2(e) times the argument of the sigmoid
-            if (kAct == RR_ACT_SILU) w = mul2(x, pack2(-kLog2e, -kLog2e));
-            else w = mul2(x, fma2(mul2(x, x), pack2(-kLog2e * kTanhA * kTanhB, -kLog2e * kTanhA * kTanhB), pack2(-kLog2e * kTanhA, -kLog2e * kTanhA)));
-            float w0, w1;
-            unpack2(w, w0, w1);
-            unpack2(add2(pack2(ex2(w0), ex2(w1)), pack2(1.0f, 1.0f)), w0, w1);
-            unpack2(mul2(pack2(fmaxf(v[j], -FLT_MAX), fmaxf(v[j + 1], -FLT_MAX)), pack2(rcp(w0), rcp(w1))), v[j], v[j + 1]);
+            float a, b;
+            unpack2(sigmoid_argument<kAct>(pack2(v[j], v[j + 1])), a, b);
+            unpack2(add2(pack2(ex2(a), ex2(b)), pack2(1.0f, 1.0f)), a, b);
+            unpack2(mul2(pack2(fmaxf(v[j], -FLT_MAX), fmaxf(v[j + 1], -FLT_MAX)), pack2(rcp(a), rcp(b))), v[j], v[j + 1]);
         }
     }
     if constexpr (kAct == RR_ACT_GELU) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-            // normal_cdf_pdf on a pair; Phi = 1/2 +- (1/2 - tail / 2), the sign that of v
-            const f32x2 x = pack2(v[j], v[j + 1]);
-            const f32x2 t2 = mul2(mul2(x, x), pack2(-0.5f * kLog2e, -0.5f * kLog2e));
-            const f32x2 d = fma2(pack2(fabsf(v[j]), fabsf(v[j + 1])), pack2(0.3275911f * 0.70710678f, 0.3275911f * 0.70710678f), pack2(1.0f, 1.0f));
-            float a, b;
-            unpack2(d, a, b);
-            const f32x2 u = pack2(rcp(a), rcp(b));
-            unpack2(t2, a, b);
-            const f32x2 e = pack2(ex2(a), ex2(b));
-            f32x2 q = fma2(pack2(0.5f * 1.061405429f, 0.5f * 1.061405429f), u, pack2(0.5f * -1.453152027f, 0.5f * -1.453152027f));
-            q = fma2(q, u, pack2(0.5f * 1.421413741f, 0.5f * 1.421413741f));
-            q = fma2(q, u, pack2(0.5f * -0.284496736f, 0.5f * -0.284496736f));
-            q = fma2(q, u, pack2(0.5f * 0.254829592f, 0.5f * 0.254829592f));
-            float h0, h1;  // 1/2 - half the tail
-            unpack2(fma2(mul2(q, u), mul2(e, pack2(-1.0f, -1.0f)), pack2(0.5f, 0.5f)), h0, h1);
+            float h0, h1;
+            f32x2 e;
+            normal_pair(v[j], v[j + 1], h0, h1, e);
             unpack2(mul2(pack2(fmaxf(v[j], -FLT_MAX), fmaxf(v[j + 1], -FLT_MAX)), add2(pack2(copysignf(h0, v[j]), copysignf(h1, v[j + 1])), pack2(0.5f, 0.5f))),
                     v[j], v[j + 1]);
         }
