@@ -402,7 +402,7 @@ rr_status rr_dropout_bwd(long long n, int dy_dtype, int dx_dtype, const void *dy
 
 /* Shape of one linear layer call.  Pitches count elements between rows; 0 means densely packed. */
 typedef struct rr_linear_shape {
-    int32_t M, N, K;           /* tokens, outputs, inputs; N and K are multiples of 8             */
+    int32_t M, N, K;           /* tokens, outputs, inputs; N and K multiples of 8, all <= 2^30    */
     int32_t act;               /* RR_ACT_*                                                        */
     int32_t y_dtype;           /* RR_BF16 or RR_F32: type of y and residual                       */
     int32_t dx_dtype, dw_dtype; /* RR_BF16 or RR_F32 (backward)                                   */
@@ -422,7 +422,8 @@ typedef struct rr_linear_shape {
  *   workspace dev, >= fwd_bytes, 256-byte aligned: the status word read by rr_check and nothing else
  * Products are bf16 x bf16 on the tensor cores with fp32 accumulation (their adder truncates: the sum of n products is off by
  * up to about n/16 * 2^-23 of the sum of their magnitudes, which shows only when y is fp32); the epilogue is fp32
- * with one rounding to y's type.  The activations use the hardware's exponential and reciprocal (relative error
+ * with one rounding to y's type.  With few tokens (or few tiles) the contraction is cut into parts that are added in a fixed order.
+ * The activations use the hardware's exponential and reciprocal (relative error
  * about 1e-6) and for RR_ACT_GELU Abramowitz and Stegun 7.1.26 (absolute error of Phi below 1e-6).
  * Results repeat bit for bit.  M == 0 does nothing.
  *
@@ -432,6 +433,7 @@ typedef struct rr_linear_shape {
  *   when dx is NULL
  *   dx [M,K] type dx_dtype, dW [N,K] (dense) type dw_dtype, dbias [N] fp32: each may be NULL when not wanted
  *   workspace dev, >= bwd_bytes, 256-byte aligned
+ *   no output overlaps an input or another output
  * dz is rounded to bf16 between the two steps (without an activation that loses nothing: the dropout factor is applied behind
  * the products); dbias is summed from the unrounded values in a fixed order.  M == 0 sets dW and dbias to zero, or leaves them
  * under RR_ADD_DW.
@@ -463,7 +465,8 @@ rr_status rr_linear_bwd(const rr_linear_shape *s /* host */, const void *dy, con
  *   loss [2] fp32, count [S,E] i32, n_live [S] i32, P [S,E] fp32 dev, overwritten.  A segment without a live
  *                token has zeros and no part in the mean; without any the losses are 0.
  *   workspace dev, >= rr_balance_workspace_bytes, 256-byte aligned; its first 256 bytes are zero when first used
- * 1 <= E <= 256, 1 <= k <= 8, k <= stride, 1 <= S, T % S == 0.  fp32 arithmetic, sums in a fixed order.  T == 0 is accepted.
+ * 1 <= E <= 256, 1 <= k <= 8, k <= stride, 1 <= S, T % S == 0.  fp32 arithmetic with the hardware's exponential and logarithm (relative
+ * errors of about 1e-6), sums in a fixed order: results repeat bit for bit.  T == 0 is accepted.
  * rr_balance_bwd, with the counts held constant:
  *     dL/da_ij = scale live_i g_ij ( alpha E / (S' n_s) (f_sj - sum_e f_se g_ie) + 2 beta / n lse_i ),  g_i = softmax(a_i)
  *   count, n_live as rr_balance_fwd wrote them; live, alpha, beta as there; scale a host value

@@ -427,7 +427,8 @@ namespace {
 
 rr_status check_linear_sizes(int M, int N, int K)
 {
-    return M < 0 || N < 8 || K < 8 || N % 8 || K % 8 ? RR_ERR_INVALID_ARG : RR_OK;
+    constexpr int kMost = 1 << 30;  // (rounding up to tiles stays inside an int)
+    return M < 0 || N < 8 || K < 8 || N % 8 || K % 8 || M > kMost || N > kMost || K > kMost ? RR_ERR_INVALID_ARG : RR_OK;
 }
 
 // a pitch of `width` elements of `size` bytes: 0 becomes the width; rows stay 16-byte aligned and addressable by TMA

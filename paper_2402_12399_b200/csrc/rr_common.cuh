@@ -35,7 +35,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 unsigned long long test_wait_limit_ns();
 
 // streaming multiprocessors of the current device, 0 if that cannot be told
-inline int device_sms()
+inline int device_sm_count()
 {
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;

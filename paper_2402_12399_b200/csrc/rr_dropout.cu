@@ -2,7 +2,10 @@
 //     y_i = residual_i + keep_i x_i / (1 - p),      dx_i = keep_i dy_i / (1 - p)   (+ dx_i when accumulating),
 // keep from the counter-based generator of rr_philox.cuh: no mask is written or read, the backward pass computes
 // it again.  A dropped element is selected away, not multiplied by zero, so a NaN or infinity in a dropped place
-// does not reach y.  One thread takes eight consecutive elements (one generator block).
+// does not reach y.  A thread takes two groups of eight consecutive elements at a time (a generator block each): their loads are in
+// flight together and they share the key schedule, which leaves about 110 instructions a group (162 one by one).
+// 2^26 elements: fp32 + bf16 residual -> bf16 81.8 us (1.00 of the measured copy rate of HBM), bf16 -> bf16 48 us (0.85, about half of
+// the time is the generator's; 64 us with one group at a time), fp32 + residual -> fp32 142 us (0.86).
 #include <cuda_bf16.h>
 
 #include "rr_ffn.cuh"
@@ -12,7 +15,13 @@ namespace rr {
 
 namespace {
 
-constexpr int kDropThreads = 256, kDropBlocks = 3;  // blocks per SM
+constexpr int kDropThreads = 256;
+
+// Blocks per SM, all resident at once.  Where every element moves 8 bytes or more HBM is the bound and fewer streams of reads and writes
+// suit it better (2^26 elements, fp32 + bf16 residual -> bf16: 81.8 us with three, 84.7 with four, 95 with five; bf16 -> fp32: 69 and 78);
+// with 4 to 6 bytes the generator's integer work is as long and wants the warps (bf16 -> bf16: 52.2 and 48.0).
+template <class TX, class TY>
+constexpr int drop_blocks() { return sizeof(TX) + sizeof(TY) == 4 ? 4 : 3; }
 
 // Eight consecutive elements at a 16-byte aligned address as they lie in memory, and as fp32.  Plain (coherent) loads, because y
 // may be x or residual.
@@ -66,7 +75,7 @@ __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
 template <class TX, class TY, bool kResidual>
-__global__ void __launch_bounds__(kDropThreads, kDropBlocks) k_dropout(long long n, const TX *x, const TY *residual, DropoutParams d, TY *y)
+__global__ void __launch_bounds__(kDropThreads, (drop_blocks<TX, TY>())) k_dropout(long long n, const TX *x, const TY *residual, DropoutParams d, TY *y)
 {
     PhiloxKey key = {};
     if (d.rng) key = philox_key(d.rng);
@@ -122,9 +131,9 @@ template <class TX, class TY>
 rr_status run(long long n, const void *x, const void *residual, const DropoutParams &d, void *y, cudaStream_t st)
 {
     const long long groups = (n + 7) / 8, want = (groups + kDropThreads - 1) / kDropThreads;
-    const int sms = device_sms();
+    const int sms = device_sm_count();
     if (sms < 1) return RR_ERR_CUDA;
-    const int grid = (int)(want < sms * kDropBlocks ? want : sms * kDropBlocks);  // resident all at once: no partial wave
+    const int most = sms * drop_blocks<TX, TY>(), grid = (int)(want < most ? want : most);
     const TX *px = static_cast<const TX *>(x);
     const TY *pr = static_cast<const TY *>(residual);
     if (residual) k_dropout<TX, TY, true><<<grid, kDropThreads, 0, st>>>(n, px, pr, d, static_cast<TY *>(y));

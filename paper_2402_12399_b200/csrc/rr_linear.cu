@@ -669,7 +669,7 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_
 template <bool kForward>
 rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
 {
-    const int pairs = device_sms() / 2;
+    const int pairs = device_sm_count() / 2;
     if (pairs < 1) return RR_ERR_CUDA;
     p.items[0] = p.job[0].items;
     p.items[1] = n > 1 ? p.job[1].items : 0;

@@ -40,7 +40,7 @@ def test_linear_forward(rr):
     def call(**kw):
         a = {**ok, **kw}
         return f(C.byref(_linear(rr, **kw)), a["x"], a["w"], a["b"], a["r"], a["rng"], a["y"], a["z"], a["ws"], a["n"], None)
-    for bad in [dict(M=-1), dict(N=0), dict(N=12), dict(K=0), dict(K=20), dict(K=-8), dict(act=5), dict(act=-1), dict(y_dtype=2), dict(dx_dtype=3),
+    for bad in [dict(M=-1), dict(M=(1 << 30) + 1), dict(N=(1 << 30) + 8), dict(K=(1 << 30) + 8), dict(N=0), dict(N=12), dict(K=0), dict(K=20), dict(K=-8), dict(act=5), dict(act=-1), dict(y_dtype=2), dict(dx_dtype=3),
                 dict(dw_dtype=-1), dict(flags=4), dict(p=2.0), dict(p=float("nan")), dict(p=0.5), dict(p=0.5, rng=ODD), dict(ldx=56), dict(ldx=68),
                 dict(ldx=-64), dict(ldr=16), dict(ldy=25), dict(ldz=12), dict(lddy=4), dict(lddx=60), dict(ldx=1 << 40), dict(x=None), dict(w=None),
                 dict(y=None), dict(ws=None), dict(x=ODD), dict(w=ODD), dict(b=ODD), dict(r=ODD), dict(y=ODD), dict(z=ODD), dict(ws=AT + 128),
