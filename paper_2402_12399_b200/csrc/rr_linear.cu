@@ -39,6 +39,22 @@ constexpr int kDenseStage = kStageA + kTN / 2 * 128;        // bytes of one k-bl
 constexpr int kDenseStages = 6;
 constexpr size_t kDenseSmem = (size_t)kDenseStages * kDenseStage + kDenseEpiWarps * kEpiBytes + sizeof(DenseShared);
 
+// Division of 0 <= n < 2^31 by a divisor that the host knows: a product and a shift (the warps find their tiles with it; the
+// compiler's division is some twenty dependent instructions, and there were six a tile in front of every epilogue).  With
+// 2^s < d <= 2^(s+1) and mul = ceil(2^(32+s) / d), n mul / 2^(32+s) exceeds n / d by less than n 2^(s+1) / (d 2^(32+s)) <= 1 / d.
+struct FastDiv {
+    uint32_t d, mul, shift;
+    __device__ __forceinline__ int operator()(int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
+};
+FastDiv fast_div(int d)
+{
+    FastDiv f = {(uint32_t)d, 0u, 0u};
+    if (d == 1) return f;
+    while ((2u << f.shift) < (uint32_t)d) ++f.shift;
+    f.mul = (uint32_t)(((1ull << (32 + f.shift)) + d - 1) / d);
+    return f;
+}
+
 // One product of a launch: C[M,N] = A B in tiles of 256 x 256.  *_mn: the operand is MN-major, its rows are the contraction.
 // With split > 1 the contraction of every tile is cut into that many items, whose results go to consecutive matrices
 // of part_rows rows (fp32) for k_combine to add up.
@@ -46,6 +62,7 @@ struct DenseJob {
     CUtensorMap mapA, mapB, mapY, mapZ;
     int M, N, m_tiles, n_tiles, kblocks, items;
     int split, part_rows;
+    FastDiv by_split, by_band, by_last;  // by split, by the tiles of a band, by the row tiles of the last band
     int a_mn, b_mn;
     Epilogue e;
 };
@@ -69,6 +86,7 @@ __device__ __forceinline__ void bias_grad(const BiasGrad &b, int c)
 struct DenseParams {
     DenseJob job[2];
     int items[2];  // of each job
+    int deal, more; // rounds of the first job's items that every pair takes part in, and how many pairs get another one
     int head;      // rounds of the second job's items that only pairs with fewer items of the first take part in
     BiasGrad bias; // (backward)
     int *status;
@@ -82,7 +100,7 @@ struct Item {
 };
 __device__ __forceinline__ Item item_of(const DenseParams &p, int it, int pair, int npairs)
 {
-    const int more = p.items[0] % npairs, mine = p.items[0] / npairs + (pair < more ? 1 : 0);
+    const int more = p.more, mine = p.deal + (pair < more ? 1 : 0);
     if (it < mine) return {0, it * npairs + pair};
     const int k = it - mine, others = npairs - more;
     int at;
@@ -98,9 +116,16 @@ struct Work {
 };
 __device__ __forceinline__ Work work_of(const DenseJob &j, int at)
 {
-    const int t = at / j.split, part = at - t * j.split;
-    const int band = 8 * j.n_tiles, b = t / band, first = 8 * b, high = min(8, j.m_tiles - first), r = t - b * band;
-    return {first + r % high, r / high, part, (int)((long long)j.kblocks * part / j.split), (int)((long long)j.kblocks * (part + 1) / j.split)};
+    const int t = j.by_split(at), part = at - t * j.split;
+    const int b = j.by_band(t), first = 8 * b, r = t - b * (8 * j.n_tiles);
+    const bool whole = first + 8 <= j.m_tiles;
+    const int n = whole ? r >> 3 : j.by_last(r), high = whole ? 8 : j.m_tiles - first;
+    Work w = {first + r - n * high, n, part, 0, j.kblocks};
+    if (j.split > 1) {
+        w.kb0 = j.by_split(j.kblocks * part);
+        w.kb1 = j.by_split(j.kblocks * (part + 1));
+    }
+    return w;
 }
 
 template <bool kForward>
@@ -230,18 +255,22 @@ k_dense(const __grid_constant__ DenseParams p)
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
             fence_after_sync();
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * TN;
+            auto release = [&]() {  // (both CTAs' warps free the accumulator at the leader)
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_peer(lead_tempty + 8u * buf);
+            };
+            if (!mine || col00 + eg * 32 >= j.N) release();
             if (mine) {
 #pragma unroll 1
                 for (int c = eg * 32; c < TN && col00 + c < j.N; c += 128) {
                     float v[32];
                     tmem_ld32(taddr + c, v);
+                    if (c + 128 >= TN || col00 + c + 128 >= j.N) release();  // this warp's last look at the accumulator
                     ew.template chunk<kForward>(j.e, v, sh->bias[eg * 4 + q], row0, w.part * j.part_rows, col00 + c, c + 128 < TN ? col00 + c + 128 : -1, j.M,
                                                  j.N, lane, st, &j.mapY, &j.mapZ);
                 }
             }
-            fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(lead_tempty + 8u * buf);
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -673,6 +702,12 @@ rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
     if (pairs < 1) return RR_ERR_CUDA;
     p.items[0] = p.job[0].items;
     p.items[1] = n > 1 ? p.job[1].items : 0;
+    for (int k = 0; k < n; ++k) {
+        DenseJob &j = p.job[k];
+        j.by_split = fast_div(j.split);
+        j.by_band = fast_div(8 * j.n_tiles);
+        j.by_last = fast_div(j.m_tiles % 8 ? j.m_tiles % 8 : 8);
+    }
     p.head = 0;
     if (n > 1) {  // (an item's epilogue and start count as three k-blocks)
         const int a = p.job[0].kblocks / p.job[0].split + 3, b = p.job[1].kblocks / p.job[1].split + 3;
@@ -680,7 +715,10 @@ rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
     }
     const long long total = (long long)p.items[0] + p.items[1];
     if (cudaFuncSetAttribute(k_dense<kForward>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseSmem) != cudaSuccess) return RR_ERR_CUDA;
-    return launch_dependent(k_dense<kForward>, dim3(2 * (unsigned)(total < pairs ? total : pairs)), kDenseThreads, kDenseSmem, 2, st, p) == cudaSuccess
+    const int used = (int)(total < pairs ? total : pairs);
+    p.deal = p.items[0] / used;
+    p.more = p.items[0] % used;
+    return launch_dependent(k_dense<kForward>, dim3(2 * (unsigned)used), kDenseThreads, kDenseSmem, 2, st, p) == cudaSuccess
                ? RR_OK : RR_ERR_CUDA;
 }
 
