@@ -20,10 +20,11 @@ namespace {
 
 constexpr int kStageA = 128 * 128;       // this CTA's 128 rows of A, one k-block of 64
 constexpr int kPanel = 64 * 128;         // MN-major panel: 64 k-rows x 64 columns
-// Warps: 0-2 TMA producers, 3 MMA issuer and TMEM owner, 4-19 epilogue.  Sixteen epilogue warps, four per scheduler: the
-// epilogue of a forward tile is some forty instructions an element with long dependent chains (generator,
-// activation), as much time as the main loop at K = 1024.
-constexpr int kDenseProducers = 3, kDenseMma = 3, kDenseEpi0 = 4, kDenseEpiWarps = 16;
+// Warps: 0-2 TMA producers, 3 MMA issuer and TMEM owner, 4-15 epilogue.  The epilogue of a forward tile with everything in it is some
+// thirty instructions an element with long dependent chains (generator, activation): at K = 1024 longer than the main loop.  Three warps
+// per scheduler hide them best against the registers they leave each other (2048 x 4096 x 1024 with a residual: 20.7 us with twelve,
+// 21.4 with eight, 22.2 with sixteen; with GELU, dropout and z as well 30.2, 29.5, 30.7; K = 128: 105, 121, 100).
+constexpr int kDenseProducers = 3, kDenseMma = 3, kDenseEpi0 = 4, kDenseEpiWarps = 12;
 constexpr int kDenseThreads = 32 * (kDenseEpi0 + kDenseEpiWarps);
 constexpr int kEpiBytes = 2048;          // staging of one epilogue warp
 
@@ -37,6 +38,7 @@ struct DenseShared {
 constexpr int kTN = 256;                                    // columns of a tile
 constexpr int kDenseStage = kStageA + kTN / 2 * 128;        // bytes of one k-block in one CTA
 constexpr int kDenseStages = 6;
+constexpr int kStep = 32 * (kDenseEpiWarps / 4);            // columns between an epilogue warp's chunks
 constexpr size_t kDenseSmem = (size_t)kDenseStages * kDenseStage + kDenseEpiWarps * kEpiBytes + sizeof(DenseShared);
 
 // Division of 0 <= n < 2^31 by a divisor that the host knows: a product and a shift (the warps find their tiles with it; the
@@ -230,7 +232,7 @@ k_dense(const __grid_constant__ DenseParams p)
             }
         }
     } else {
-        // Epilogue: four warps per TMEM lane quarter take the chunks of 32 columns in turn
+        // Epilogue: three warps per TMEM lane quarter take the chunks of 32 columns in turn
         const int eg = (warp - kDenseEpi0) >> 2, q = warp & 3;
         uint8_t *st = staging + (size_t)(eg * 4 + q) * kEpiBytes;
         EpilogueWarp ew;
@@ -248,8 +250,8 @@ k_dense(const __grid_constant__ DenseParams p)
             const int col00 = w.n * TN;
             const bool mine = row0 < j.M;
             if (mine) ew.template fetch<kForward>(j.e, row0 + lane, col00 + eg * 32, j.M, j.N, lane);
-            // Every warp waits for itself, asleep: sixteen warps that poll would take issue slots from the producers and the MMA
-            // issuer, and a barrier in front of the tile would hold the early ones back.
+            // Every warp waits for itself, asleep: a dozen warps that poll take issue slots from the producers and the MMA issuer (one tile a
+            // pair at K = 4096: 39 us instead of 34), and a barrier in front of the tile holds the early ones back.
             int ok = 1;
             if (lane == 0) ok = mbar_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status) ? 1 : 0;
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
@@ -263,11 +265,11 @@ k_dense(const __grid_constant__ DenseParams p)
             if (!mine || col00 + eg * 32 >= j.N) release();
             if (mine) {
 #pragma unroll 1
-                for (int c = eg * 32; c < TN && col00 + c < j.N; c += 128) {
+                for (int c = eg * 32; c < TN && col00 + c < j.N; c += kStep) {
                     float v[32];
                     tmem_ld32(taddr + c, v);
-                    if (c + 128 >= TN || col00 + c + 128 >= j.N) release();  // this warp's last look at the accumulator
-                    ew.template chunk<kForward>(j.e, v, sh->bias[eg * 4 + q], row0, w.part * j.part_rows, col00 + c, c + 128 < TN ? col00 + c + 128 : -1, j.M,
+                    if (c + kStep >= TN || col00 + c + kStep >= j.N) release();  // this warp's last look at the accumulator
+                    ew.template chunk<kForward>(j.e, v, sh->bias[eg * 4 + q], row0, w.part * j.part_rows, col00 + c, c + kStep < TN ? col00 + c + kStep : -1, j.M,
                                                  j.N, lane, st, &j.mapY, &j.mapZ);
                 }
             }
