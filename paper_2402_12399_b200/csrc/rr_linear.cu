@@ -252,9 +252,7 @@ k_dense(const __grid_constant__ DenseParams p)
             if (mine) ew.template fetch<kForward>(j.e, row0 + lane, col00 + eg * 32, j.M, j.N, lane);
             // Every warp waits for itself, asleep: a dozen warps that poll take issue slots from the producers and the MMA issuer (one tile a
             // pair at K = 4096: 39 us instead of 34), and a barrier in front of the tile holds the early ones back.
-            int ok = 1;
-            if (lane == 0) ok = mbar_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status) ? 1 : 0;
-            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            if (!warp_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status)) break;
             fence_after_sync();
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * TN;
             auto release = [&]() {  // (both CTAs' warps free the accumulator at the leader)
@@ -274,13 +272,13 @@ k_dense(const __grid_constant__ DenseParams p)
                 }
             }
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the staging tiles stay until they are read)
     }
 
     __syncwarp();
     __syncthreads();
     if (sh->abort_flag) __nanosleep(2000000);  // let copies that are still in flight land
-    cluster_sync_all();  // neither CTA leaves while its peer may still signal its barriers
+    cluster_sync_all();  // neither CTA leaves before what its peer has signalled it has arrived (a release: it waits for that)
     if (warp == kDenseMma) {
         fence_after_sync();
         tmem_dealloc_pair(tmem_base, 2 * TN);
@@ -398,7 +396,7 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
             }
             if (ok) mma_commit_one(&sh->done);
         }
-    } else if (warp_wait(&sh->done, 0, abort_flag, p.status)) {
+    } else if (warp_wait_brisk(&sh->done, 0, abort_flag, p.status)) {
         // every load has landed and every MMA has read its operands: the ring's memory takes the partial tile,
         // [token][128 features]
         fence_after_sync();
@@ -456,7 +454,9 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
         __nanosleep(2000000);  // let copies that are still in flight land
     }
     __syncwarp();
-    if (p.split > 1) cluster_sync_all();  // no CTA leaves while another may still read its partial tile
+    // No CTA leaves while another may still read its partial tile; every such read has been added up by now, and there is no other
+    // traffic between the CTAs, so the barrier need not order anything.
+    if (p.split > 1) cluster_sync_relaxed();
     if (warp == 1) {
         fence_after_sync();
         tmem_dealloc_one(tmem_base, kCols);

@@ -113,6 +113,14 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volati
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
+// Lane 0 waits asleep, the whole warp learns the outcome.
+__device__ __forceinline__ bool warp_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status)
+{
+    int ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = mbar_wait_brisk(bar, parity, abort_flag, status) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
 // ---- TMA ------------------------------------------------------------------------------
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *m)
 {
@@ -204,6 +212,12 @@ __device__ __forceinline__ uint32_t map_to_cta(const void *p, uint32_t rank)
 __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same barrier where nothing written has to be visible behind it -- it only keeps a CTA's shared memory and barriers in place until
+// its peers are done with them.  (A release waits for this CTA's stores to global memory: about a microsecond at the end of a kernel.)
+__device__ __forceinline__ void cluster_sync_relaxed()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // arrive on an mbarrier given by its shared::cluster address (may live in the peer CTA)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
