@@ -47,9 +47,10 @@ __device__ __forceinline__ void load_row(const float *__restrict__ a, bool in, i
     }
 }
 // g becomes exp(a - m), m the row's maximum; returns log sum_e exp(a_e) and, in inv, the factor that makes g the softmax.  These
-// kernels are bound by the instructions they issue, so: one fused multiply-add per pair of columns, the hardware's exponential,
-// logarithm and reciprocal (relative errors of about 2^-22).  The shift is the rounded product m log2(e) itself, which
-// the logarithm adds back, so its rounding cancels.  The row of a dead token gives garbage that its group keeps to itself.
+// kernels are bound by the instructions they issue, so: packed pairs of columns, the hardware's exponential, logarithm and reciprocal
+// (relative errors of about 2^-22).  The maximum is taken off before anything is multiplied, so that a row whose scores are all the type's
+// lowest value (a mask that leaves nothing) is a uniform one and not a difference of infinities.  The row of a dead token gives
+// garbage that its group keeps to itself.
 template <int GS, int CPL>
 __device__ __forceinline__ float softmax_lse(float (&g)[CPL], float &inv)
 {
@@ -57,13 +58,13 @@ __device__ __forceinline__ float softmax_lse(float (&g)[CPL], float &inv)
     float m = -INFINITY;
 #pragma unroll
     for (int c = 0; c < CPL; ++c) m = fmaxf(m, g[c]);
-    const float shift = group_max<GS>(m) * kLog2e;
+    m = group_max<GS>(m);
     float z = 0.f;
     if constexpr (CPL % 2 == 0) {
         f32x2 sum = pack2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < CPL; c += 2) {
-            unpack2(fma2(pack2(g[c], g[c + 1]), pack2(kLog2e, kLog2e), pack2(-shift, -shift)), g[c], g[c + 1]);
+            unpack2(mul2(add2(pack2(g[c], g[c + 1]), pack2(-m, -m)), pack2(kLog2e, kLog2e)), g[c], g[c + 1]);
             g[c] = ex2(g[c]);  // (exp(-inf) = 0 for the columns past E)
             g[c + 1] = ex2(g[c + 1]);
             sum = add2(sum, pack2(g[c], g[c + 1]));
@@ -74,13 +75,13 @@ __device__ __forceinline__ float softmax_lse(float (&g)[CPL], float &inv)
     } else {
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-            g[c] = ex2(fmaf(g[c], kLog2e, -shift));
+            g[c] = ex2((g[c] - m) * kLog2e);
             z += g[c];
         }
     }
     z = group_sum<GS>(z);
     inv = rcp(z);
-    return (shift + lg2(z)) * 0.693147180559945f;
+    return fmaf(lg2(z), 0.693147180559945f, m);
 }
 // acc += inv * g
 template <int CPL>
@@ -337,7 +338,7 @@ k_balance_final(const BalShape b, float alpha, float beta, const BalScratch w, f
         w.hdr->sync[8] = 0;
     }
     loss[0] = segs > 0 ? alpha * (float)E / (float)segs * dots : 0.f;
-    loss[1] = live > 0 ? beta / (float)live * z : 0.f;
+    loss[1] = live > 0 && beta != 0.f ? beta / (float)live * z : 0.f;  // (the sum may be infinite)
 }
 
 // Backward: items of up to `slab` tokens of one segment, dealt to the blocks in turn.

@@ -75,6 +75,29 @@ def test_batch_of_padded_sequences_with_garbage_behind_their_ends():
     assert all(torch.equal(x, y) for x, y in zip((loss, count, n, P, d), again))   # and the results repeat
 
 
+def test_masked_experts_of_live_tokens():
+    """Scores at the type's lowest value: of some experts (they get nothing), and of a whole row (a uniform one; its log-sum-exp is out
+    of range, so the z-loss is off)."""
+    import paper_2402_12399_b200 as rr
+    low = torch.finfo(torch.float32).min
+    for E in (5, 8, 64):
+        a, table, _ = _inputs(2, 300, E, 2, E)
+        a[::7, : E // 2] = low
+        a[5, 1:] = float("-inf")
+        table = torch.topk(a, 2, 1).indices.int().contiguous()
+        _check(torch.nan_to_num(a, neginf=low), table, 2, 2, None)
+        first = rr.balance_fwd(a, table, 2, 0.1, 0.1, segments=2)
+        a[5, 1:] = low
+        assert all(torch.equal(x, y) for x, y in zip(first, rr.balance_fwd(a, table, 2, 0.1, 0.1, segments=2)))
+        a[77] = low
+        loss, count, n, P = rr.balance_fwd(a, table, 2, 0.1, segments=2)
+        b = a.clone()
+        b[77] = 0                                               # a uniform row like any other
+        want = rr.balance_fwd(b, table, 2, 0.1, segments=2)
+        assert torch.equal(P, want[3]) and torch.equal(loss, want[0]) and float(loss[1]) == 0
+        assert torch.equal(rr.balance_bwd(a, count, n, 2, 0.1), rr.balance_bwd(b, count, n, 2, 0.1))
+
+
 def test_many_and_few_segments():
     for S, L in ((4096, 3), (1, 65536), (592, 5), (1000, 1)):
         _check(*_inputs(S, L, 8, 2, S)[:2], 2, S, None)

@@ -196,6 +196,19 @@ def test_in_place_residual_and_parts_of_the_gradient():
         assert all(torch.equal(part[i], bufs[i]) for i in keep)
 
 
+def test_everything_dropped():
+    import paper_2402_12399_b200 as rr
+    g = torch.Generator("cuda").manual_seed(4)
+    for M in (3, 300):
+        x, w, r, rng = _ints(g, M, 64), _ints(g, 72, 64), _ints(g, M, 72), _rng(1)
+        x[0] = float("nan")
+        assert torch.equal(rr.linear_fwd(x, w, residual=r, act=rr.ACT_GELU, p=1.0, rng=rng), r)
+        dx, dw, db = torch.ones(M, 64, device="cuda"), torch.ones(72, 64, device="cuda"), torch.ones(72, device="cuda")
+        x[0] = 1
+        rr.linear_bwd(r, x, w, p=1.0, rng=rng, dx=dx, dw=dw, dbias=db)
+        assert not dx.any() and not dw.any() and not db.any()
+
+
 def test_no_tokens():
     import paper_2402_12399_b200 as rr
     x, w = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(8, 64, dtype=torch.bfloat16, device="cuda")
