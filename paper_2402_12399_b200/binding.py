@@ -461,9 +461,16 @@ def aux_loss_bwd(logits: torch.Tensor, f: torch.Tensor, alpha: float, scale: flo
 
 
 # ---- the parts of a block around the expert layer ------------------------------------------------------
-# Their calls are short next to the interpreter's time per call, so the checks and the marshalling below are kept lean.
+# Their kernels often run no longer than the interpreter needs for a call, so the checks below ask their questions in line and go
+# to a helper only to say what is wrong.
 
-_TYPE_CODE = {torch.bfloat16: BF16, torch.float32: F32}
+_BF = torch.bfloat16
+_F32 = torch.float32
+_I32 = torch.int32
+_TYPE_CODE = {_BF: BF16, _F32: F32}
+_here = torch.cuda.current_device
+# the current stream's handle without a Stream object around it: 0.1 us instead of 3
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _code(t: torch.Tensor, what: str) -> int:
@@ -473,29 +480,22 @@ def _code(t: torch.Tensor, what: str) -> int:
     return code
 
 
-def _on_device(*tensors) -> None:
-    """Every tensor lies on the current device, whose current stream the call uses."""
-    here = torch.cuda.current_device()
+def _elsewhere(here, *tensors):
+    """Raises for the first tensor that is not on the current device, whose current stream the call uses."""
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the call runs on the current device cuda:{here}")
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _raw_stream() -> int:
-    # (the stream's handle without a Stream object around it: 0.1 us instead of 3)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-
-
-def _check_rng(rng, p: float) -> None:
+def _rng_ptr(rng, p: float):
+    """Address of the generator state {seed, offset}."""
     if rng is None:
         if p:
             raise ValueError("dropout needs rng: two int64 on the device, {seed, offset}")
-    elif rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous():
+        return None
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous():
         raise TypeError("rng is two contiguous int64 (or uint64), {seed, offset}")
+    return rng.data_ptr()
 
 
 def _same_shape(t, shape, what):
@@ -509,16 +509,20 @@ def dropout_fwd(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: t
     `rng` is {seed, offset}, two int64 on the device; the mask is a function of it and the flat element index."""
     if out is None:
         out = torch.empty(x.shape, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
-    _on_device(x, residual, rng, out)
-    _check_rng(rng, p)
-    _same_shape(out, x.shape, "out")
-    _same_shape(residual, x.shape, "residual")
+    here = _here()
+    _elsewhere(here, x, residual, rng, out)
+    if out.shape != x.shape or (residual is not None and residual.shape != x.shape):
+        _same_shape(out, x.shape, "out")
+        _same_shape(residual, x.shape, "residual")
     if not (x.is_contiguous() and out.is_contiguous() and (residual is None or residual.is_contiguous())):
         raise ValueError("dropout takes contiguous tensors")
     if residual is not None and residual.dtype != out.dtype:
         raise TypeError(f"residual is {residual.dtype}, the result {out.dtype}")
-    _ok(lib().rr_dropout_fwd(x.numel(), _code(x, "x"), _code(out, "out"), x.data_ptr(), _at(residual), p, _at(rng), out.data_ptr(),
-                             _raw_stream()), "rr_dropout_fwd")
+    code = (_lib or lib()).rr_dropout_fwd(x.numel(), _code(x, "x"), _code(out, "out"), x.data_ptr(),
+                                          None if residual is None else residual.data_ptr(), p, _rng_ptr(rng, p), out.data_ptr(),
+                                          _stream_of(here))
+    if code:
+        raise RRError(code, "rr_dropout_fwd")
     return out
 
 
@@ -530,13 +534,16 @@ def dropout_bwd(dy: torch.Tensor, p: float, rng: torch.Tensor | None, out: torch
         if accumulate:
             raise ValueError("accumulate needs out")
         out = torch.empty(dy.shape, dtype=out_dtype or dy.dtype, device=dy.device)
-    _on_device(dy, rng, out)
-    _check_rng(rng, p)
-    _same_shape(out, dy.shape, "out")
+    here = _here()
+    _elsewhere(here, dy, rng, out)
+    if out.shape != dy.shape:
+        _same_shape(out, dy.shape, "out")
     if not (dy.is_contiguous() and out.is_contiguous()):
         raise ValueError("dropout takes contiguous tensors")
-    _ok(lib().rr_dropout_bwd(dy.numel(), _code(dy, "dy"), _code(out, "out"), dy.data_ptr(), p, _at(rng), int(accumulate), out.data_ptr(),
-                             _raw_stream()), "rr_dropout_bwd")
+    code = (_lib or lib()).rr_dropout_bwd(dy.numel(), _code(dy, "dy"), _code(out, "out"), dy.data_ptr(), p, _rng_ptr(rng, p),
+                                          1 if accumulate else 0, out.data_ptr(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_dropout_bwd")
     return out
 
 
@@ -548,22 +555,24 @@ def linear_workspace_bytes(M: int, N: int, K: int):
 
 
 def _pitch(t, rows: int, cols: int, what: str) -> int:
-    """Elements between the rows of a [rows, cols] matrix whose columns lie together (0: not given)."""
+    """Elements between the rows of a [rows, cols] matrix whose columns lie together (0: not given, or densely packed)."""
     if t is None:
         return 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if t.is_contiguous():
+        return 0
     row, col = t.stride()
     if col != 1:
         raise ValueError(f"{what} must be row-major, its columns are {col} elements apart")
-    if rows > 1 and row < cols:
+    if row < cols:
         raise ValueError(f"the rows of {what} overlap")
-    return row if rows > 1 else 0
+    return row
 
 
-def _bf16(**tensors):
+def _not_bf16(**tensors):
     for what, t in tensors.items():
-        if t is not None and t.dtype != torch.bfloat16:
+        if t is not None and t.dtype != _BF:
             raise TypeError(f"{what} must be bfloat16, got {t.dtype}")
 
 
@@ -576,22 +585,27 @@ def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = Non
     M, K = x.shape
     N = W.shape[0]
     if out is None:
-        out = torch.empty(M, N, dtype=out_dtype or (torch.bfloat16 if residual is None else residual.dtype), device=x.device)
+        out = torch.empty(M, N, dtype=out_dtype or (_BF if residual is None else residual.dtype), device=x.device)
     if workspace is None:
         workspace = alloc_workspace(linear_workspace_bytes(M, N, K)[0], x.device)
-    _on_device(x, W, bias, residual, rng, out, z, workspace)
-    _bf16(x=x, W=W, bias=bias, z=z)
-    _check_rng(rng, p)
-    _same_shape(W, (N, K), "W")
-    _same_shape(bias, (N,), "bias")
+    here = _here()
+    _elsewhere(here, x, W, bias, residual, rng, out, z, workspace)
+    if x.dtype != _BF or W.dtype != _BF or (bias is not None and bias.dtype != _BF) or (z is not None and z.dtype != _BF):
+        _not_bf16(x=x, W=W, bias=bias, z=z)
+    if W.shape != (N, K) or (bias is not None and bias.shape != (N,)):
+        _same_shape(W, (N, K), "W")
+        _same_shape(bias, (N,), "bias")
     if not W.is_contiguous() or (bias is not None and not bias.is_contiguous()):
         raise ValueError("W and bias must be contiguous")
     if residual is not None and residual.dtype != out.dtype:
         raise TypeError(f"residual is {residual.dtype}, the result {out.dtype}")
     s = _CLinear(M, N, K, act, _code(out, "out"), 0, 0, 0, p, _pitch(x, M, K, "x"), _pitch(residual, M, N, "residual"),
                  _pitch(out, M, N, "out"), _pitch(z, M, N, "z"), 0, 0)
-    _ok(lib().rr_linear_fwd(C.byref(s), x.data_ptr(), W.data_ptr(), _at(bias), _at(residual), _at(rng), out.data_ptr(), _at(z),
-                            workspace.data_ptr(), workspace.numel(), _raw_stream()), "rr_linear_fwd")
+    code = (_lib or lib()).rr_linear_fwd(C.byref(s), x.data_ptr(), W.data_ptr(), None if bias is None else bias.data_ptr(),
+                                         None if residual is None else residual.data_ptr(), _rng_ptr(rng, p), out.data_ptr(),
+                                         None if z is None else z.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_linear_fwd")
     out._workspace = workspace
     return out
 
@@ -606,21 +620,28 @@ def linear_bwd(dy: torch.Tensor, x: torch.Tensor | None, W: torch.Tensor, z: tor
     K = W.shape[1]
     if workspace is None:
         workspace = alloc_workspace(linear_workspace_bytes(M, N, K)[1], dy.device)
-    _on_device(dy, x, W, z, rng, dx, dw, dbias, workspace)
-    _bf16(dy=dy, x=x, W=W, z=z)
-    _check_rng(rng, p)
-    _same_shape(W, (N, K), "W")
-    _same_shape(dw, (N, K), "dw")
-    _same_shape(dbias, (N,), "dbias")
-    if not W.is_contiguous() or (dw is not None and not dw.is_contiguous()) or (dbias is not None and not dbias.is_contiguous()):
-        raise ValueError("W, dw and dbias must be contiguous")
-    if dbias is not None and dbias.dtype != torch.float32:
-        raise TypeError(f"dbias must be float32, got {dbias.dtype}")
+    here = _here()
+    _elsewhere(here, dy, x, W, z, rng, dx, dw, dbias, workspace)
+    if dy.dtype != _BF or W.dtype != _BF or (x is not None and x.dtype != _BF) or (z is not None and z.dtype != _BF):
+        _not_bf16(dy=dy, x=x, W=W, z=z)
+    if W.shape != (N, K) or not W.is_contiguous():
+        _same_shape(W, (N, K), "W")
+        raise ValueError("W must be contiguous")
+    if dw is not None and (dw.shape != (N, K) or not dw.is_contiguous()):
+        _same_shape(dw, (N, K), "dw")
+        raise ValueError("dw must be contiguous")
+    if dbias is not None and (dbias.shape != (N,) or not dbias.is_contiguous() or dbias.dtype != _F32):
+        _same_shape(dbias, (N,), "dbias")
+        raise TypeError(f"dbias must be contiguous float32, got {dbias.dtype}")
     s = _CLinear(M, N, K, act, 0, 0 if dx is None else _code(dx, "dx"), 0 if dw is None else _code(dw, "dw"),
                  (ADD_DX if add_dx else 0) | (ADD_DW if add_dw else 0), p, _pitch(x, M, K, "x"), 0, 0, _pitch(z, M, N, "z"),
                  _pitch(dy, M, N, "dy"), _pitch(dx, M, K, "dx"))
-    _ok(lib().rr_linear_bwd(C.byref(s), dy.data_ptr(), _at(x), W.data_ptr(), _at(z), _at(rng), _at(dx), _at(dw), _at(dbias),
-                            workspace.data_ptr(), workspace.numel(), _raw_stream()), "rr_linear_bwd")
+    code = (_lib or lib()).rr_linear_bwd(C.byref(s), dy.data_ptr(), None if x is None else x.data_ptr(), W.data_ptr(),
+                                         None if z is None else z.data_ptr(), _rng_ptr(rng, p), None if dx is None else dx.data_ptr(),
+                                         None if dw is None else dw.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                                         workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_linear_bwd")
     for t in (dx, dw, dbias):
         if t is not None:
             t._workspace = workspace
@@ -635,7 +656,7 @@ def balance_workspace_bytes(T: int, E: int, segments: int = 1) -> int:
 
 
 def _check_scores(logits, live):
-    if logits.dtype != torch.float32 or logits.dim() != 2 or not logits.is_contiguous():
+    if logits.dtype != _F32 or not logits.is_contiguous():
         raise TypeError("logits is a contiguous float32 [T,E]")
     if live is not None and (live.dtype not in (torch.uint8, torch.bool) or live.numel() != logits.shape[0] or not live.is_contiguous()):
         raise TypeError("live is a contiguous uint8 or bool with one element per token")
@@ -648,24 +669,26 @@ def balance_fwd(logits: torch.Tensor, topk_expert: torch.Tensor, k: int, alpha: 
     T, E = logits.shape
     if workspace is None:
         workspace = alloc_workspace(balance_workspace_bytes(T, E, segments), logits.device)
+    here = _here()
     if out is None:
         dev = logits.device
-        out = (torch.empty(2, dtype=torch.float32, device=dev), torch.empty(segments, E, dtype=torch.int32, device=dev),
-               torch.empty(segments, dtype=torch.int32, device=dev), torch.empty(segments, E, dtype=torch.float32, device=dev))
+        out = (torch.empty(2, dtype=_F32, device=dev), torch.empty(segments, E, dtype=_I32, device=dev),
+               torch.empty(segments, dtype=_I32, device=dev), torch.empty(segments, E, dtype=_F32, device=dev))
     else:
-        for t, shape, dtype in zip(out, ((2,), (segments, E), (segments,), (segments, E)),
-                                   (torch.float32, torch.int32, torch.int32, torch.float32)):
+        for t, shape, dtype in zip(out, ((2,), (segments, E), (segments,), (segments, E)), (_F32, _I32, _I32, _F32)):
             if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
                 raise ValueError(f"out: expected contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-        _on_device(*out)
+        _elsewhere(here, *out)
     loss, count, n_live, P = out
-    _on_device(logits, topk_expert, live, workspace)
+    _elsewhere(here, logits, topk_expert, live, workspace)
     _check_scores(logits, live)
-    if topk_expert.dtype != torch.int32 or topk_expert.dim() != 2 or topk_expert.shape[0] != T or not topk_expert.is_contiguous():
+    if topk_expert.dtype != _I32 or topk_expert.dim() != 2 or topk_expert.shape[0] != T or not topk_expert.is_contiguous():
         raise TypeError("topk_expert is a contiguous int32 [T,n]")
-    _ok(lib().rr_balance_fwd(T, E, k, topk_expert.shape[1], segments, logits.data_ptr(), topk_expert.data_ptr(), _at(live), alpha, beta,
-                             loss.data_ptr(), count.data_ptr(), n_live.data_ptr(), P.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                             _raw_stream()), "rr_balance_fwd")
+    code = (_lib or lib()).rr_balance_fwd(T, E, k, topk_expert.shape[1], segments, logits.data_ptr(), topk_expert.data_ptr(),
+                                          None if live is None else live.data_ptr(), alpha, beta, loss.data_ptr(), count.data_ptr(),
+                                          n_live.data_ptr(), P.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_balance_fwd")
     loss._workspace = workspace
     return out
 
@@ -678,15 +701,18 @@ def balance_bwd(logits: torch.Tensor, count: torch.Tensor, n_live: torch.Tensor,
     if dlogits is None:
         if accumulate:
             raise ValueError("accumulate needs dlogits")
-        dlogits = torch.empty(T, E, dtype=torch.float32, device=logits.device)
-    _on_device(logits, count, n_live, live, dlogits)
+        dlogits = torch.empty(T, E, dtype=_F32, device=logits.device)
+    here = _here()
+    _elsewhere(here, logits, count, n_live, live, dlogits)
     _check_scores(logits, live)
     S = n_live.numel()
-    if count.dtype != torch.int32 or count.shape != (S, E) or not count.is_contiguous() or n_live.dtype != torch.int32 or \
-            not n_live.is_contiguous():
+    if count.dtype != _I32 or count.shape != (S, E) or not count.is_contiguous() or n_live.dtype != _I32 or not n_live.is_contiguous():
         raise TypeError("count and n_live are what balance_fwd returned")
-    if dlogits.dtype != torch.float32 or dlogits.shape != (T, E) or not dlogits.is_contiguous():
+    if dlogits.dtype != _F32 or dlogits.shape != (T, E) or not dlogits.is_contiguous():
         raise TypeError("dlogits is a contiguous float32 [T,E]")
-    _ok(lib().rr_balance_bwd(T, E, k, S, logits.data_ptr(), count.data_ptr(), n_live.data_ptr(), _at(live), alpha, beta, scale,
-                             int(accumulate), dlogits.data_ptr(), _raw_stream()), "rr_balance_bwd")
+    code = (_lib or lib()).rr_balance_bwd(T, E, k, S, logits.data_ptr(), count.data_ptr(), n_live.data_ptr(),
+                                          None if live is None else live.data_ptr(), alpha, beta, scale, 1 if accumulate else 0,
+                                          dlogits.data_ptr(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_balance_bwd")
     return dlogits

@@ -133,12 +133,10 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
     __shared__ int cnt[kMaxE];
     __shared__ float red_lse[kBalWarps];
     __shared__ int red_n[kBalWarps];
-    // the second kernel is launched as a programmatic dependent: it may be made ready at once (it waits for the whole of this
-    // grid before it reads the partial sums)
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
     for (int j = threadIdx.x; j < E; j += kBalThreads) cnt[j] = 0;
     __syncthreads();
+    dependent_start();
     const int s = blockIdx.x / b.cps, c0 = blockIdx.x - s * b.cps;
     const long long seg0 = s * b.L, t0 = seg0 + (long long)c0 * b.slab;
     const long long t1 = min(seg0 + b.L, t0 + b.slab);
@@ -259,7 +257,7 @@ k_balance_final(const BalShape b, float alpha, float beta, const BalScratch w, f
     const size_t row0 = (size_t)s * b.cps;
     float sum[V] = {}, lse2 = 0.f;
     int cnt[V] = {}, n = 0;
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the first kernel has completed and its sums are visible
+    dependent_start();  // (the first kernel has completed and its sums are visible)
     for (int c = lane; c < b.cps; c += 32) { lse2 += w.plse[row0 + c]; n += w.pn[row0 + c]; }  // (every warp for itself: no barrier)
     if (j < E) {
 #pragma unroll 4
@@ -351,6 +349,7 @@ k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__r
     __shared__ uint32_t buf[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = lane / GS, gl = lane % GS, E = b.E;
     int segs = 0, tokens = 0;
+    dependent_start();
     for (int q = threadIdx.x; q < b.S; q += kBalThreads) {
         const int m = __ldg(n_live + q);
         tokens += m;
@@ -455,8 +454,8 @@ template <int GS, int CPL, bool VEC>
 rr_status run_fwd(const BalShape &b, const float *logits, const int32_t *topk, const uint8_t *live, const BalScratch &w,
                   cudaStream_t st)
 {
-    k_balance_partial<GS, CPL, VEC><<<b.S * b.cps, kBalThreads, 0, st>>>(b, logits, topk, live, w);
-    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    return launch_dependent(k_balance_partial<GS, CPL, VEC>, dim3((unsigned)(b.S * b.cps)), kBalThreads, 0, 1, st, b, logits, topk, live, w) == cudaSuccess
+               ? RR_OK : RR_ERR_CUDA;
 }
 
 template <int GS, int CPL, bool VEC>
@@ -465,8 +464,9 @@ rr_status run_bwd(const BalShape &b, const float *logits, const int *count, cons
 {
     const long long items = (long long)b.S * b.cps;
     const int grid = (int)(items < kBalBlocks ? items : kBalBlocks);
-    k_balance_bwd<GS, CPL, VEC><<<grid, kBalThreads, 0, st>>>(b, logits, count, n, live, coef_b, coef_z, accumulate, dlogits);
-    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    return launch_dependent(k_balance_bwd<GS, CPL, VEC>, dim3(grid), kBalThreads, 0, 1, st, b, logits, count, n, live, coef_b, coef_z, accumulate,
+                            dlogits) == cudaSuccess
+               ? RR_OK : RR_ERR_CUDA;
 }
 
 }  // namespace
@@ -483,18 +483,8 @@ rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float
     rr_status rc = RR_OK;
     RR_ROWS_DISPATCH(rc = run_fwd, E, b, logits, topk, live, w, st);
     if (rc) return rc;
-    // as a programmatic dependent of the first kernel: its launch overlaps the first one's run
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(S);
-    cfg.blockDim = dim3(kBalFinal);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t err = E % 4 == 0 ? cudaLaunchKernelEx(&cfg, k_balance_final<true>, b, alpha, beta, w, loss, count, n_live, P)
-                                       : cudaLaunchKernelEx(&cfg, k_balance_final<false>, b, alpha, beta, w, loss, count, n_live, P);
+    const cudaError_t err = launch_dependent(E % 4 == 0 ? k_balance_final<true> : k_balance_final<false>, dim3(S), kBalFinal, 0, 1, st, b, alpha, beta, w,
+                                             loss, count, n_live, P);
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 

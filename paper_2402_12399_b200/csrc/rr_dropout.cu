@@ -77,6 +77,7 @@ __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bf
 template <class TX, class TY, bool kResidual>
 __global__ void __launch_bounds__(kDropThreads, (drop_blocks<TX, TY>())) k_dropout(long long n, const TX *x, const TY *residual, DropoutParams d, TY *y)
 {
+    dependent_start();
     PhiloxKey key = {};
     if (d.rng) key = philox_key(d.rng);
     const uint32_t bound = keep_bound(d.drop);
@@ -136,9 +137,9 @@ rr_status run(long long n, const void *x, const void *residual, const DropoutPar
     const int most = sms * drop_blocks<TX, TY>(), grid = (int)(want < most ? want : most);
     const TX *px = static_cast<const TX *>(x);
     const TY *pr = static_cast<const TY *>(residual);
-    if (residual) k_dropout<TX, TY, true><<<grid, kDropThreads, 0, st>>>(n, px, pr, d, static_cast<TY *>(y));
-    else k_dropout<TX, TY, false><<<grid, kDropThreads, 0, st>>>(n, px, pr, d, static_cast<TY *>(y));
-    return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    const cudaError_t err = launch_dependent(residual ? k_dropout<TX, TY, true> : k_dropout<TX, TY, false>, dim3(grid), kDropThreads, 0, 1, st, n, px, pr, d,
+                                             static_cast<TY *>(y));
+    return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 
 }  // namespace

@@ -160,10 +160,8 @@ k_dense(const __grid_constant__ DenseParams p)
     const uint32_t tmem_base = sh->tmem_base;
     volatile int *abort_flag = &sh->abort_flag;
     const uint32_t lead_full = map_to_cta(&sh->full[0], 0), lead_tempty = map_to_cta(&sh->tempty[0], 0);
-    // Launched as a programmatic dependent: all of the above overlaps the end of the kernel in front; nothing it wrote is
-    // read, and nothing written, before this wait.
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (all of the above overlaps the end of the kernel in front)
+    dependent_start();
 
     if (warp < kDenseProducers) {
         // TMA producers: producer j takes the k-blocks j, j + 3, ... of this CTA's stream
@@ -355,10 +353,8 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
     fence_after_sync();
     const uint32_t tmem_base = sh->tmem_base;
     volatile int *abort_flag = &sh->abort_flag;
-    // Launched as a programmatic dependent: all of the above overlaps the kernel in front; nothing it wrote is read,
-    // and nothing written, before this wait.
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (all of the above overlaps the kernel in front)
+    dependent_start();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -467,8 +463,7 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
 // y = finish(sum of `split` fp32 matrices [M,N], part_rows rows apart, in their order)
 __global__ void __launch_bounds__(256) k_combine(int M, int N, const float *__restrict__ parts, int split, int part_rows, Epilogue e, void *y, long long ldy)
 {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    dependent_start();
     const int groups = N >> 3;
     const long long n = (long long)M * groups, step = (long long)part_rows * N;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
@@ -500,8 +495,7 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
     __shared__ float red[kRows][kDzCols];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, col = blockIdx.x * kDzCols + tx * 8;
     const int r0 = blockIdx.y * slab, r1 = min(M, r0 + slab);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    dependent_start();
     PhiloxKey key = {};
     if (d.rng) key = philox_key(d.rng);
     const uint32_t bound = keep_bound(d.drop);
@@ -555,7 +549,11 @@ k_dz(int M, int N, const __nv_bfloat16 *__restrict__ dy, long long lddy, const _
     }
 }
 
-__global__ void __launch_bounds__(256) k_dbias(const BiasGrad b) { bias_grad(b, blockIdx.x * 256 + threadIdx.x); }
+__global__ void __launch_bounds__(256) k_dbias(const BiasGrad b)
+{
+    dependent_start();
+    bias_grad(b, blockIdx.x * 256 + threadIdx.x);
+}
 
 int dz_slabs(int M, int N)
 {
@@ -676,26 +674,6 @@ bool make_job(DenseJob *j, Matrix a, Matrix b, int M, int N, int K, void *y, lon
     return true;
 }
 
-template <class... P, class... A>
-cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, A... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 // `n` jobs of p, the one with the longer items first
 template <bool kForward>
 rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
@@ -776,11 +754,11 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
 }
 
 template <int kAct>
-void launch_dz(dim3 grid, cudaStream_t st, int M, int N, const void *dy, long long lddy, const void *z, long long ldz, const DropoutParams &d,
-               int slab, __nv_bfloat16 *dz, float *partial)
+cudaError_t launch_dz(dim3 grid, cudaStream_t st, int M, int N, const void *dy, long long lddy, const void *z, long long ldz, const DropoutParams &d,
+                      int slab, __nv_bfloat16 *dz, float *partial)
 {
-    k_dz<kAct><<<grid, kDzThreads, 0, st>>>(M, N, static_cast<const __nv_bfloat16 *>(dy), lddy, static_cast<const __nv_bfloat16 *>(z), ldz, d,
-                                            slab, dz, partial);
+    return launch_dependent(k_dz<kAct>, grid, kDzThreads, 0, 0, st, M, N, static_cast<const __nv_bfloat16 *>(dy), lddy,
+                            static_cast<const __nv_bfloat16 *>(z), ldz, d, slab, dz, partial);
 }
 
 }  // namespace
@@ -826,14 +804,15 @@ rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void
         const dim3 grid((s.N + kDzCols - 1) / kDzCols, slabs);
         __nv_bfloat16 *out = want_dz ? ws.dz : nullptr;
         float *partial = dbias ? ws.partial : nullptr;
+        cudaError_t err;
         switch (s.act) {
-        case RR_ACT_NONE: launch_dz<RR_ACT_NONE>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
-        case RR_ACT_RELU: launch_dz<RR_ACT_RELU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
-        case RR_ACT_GELU: launch_dz<RR_ACT_GELU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
-        case RR_ACT_GELU_TANH: launch_dz<RR_ACT_GELU_TANH>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
-        default: launch_dz<RR_ACT_SILU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
+        case RR_ACT_NONE: err = launch_dz<RR_ACT_NONE>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
+        case RR_ACT_RELU: err = launch_dz<RR_ACT_RELU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
+        case RR_ACT_GELU: err = launch_dz<RR_ACT_GELU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
+        case RR_ACT_GELU_TANH: err = launch_dz<RR_ACT_GELU_TANH>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
+        default: err = launch_dz<RR_ACT_SILU>(grid, st, s.M, s.N, dy, s.lddy, z, s.ldz, d, slab, out, partial); break;
         }
-        if (cudaGetLastError() != cudaSuccess) return RR_ERR_CUDA;
+        if (err != cudaSuccess) return RR_ERR_CUDA;
     }
     BiasGrad bias = {};
     if (dbias) bias = {ws.partial, dbias, s.N, dz_slabs(s.M, s.N), (s.flags & RR_ADD_DW) ? 1 : 0, d.rng ? d.factor : 1.0f};
@@ -856,8 +835,8 @@ rr_status launch_linear_bwd(const rr_linear_shape &s, const void *dy, const void
         dx = nullptr;
     }
     if (!dx && !dw) {
-        if (dbias) k_dbias<<<(s.N + 255) / 256, 256, 0, st>>>(bias);
-        return cudaGetLastError() == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+        if (dbias && launch_dependent(k_dbias, dim3((s.N + 255) / 256), 256, 0, 1, st, bias) != cudaSuccess) return RR_ERR_CUDA;
+        return RR_OK;
     }
     const Plan plan = plan_bwd(s.M, s.N, s.K, dx, dw);
     DenseParams p;
