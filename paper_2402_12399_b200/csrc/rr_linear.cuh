@@ -299,7 +299,7 @@ struct EpilogueWarp {
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] *= e.alpha;
+            for (int j = 0; j < 32; j += 2) tc::unpack2(tc::mul2(tc::pack2(v[j], v[j + 1]), tc::pack2(e.alpha, e.alpha)), v[j], v[j + 1]);
         }
         if (!e.y_f32) {
             if (e.residual) {

@@ -178,17 +178,18 @@ def test_rows_of_infinities_and_nans_stay_in_their_rows():
         assert torch.equal(dx[:, 0], torch.tensor([8.0, 0.0, 8.0, 0.0], device="cuda"))
 
 
-def test_in_place_residual_and_parts_of_the_gradient():
+@pytest.mark.parametrize("M", [5, 333])
+def test_in_place_residual_and_parts_of_the_gradient(M):
     import paper_2402_12399_b200 as rr
     g = torch.Generator("cuda").manual_seed(4)
-    x, w, b = _ints(g, 333, 200), _ints(g, 520, 200), _ints(g, 520)
+    x, w, b = _ints(g, M, 200), _ints(g, 520, 200), _ints(g, 520)
     for dtype in (torch.bfloat16, torch.float32):
-        r = _ints(g, 333, 520).to(dtype)
+        r = _ints(g, M, 520).to(dtype)
         want = rr.linear_fwd(x, w, b, r, act=rr.ACT_SILU)
         same = r.clone()
         assert rr.linear_fwd(x, w, b, same, act=rr.ACT_SILU, out=same) is same and torch.equal(same, want)
-    dy = _ints(g, 333, 520)
-    bufs = [torch.empty(333, 200, device="cuda"), torch.empty(520, 200, device="cuda"), torch.empty(520, device="cuda")]
+    dy = _ints(g, M, 520)
+    bufs = [torch.empty(M, 200, device="cuda"), torch.empty(520, 200, device="cuda"), torch.empty(520, device="cuda")]
     rr.linear_bwd(dy, x, w, dx=bufs[0], dw=bufs[1], dbias=bufs[2])
     for keep in ((0,), (1,), (2,), (0, 2), (1, 2), ()):
         part = [torch.full_like(t, 3.0) if i in keep else None for i, t in enumerate(bufs)]
