@@ -290,8 +290,7 @@ k_dense(const __grid_constant__ DenseParams p)
 // tiles meet in shared memory: each CTA of the cluster adds up its share of the tokens, in the order of the
 // ranks (the result repeats bit for bit), and finishes them.  About 110 KB of shared memory a CTA: two share an SM.
 // 1 x 4096 x 4096: 8.8 us, 3.8 TB/s (256 CTAs; the read alone takes 5.1); 37 x 14336 x 4096: 23.2 us, 5.1 TB/s (0.79 of the measured copy
-// rate).  With more tokens the parts' way through the SM-to-SM network counts: 64 KB a CTA at about 4 TB/s over all SMs
-// (128 x 4096 x 4096: 15.4 us, 4 of them the sums).
+// rate).  With more tokens the parts' way through the SM-to-SM network counts, at about 4 TB/s over all SMs (128 x 4096 x 4096: 13.0 us).
 //   kWmn: the weights are MN-major (dx = dz W: the features are the columns of W, the contraction runs over its rows).
 constexpr int kSlimTokens = 128;   // up to here always
 constexpr int kSlimThreads = 320;  // warp 0: TMA, warp 1: MMA, warps 2-9: TMEM; all of them finish
@@ -729,7 +728,14 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
                       int *status, cudaStream_t st)
 {
     CUtensorMap mW, mX;
-    const int BN = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+    const int f_tiles = (features + 127) / 128;
+    int BN = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+    // Where the tiles are few, narrower ones: the weights are read again, from L2, but the clusters join half as much each and there is room
+    // to split (128 x 4096 x 4096: 13.0 us with 64 tokens a tile, 15.3 with 128; 512 x 1024 x 4096: 11.1 and 13.9).  The shorter the
+    // contraction, the more the join is of the whole, and the narrower (128 x 1024 x 1024: 5.5 us with 32, 5.9 with 64; but 48 x 4096 x
+    // 4096: 11.1 and 10.3; 200 x 256 x 256: 3.7 with 16, 4.3 with 32).
+    const int least = kblocks_of(K) <= 4 ? 16 : kblocks_of(K) <= 32 ? 32 : 64;
+    while (BN > least && (long long)f_tiles * ((tokens + BN / 2 - 1) / (BN / 2)) <= 74) BN /= 2;
     if (!(kWmn ? map_2d(&mW, w.p, K, features, w.pitch, false, 64, 64) : map_2d(&mW, w.p, features, K, w.pitch, false, 64, 128))) return RR_ERR_CUDA;
     if (!map_2d(&mX, x.p, tokens, K, x.pitch, false, 64, BN)) return RR_ERR_CUDA;
     SlimParams p;
@@ -743,7 +749,6 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
     p.z = static_cast<__nv_bfloat16 *>(z);
     p.ldz = ldz;
     p.status = status;
-    const int f_tiles = (features + 127) / 128;
     // two CTAs on every SM, if each is left four k-blocks (1 x 4096 x 4096: 9.5 us with 256 CTAs, 10.0 with 128; 64 x 4096 x 1024: 6.9 us with
     // 128 CTAs of four k-blocks, 8.1 with 256 of two)
     p.split = 1;
