@@ -174,3 +174,78 @@ def test_one_workspace_for_every_call_in_turn():
     b.check()
     for i, (x, y) in enumerate(zip(want, b.outputs())):
         assert torch.allclose(x.double(), y.double(), rtol=2e-2, atol=2e-2 * float(y.double().square().mean().sqrt()) + 1e-12), i
+
+
+def test_calls_that_follow_at_once_see_each_other():
+    """Every kernel may be made ready while the one in front still runs: chains whose calls read what the call in front wrote and overwrite
+    what it read, with and without a synchronisation between the calls."""
+    import paper_2402_12399_b200 as rr
+    g = torch.Generator("cuda").manual_seed(1)
+    bf = dict(device="cuda", dtype=torch.bfloat16)
+    for M, N in ((700, 512), (5, 4096), (64, 256)):
+        w = (torch.randn(N, N, generator=g, device="cuda") * N ** -0.5).bfloat16()
+        b = torch.randn(N, generator=g, device="cuda").bfloat16()
+        start = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+        rng = torch.tensor([3, 0], device="cuda")
+        fb, bb = rr.linear_workspace_bytes(M, N, N)
+        ws, wb = rr.alloc_workspace(fb), rr.alloc_workspace(bb)
+
+        def chain(wait):
+            x, y, z, dw, db = start.clone(), torch.empty(M, N, **bf), torch.empty(M, N, **bf), torch.zeros(N, N, device="cuda"), torch.zeros(N, device="cuda")
+            a = torch.empty(M, N, device="cuda")
+            for i in range(12):
+                for call in (lambda: rr.linear_fwd(x, w, b, x, act=rr.ACT_SILU, p=0.1, rng=rng, out=y, z=z, workspace=ws),
+                             lambda: rr.dropout_fwd(y, 0.2, rng, out=x),
+                             lambda: rr.dropout_fwd(x, 0.0, None, out=a, out_dtype=torch.float32),
+                             lambda: rr.linear_bwd(x, z, w, z, act=rr.ACT_SILU, p=0.1, rng=rng, dx=y, dw=dw, dbias=db, add_dw=True, workspace=wb),
+                             lambda: rr.dropout_fwd(y, 0.3, rng, residual=x, out=x)):
+                    call()
+                    if wait:
+                        torch.cuda.synchronize()
+                x.clamp_(-4, 4)
+            torch.cuda.synchronize()
+            rr.check(ws), rr.check(wb)
+            return x, y, z, a, dw, db
+        for p, q in zip(chain(True), chain(False)):
+            assert torch.equal(p, q)
+
+
+def test_captured_with_branches():
+    """A graph whose branches fork and join between the calls gives what the eager calls give."""
+    import paper_2402_12399_b200 as rr
+    g = torch.Generator("cuda").manual_seed(2)
+    bf = dict(device="cuda", dtype=torch.bfloat16)
+    x, w = torch.randn(300, 256, generator=g, device="cuda").bfloat16(), torch.randn(512, 256, generator=g, device="cuda").bfloat16()
+    a, rng = torch.randn(256, 8, generator=g, device="cuda"), torch.tensor([1, 2], device="cuda")
+    table = torch.topk(a, 3, 1).indices.int().contiguous()
+    ws, ws2, wb = rr.alloc_workspace(256), rr.alloc_workspace(256), rr.alloc_workspace(rr.balance_workspace_bytes(256, 8, 4))
+    y = [torch.empty(300, 512, **bf) for _ in range(3)] + [torch.empty(3, 512, **bf)]
+    side = torch.cuda.Stream()
+
+    def step():
+        main = torch.cuda.current_stream()
+        rr.linear_fwd(x, w, out=y[0], workspace=ws)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            rr.linear_fwd(x, w, act=rr.ACT_GELU, out=y[1], workspace=ws2)
+            out = rr.balance_fwd(a, table, 2, 0.1, 0.1, segments=4, workspace=wb)
+        rr.dropout_fwd(y[0], 0.5, rng, out=y[2])
+        main.wait_stream(side)
+        rr.dropout_fwd(y[1], 0.5, rng, residual=y[2], out=y[2])
+        rr.linear_fwd(x[:3], w, out=y[3], workspace=ws)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            d = rr.balance_bwd(a, out[1], out[2], 2, 0.1, 0.1)
+        main.wait_stream(side)
+        return [*y, *out, d]
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for t in y:
+        t.zero_()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
