@@ -109,6 +109,7 @@ struct BalShape {
     int S;         // segments
     int cps;       // blocks per segment (forward)
     int slab;      // tokens of a block (forward)
+    int one;       // the first forward kernel finishes the segments itself
 };
 
 struct BalScratch {
@@ -122,11 +123,164 @@ struct BalScratch {
     int *sn;         // [S]
 };
 
-// Forward, first kernel: block (s, c) adds up the tokens of its slab of segment s.
-template <int GS, int CPL, bool VEC>
+// sums over the warp, the same in every lane, and over the block (any number of warps up to 32), in a fixed order
+template <class T>
+__device__ __forceinline__ T warp_sum(T v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <class... T>
+__device__ __forceinline__ void block_sums(uint32_t (*buf)[32], T &...v)
+{
+    const int lane = threadIdx.x & 31, warps = (int)(blockDim.x >> 5);
+    int k = 0;
+    auto store = [&](auto &x) {
+        x = warp_sum(x);
+        if (lane == 0) buf[k][threadIdx.x >> 5] = *reinterpret_cast<const uint32_t *>(&x);
+        ++k;
+    };
+    __syncthreads();  // (buf may still be read from the call before)
+    (store(v), ...);
+    __syncthreads();
+    k = 0;
+    auto load = [&](auto &x) {
+        const uint32_t u = lane < warps ? buf[k][lane] : 0u;  // (the bits of a zero of either type)
+        x = warp_sum(*reinterpret_cast<const typename std::remove_reference<decltype(x)>::type *>(&u));
+        ++k;
+    };
+    (load(v), ...);
+}
+
+// What the forward pass writes.
+struct BalOut {
+    float alpha, beta;
+    float *loss, *P;
+    int *count, *n_live;
+};
+
+// A sum of another block: past L1 when that block is of the same kernel (else its 32 warps share what the first of them fetched).
+template <bool kFresh, class T>
+__device__ __forceinline__ T other_block(const T *p)
+{
+    return kFresh ? __ldcg(p) : *p;
+}
+
+// Adds up the blocks of segment s; the caller that finishes last of the S adds up the segments.  NT threads.  Thread (r, j) takes the rows
+// r, r + R, ... of column j (of the four columns from j on when VEC); the R sums of a column are then added in two steps.
+template <bool VEC, int NT, bool kFresh>
+__device__ __forceinline__ void finish_segment(const BalShape &b, const BalScratch &w, const BalOut &o, int s)
+{
+    constexpr int V = VEC ? 4 : 1, kParts = NT / kMaxE;
+    __shared__ float sp[NT * V];
+    __shared__ int sc[NT * V];
+    __shared__ float tp[kParts][kMaxE];
+    __shared__ int tc[kParts][kMaxE];
+    __shared__ uint32_t buf[4][32];
+    __shared__ int last;
+    const int E = b.E, tid = threadIdx.x, lane = tid & 31;
+    int epad = V;
+    while (epad < E) epad <<= 1;
+    const int cols = epad / V, R = NT / cols, r = tid / cols, j = (tid % cols) * V;
+    const size_t row0 = (size_t)s * b.cps;
+    float sum[V] = {}, lse2 = 0.f;
+    int cnt[V] = {}, n = 0;
+    for (int c = lane; c < b.cps; c += 32) { lse2 += other_block<kFresh>(w.plse + row0 + c); n += other_block<kFresh>(w.pn + row0 + c); }  // (every warp for itself: no barrier)
+    if (j < E) {
+#pragma unroll 4
+        for (int c = r; c < b.cps; c += R) {
+            if constexpr (VEC) {
+                const float4 x = other_block<kFresh>(reinterpret_cast<const float4 *>(w.partial + (row0 + c) * E + j));
+                const int4 y = other_block<kFresh>(reinterpret_cast<const int4 *>(w.pcount + (row0 + c) * E + j));
+                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+                cnt[0] += y.x; cnt[1] += y.y; cnt[2] += y.z; cnt[3] += y.w;
+            } else {
+                sum[0] += other_block<kFresh>(w.partial + (row0 + c) * E + j);
+                cnt[0] += other_block<kFresh>(w.pcount + (row0 + c) * E + j);
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        sp[r * epad + j + v] = sum[v];
+        sc[r * epad + j + v] = cnt[v];
+    }
+    n = warp_sum(n);
+    lse2 = warp_sum(lse2);
+    __syncthreads();
+    {
+        const int c = tid % kMaxE, part = tid / kMaxE, rows = min(R, b.cps);  // (the other rows are zero)
+        float t = 0.f;
+        int m = 0;
+        if (c < E)
+            for (int q = part; q < rows; q += kParts) { t += sp[q * epad + c]; m += sc[q * epad + c]; }
+        tp[part][c] = t;
+        tc[part][c] = m;
+    }
+    __syncthreads();
+    float prod = 0.f;
+    if (tid < E) {
+        float tot = 0.f;
+        int m = 0;
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) { tot += tp[q][tid]; m += tc[q][tid]; }
+        const float p = n > 0 ? tot / (float)n : 0.f;
+        o.count[(size_t)s * E + tid] = m;
+        o.P[(size_t)s * E + tid] = p;
+        if (n > 0) prod = (float)m / ((float)b.k * (float)n) * p;
+    }
+    block_sums(buf, prod);
+    float dots = 0.f, z = 0.f;
+    int segs = 0, live = 0;
+    if (b.S == 1) {
+        if (tid) return;
+        o.n_live[0] = n;
+        dots = prod;
+        z = lse2;
+        segs = n > 0 ? 1 : 0;
+        live = n;
+    } else {
+        if (tid == 0) {
+            o.n_live[s] = n;
+            w.dot[s] = prod;
+            w.slse[s] = lse2;
+            w.sn[s] = n;
+            __threadfence();
+            last = atomicAdd(&w.hdr->sync[8], 1) == b.S - 1;
+        }
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        for (int q = tid; q < b.S; q += NT) {
+            dots += __ldcg(w.dot + q);
+            z += __ldcg(w.slse + q);
+            const int m = __ldcg(w.sn + q);
+            live += m;
+            segs += m > 0 ? 1 : 0;
+        }
+        block_sums(buf, dots, z, segs, live);
+        if (tid) return;
+        w.hdr->sync[8] = 0;
+    }
+    o.loss[0] = segs > 0 ? o.alpha * (float)E / (float)segs * dots : 0.f;
+    o.loss[1] = live > 0 && o.beta != 0.f ? o.beta / (float)live * z : 0.f;  // (the sum may be infinite)
+}
+
+// Forward, second kernel: block s finishes segment s.
+template <bool VEC>
+__global__ void __launch_bounds__(kBalFinal) k_balance_final(const BalShape b, const BalScratch w, const BalOut o)
+{
+    dependent_start();  // (the first kernel has completed and its sums are visible)
+    finish_segment<VEC, kBalFinal, false>(b, w, o, blockIdx.x);
+}
+
+// Forward, first kernel: block (s, c) adds up the tokens of its slab of segment s.  With kOne it is the only kernel: the block of a
+// segment that ends last finishes it.
+template <int GS, int CPL, bool VEC, bool kOne>
 __global__ void __launch_bounds__(kBalThreads)
 k_balance_partial(const BalShape b, const float *__restrict__ logits, const int32_t *__restrict__ topk,
-                  const uint8_t *__restrict__ live, const BalScratch w)
+                  const uint8_t *__restrict__ live, const BalScratch w, const BalOut o)
 {
     constexpr int TPW = 32 / GS;
     __shared__ float red[kBalWarps][kMaxE];
@@ -204,139 +358,23 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
         w.plse[blockIdx.x] = sum;
         w.pn[blockIdx.x] = m;
     }
-}
-
-// sums over the warp, the same in every lane, and over the block (any number of warps up to 32), in a fixed order
-template <class T>
-__device__ __forceinline__ T warp_sum(T v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-template <class... T>
-__device__ __forceinline__ void block_sums(uint32_t (*buf)[32], T &...v)
-{
-    const int lane = threadIdx.x & 31, warps = (int)(blockDim.x >> 5);
-    int k = 0;
-    auto store = [&](auto &x) {
-        x = warp_sum(x);
-        if (lane == 0) buf[k][threadIdx.x >> 5] = *reinterpret_cast<const uint32_t *>(&x);
-        ++k;
-    };
-    __syncthreads();  // (buf may still be read from the call before)
-    (store(v), ...);
-    __syncthreads();
-    k = 0;
-    auto load = [&](auto &x) {
-        const uint32_t u = lane < warps ? buf[k][lane] : 0u;  // (the bits of a zero of either type)
-        x = warp_sum(*reinterpret_cast<const typename std::remove_reference<decltype(x)>::type *>(&u));
-        ++k;
-    };
-    (load(v), ...);
-}
-
-// Forward, second kernel: block s adds up the blocks of segment s; the block that finishes last adds up the segments.
-// Thread (r, j) takes the rows r, r + R, ... of column j (of the four columns from j on when VEC); the R sums of a column are then
-// added in two steps.
-template <bool VEC>
-__global__ void __launch_bounds__(kBalFinal)
-k_balance_final(const BalShape b, float alpha, float beta, const BalScratch w, float *loss, int *count, int *n_live, float *P)
-{
-    constexpr int V = VEC ? 4 : 1, kParts = kBalFinal / kMaxE;
-    __shared__ float sp[kBalFinal * V];
-    __shared__ int sc[kBalFinal * V];
-    __shared__ float tp[kParts][kMaxE];
-    __shared__ int tc[kParts][kMaxE];
-    __shared__ uint32_t buf[4][32];
-    __shared__ int last;
-    const int s = blockIdx.x, E = b.E, tid = threadIdx.x, lane = tid & 31;
-    int epad = V;
-    while (epad < E) epad <<= 1;
-    const int cols = epad / V, R = kBalFinal / cols, r = tid / cols, j = (tid % cols) * V;
-    const size_t row0 = (size_t)s * b.cps;
-    float sum[V] = {}, lse2 = 0.f;
-    int cnt[V] = {}, n = 0;
-    dependent_start();  // (the first kernel has completed and its sums are visible)
-    for (int c = lane; c < b.cps; c += 32) { lse2 += w.plse[row0 + c]; n += w.pn[row0 + c]; }  // (every warp for itself: no barrier)
-    if (j < E) {
-#pragma unroll 4
-        for (int c = r; c < b.cps; c += R) {
-            if constexpr (VEC) {
-                const float4 x = *reinterpret_cast<const float4 *>(w.partial + (row0 + c) * E + j);
-                const int4 y = *reinterpret_cast<const int4 *>(w.pcount + (row0 + c) * E + j);
-                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-                cnt[0] += y.x; cnt[1] += y.y; cnt[2] += y.z; cnt[3] += y.w;
-            } else {
-                sum[0] += w.partial[(row0 + c) * E + j];
-                cnt[0] += w.pcount[(row0 + c) * E + j];
+    if constexpr (kOne) {
+        if (b.cps > 1) {
+            __shared__ int last;
+            __threadfence();  // (every thread's sums are visible before the block is counted)
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                last = atomicAdd(&w.hdr->segs[s], 1) == b.cps - 1;
+                if (last) w.hdr->segs[s] = 0;
             }
-        }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        sp[r * epad + j + v] = sum[v];
-        sc[r * epad + j + v] = cnt[v];
-    }
-    n = warp_sum(n);
-    lse2 = warp_sum(lse2);
-    __syncthreads();
-    {
-        const int c = tid % kMaxE, part = tid / kMaxE, rows = min(R, b.cps);  // (the other rows are zero)
-        float t = 0.f;
-        int m = 0;
-        if (c < E)
-            for (int q = part; q < rows; q += kParts) { t += sp[q * epad + c]; m += sc[q * epad + c]; }
-        tp[part][c] = t;
-        tc[part][c] = m;
-    }
-    __syncthreads();
-    float prod = 0.f;
-    if (tid < E) {
-        float tot = 0.f;
-        int m = 0;
-#pragma unroll
-        for (int q = 0; q < kParts; ++q) { tot += tp[q][tid]; m += tc[q][tid]; }
-        const float p = n > 0 ? tot / (float)n : 0.f;
-        count[(size_t)s * E + tid] = m;
-        P[(size_t)s * E + tid] = p;
-        if (n > 0) prod = (float)m / ((float)b.k * (float)n) * p;
-    }
-    block_sums(buf, prod);
-    float dots = 0.f, z = 0.f;
-    int segs = 0, live = 0;
-    if (b.S == 1) {
-        if (tid) return;
-        n_live[0] = n;
-        dots = prod;
-        z = lse2;
-        segs = n > 0 ? 1 : 0;
-        live = n;
-    } else {
-        if (tid == 0) {
-            n_live[s] = n;
-            w.dot[s] = prod;
-            w.slse[s] = lse2;
-            w.sn[s] = n;
+            __syncthreads();
+            if (!last) return;
             __threadfence();
-            last = atomicAdd(&w.hdr->sync[8], 1) == b.S - 1;
+        } else {
+            __syncthreads();  // (its own sums)
         }
-        __syncthreads();
-        if (!last) return;
-        __threadfence();
-        for (int q = tid; q < b.S; q += kBalFinal) {
-            dots += __ldcg(w.dot + q);
-            z += __ldcg(w.slse + q);
-            const int m = __ldcg(w.sn + q);
-            live += m;
-            segs += m > 0 ? 1 : 0;
-        }
-        block_sums(buf, dots, z, segs, live);
-        if (tid) return;
-        w.hdr->sync[8] = 0;
+        finish_segment<VEC, kBalThreads, true>(b, w, o, s);
     }
-    loss[0] = segs > 0 ? alpha * (float)E / (float)segs * dots : 0.f;
-    loss[1] = live > 0 && beta != 0.f ? beta / (float)live * z : 0.f;  // (the sum may be infinite)
 }
 
 // Backward: items of up to `slab` tokens of one segment, dealt to the blocks in turn.
@@ -425,6 +463,10 @@ BalShape balance_shape(int T, int E, int k, int stride, int S, int want, int pas
     if (b.slab < 1) b.slab = 1;
     b.cps = (int)((b.L + b.slab - 1) / b.slab);
     if (b.cps < 1) b.cps = 1;
+    // One launch where the header has a counter for every segment and a block adds up a segment's parts in about the time that the second
+    // kernel takes to start: the device takes as long (four segments of 16 tokens: 6.7 us, 7.5 with two launches; 32 of 2048: 10.8 and
+    // 10.4), the caller 2 us less.  A segment in hundreds of parts keeps the second kernel, whose blocks are twice as large.
+    b.one = S <= 32 && b.cps <= 32;
     return b;
 }
 BalShape forward_shape(int T, int E, int k, int stride, int S)
@@ -452,9 +494,10 @@ size_t balance_layout(void *ws, int T, int E, int S, BalScratch *out)
 
 template <int GS, int CPL, bool VEC>
 rr_status run_fwd(const BalShape &b, const float *logits, const int32_t *topk, const uint8_t *live, const BalScratch &w,
-                  cudaStream_t st)
+                  const BalOut &o, cudaStream_t st)
 {
-    return launch_dependent(k_balance_partial<GS, CPL, VEC>, dim3((unsigned)(b.S * b.cps)), kBalThreads, 0, 1, st, b, logits, topk, live, w) == cudaSuccess
+    return launch_dependent(b.one ? k_balance_partial<GS, CPL, VEC, true> : k_balance_partial<GS, CPL, VEC, false>, dim3((unsigned)(b.S * b.cps)), kBalThreads, 0, 1, st, b, logits, topk, live, w,
+                            o) == cudaSuccess
                ? RR_OK : RR_ERR_CUDA;
 }
 
@@ -481,10 +524,10 @@ rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float
     BalScratch w;
     balance_layout(workspace, T, E, S, &w);
     rr_status rc = RR_OK;
-    RR_ROWS_DISPATCH(rc = run_fwd, E, b, logits, topk, live, w, st);
-    if (rc) return rc;
-    const cudaError_t err = launch_dependent(E % 4 == 0 ? k_balance_final<true> : k_balance_final<false>, dim3(S), kBalFinal, 0, 1, st, b, alpha, beta, w,
-                                             loss, count, n_live, P);
+    const BalOut o = {alpha, beta, loss, P, count, n_live};
+    RR_ROWS_DISPATCH(rc = run_fwd, E, b, logits, topk, live, w, o, st);
+    if (rc || b.one) return rc;
+    const cudaError_t err = launch_dependent(E % 4 == 0 ? k_balance_final<true> : k_balance_final<false>, dim3(S), kBalFinal, 0, 1, st, b, w, o);
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 

@@ -23,7 +23,8 @@ struct Header {
     // [1] set when a block gave up waiting, [2] blocks that have left.  The last block to leave puts
     // them back to zero, so a finished call leaves them as it found them.
     int sync[16];
-    int pad1[32];
+    // blocks of each segment that have finished (balance loss; its one kernel puts them back to zero, as it does sync[8])
+    int segs[32];
 };
 static_assert(sizeof(Header) == kHeaderBytes, "the header fills the first 256 bytes of a workspace");
 
