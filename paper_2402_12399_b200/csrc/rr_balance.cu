@@ -10,6 +10,8 @@
 // launch latency below.  The row of a dead token is read and selected away (its load does not wait for the
 // mask), so what it holds -- NaN, infinities -- reaches no sum.  All sums are fp32 in a fixed order (counts are
 // integers), so the results repeat bit for bit.
+// 65536 x 64, top-2, 32 padded segments: forward 10.9 us, gradient 8.6 (latency: a few dependent loads, the joining of the parts); 2^20
+// tokens: 68 us, 4.2 TB/s read (loads in flight: registers hold two tokens a lane group) and 97 us, 5.5 TB/s.
 #include <type_traits>
 
 #include "rr_ffn.cuh"
