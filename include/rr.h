@@ -6,7 +6,8 @@
  *  - "dev" pointers are CUDA device pointers of the current device, "host"
  *    pointers are ordinary host memory.  All dev pointers must be 16-byte
  *    aligned; hidden / weight / dout tensors must be 128-byte aligned (they are
- *    read through TMA).  Everything is row-major and densely packed.
+ *    read through TMA).  Everything is row-major and densely packed (rr_linear_* ask for 16 bytes
+ *    and take pitches).
  *  - The caller owns and allocates every buffer, including the workspace.  The
  *    library allocates no device memory and keeps no state between calls other
  *    than lazily resolved driver entry points.
