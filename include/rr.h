@@ -410,7 +410,7 @@ typedef struct rr_linear_shape {
     uint32_t flags;            /* RR_ADD_DX | RR_ADD_DW (backward)                                */
     float p;                   /* dropout probability                                             */
     int64_t ldx, ldr, ldy, ldz; /* pitches of x, residual, y, z: at least their widths, rows a    */
-    int64_t lddy, lddx;        /* multiple of 16 bytes apart; of dy and dx                        */
+    int64_t lddy, lddx;        /* multiple of 16 bytes (and less than 2^40) apart; of dy and dx   */
 } rr_linear_shape;
 
 /*

@@ -431,11 +431,13 @@ rr_status check_linear_sizes(int M, int N, int K)
     return M < 0 || N < 8 || K < 8 || N % 8 || K % 8 || M > kMost || N > kMost || K > kMost ? RR_ERR_INVALID_ARG : RR_OK;
 }
 
-// a pitch of `width` elements of `size` bytes: 0 becomes the width; rows stay 16-byte aligned and addressable by TMA
-bool fill_pitch(int64_t *ld, int width, int size)
+// a pitch of `width` elements of `size` bytes: 0 becomes the width; rows stay 16-byte aligned, addressable by TMA (below 2^40 bytes
+// apart) and, all `rows` of them, inside 62 bits.  Compared in elements: in bytes a pitch may wrap to something small.
+bool fill_pitch(int64_t *ld, int width, int size, int rows)
 {
     if (*ld == 0) *ld = width;
-    return *ld >= width && *ld % (16 / size) == 0 && *ld * size < (1ll << 40);
+    if (*ld < width || *ld % (16 / size) || *ld >= (1ll << 40) / size) return false;
+    return *ld <= (1ll << 62) / size / (rows > 0 ? rows : 1);
 }
 
 rr_status check_linear(const rr_linear_shape *in, rr_linear_shape *s)
@@ -448,8 +450,9 @@ rr_status check_linear(const rr_linear_shape *in, rr_linear_shape *s)
         return RR_ERR_INVALID_ARG;
     if (s->flags & ~(RR_ADD_DX | RR_ADD_DW)) return RR_ERR_INVALID_ARG;
     const int ys = s->y_dtype == RR_F32 ? 4 : 2, xs = s->dx_dtype == RR_F32 ? 4 : 2;
-    if (!fill_pitch(&s->ldx, s->K, 2) || !fill_pitch(&s->ldr, s->N, ys) || !fill_pitch(&s->ldy, s->N, ys) || !fill_pitch(&s->ldz, s->N, 2) ||
-        !fill_pitch(&s->lddy, s->N, 2) || !fill_pitch(&s->lddx, s->K, xs))
+    const int M = s->M, N = s->N, K = s->K;
+    if (!fill_pitch(&s->ldx, K, 2, M) || !fill_pitch(&s->ldr, N, ys, M) || !fill_pitch(&s->ldy, N, ys, M) || !fill_pitch(&s->ldz, N, 2, M) ||
+        !fill_pitch(&s->lddy, N, 2, M) || !fill_pitch(&s->lddx, K, xs, M))
         return RR_ERR_INVALID_ARG;
     return RR_OK;
 }
