@@ -382,7 +382,7 @@ rr_status rr_aux_loss_bwd(int T, int E, const float *logits, const float *f, flo
  *                 residual is dy itself.
  *   n         elements, >= 0 (n == 0 does nothing)
  *   x, dy     dev, element type x_dtype / dy_dtype;  residual, y, dx   dev, element type y_dtype / dx_dtype
- *   y may be the same buffer as residual, and as x if the types are equal; any other overlap is not allowed.
+ *   y may be the same buffer as residual, and as x if the types are equal; any other overlap is refused.
  * fp32 arithmetic, one rounding to the type of the result.  One kernel, no workspace.
  */
 rr_status rr_dropout_fwd(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p,
@@ -417,8 +417,8 @@ typedef struct rr_linear_shape {
  * rr_linear_fwd -- matrix product with everything behind it in its epilogue:
  *     z = x W^T + bias,     y = residual + D(act(z)),     D = dropout (above) on the index row*N + column
  *   x [M,K], W [N,K], bias [N] (or NULL)   dev bf16, 16-byte aligned, read only
- *   residual [M,N] (or NULL), y [M,N]      dev, type y_dtype; y may be the same buffer as residual (same pitch),
- *                                          no other overlap
+ *   residual [M,N] (or NULL), y [M,N]      dev, type y_dtype; y may be the same buffer as residual (same pitch);
+ *                                          y and z overlap nothing else
  *   z [M,N] dev bf16, or NULL: the pre-activations for rr_linear_bwd, rounded to bf16 (needed unless act is RR_ACT_NONE)
  *   workspace dev, >= fwd_bytes, 256-byte aligned: the status word read by rr_check and nothing else
  * Products are bf16 x bf16 on the tensor cores with fp32 accumulation (their adder truncates: the sum of n products is off by
@@ -434,12 +434,13 @@ typedef struct rr_linear_shape {
  *   when dx is NULL
  *   dx [M,K] type dx_dtype, dW [N,K] (dense) type dw_dtype, dbias [N] fp32: each may be NULL when not wanted
  *   workspace dev, >= bwd_bytes, 256-byte aligned
- *   no output overlaps an input or another output
+ *   no output overlaps an input that is read or another output
  * dz is rounded to bf16 between the two steps (without an activation that loses nothing: the dropout factor is applied behind
  * the products); dbias is summed from the unrounded values in a fixed order.  M == 0 sets dW and dbias to zero, or leaves them
  * under RR_ADD_DW.
  * Both return RR_ERR_INVALID_ARG for a shape outside the limits, a pitch below the width, a pointer that is missing or not 16-byte
- * aligned.  Calls that share a workspace must not overlap on the GPU.
+ * aligned, and for such an overlap (columns of one wider buffer do not overlap; two views of one buffer whose rows lie apart by different
+ * pitches are not looked into).  Calls that share a workspace must not overlap on the GPU.
  */
 rr_status rr_linear_workspace_bytes(int M, int N, int K, size_t *fwd_bytes, size_t *bwd_bytes);
 rr_status rr_linear_fwd(const rr_linear_shape *s /* host */, const void *x, const void *W, const void *bias,

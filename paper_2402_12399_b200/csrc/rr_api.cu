@@ -387,6 +387,32 @@ namespace {
 
 bool is_dtype(int t) { return t == RR_BF16 || t == RR_F32; }
 
+// `rows` rows of `width` bytes, `pitch` bytes apart (pitches: fill_pitch, so no sum below leaves 64 bits)
+struct Region {
+    const void *p;
+    long long rows, width, pitch;
+    long long at() const { return (long long)(uintptr_t)p; }
+    long long end() const { return at() + (rows - 1) * pitch + width; }
+    bool whole() const { return rows == 1 || width == pitch; }  // no gaps
+};
+// Do two matrices share a byte?  Columns of one wider buffer do not, however their rows interleave.  Not decided, and taken for apart:
+// interleaved rows with two different pitches.
+bool overlap(const Region &a, const Region &b)
+{
+    if (!a.p || !b.p || a.end() <= b.at() || b.end() <= a.at()) return false;
+    if (a.whole() && b.whole()) return true;
+    if (b.whole()) return overlap(b, a);
+    if (a.whole()) {  // the first row of b that ends behind the start of a, if there is one, starts in front of its end
+        const long long behind = a.at() - b.at() - b.width, row = behind < 0 ? 0 : behind / b.pitch + 1;
+        return row < b.rows && b.at() + row * b.pitch < a.end();
+    }
+    if (a.pitch != b.pitch) return false;
+    // row j of b starts `off` bytes into row j + shift of a, the gap behind it included, and may reach into row j + shift + 1
+    const long long d = b.at() - a.at(), shift = d >= 0 ? d / a.pitch : -((-d + a.pitch - 1) / a.pitch), off = d - shift * a.pitch;
+    auto meet = [&](long long s) { return s < a.rows && s > -b.rows; };
+    return (off < a.width && meet(shift)) || (off + b.width > a.pitch && meet(shift + 1));
+}
+
 // probability and generator state
 bool check_dropout(float p, const void *rng)
 {
@@ -398,10 +424,13 @@ bool check_dropout(float p, const void *rng)
 rr_status check_dropout_call(long long n, int x_dtype, int y_dtype, const void *x, const void *residual, float p, const void *rng,
                              const void *y)
 {
-    if (n < 0 || !is_dtype(x_dtype) || !is_dtype(y_dtype) || !check_dropout(p, rng)) return RR_ERR_INVALID_ARG;
+    if (n < 0 || n > (1ll << 60) || !is_dtype(x_dtype) || !is_dtype(y_dtype) || !check_dropout(p, rng)) return RR_ERR_INVALID_ARG;
     if (n == 0) return RR_OK;
     if (!x || !y || !aligned(x, 16) || !aligned(y, 16) || !aligned(residual, 16)) return RR_ERR_INVALID_ARG;
     if (x == y && x_dtype != y_dtype) return RR_ERR_INVALID_ARG;
+    const long long xb = n * (x_dtype == RR_F32 ? 4 : 2), yb = n * (y_dtype == RR_F32 ? 4 : 2);
+    const Region out = {y, 1, yb, yb};
+    if ((x != y && overlap({x, 1, xb, xb}, out)) || (residual != y && overlap({residual, 1, yb, yb}, out))) return RR_ERR_INVALID_ARG;
     return RR_OK;
 }
 
@@ -439,6 +468,8 @@ bool fill_pitch(int64_t *ld, int width, int size, int rows)
     if (*ld < width || *ld % (16 / size) || *ld >= (1ll << 40) / size) return false;
     return *ld <= (1ll << 62) / size / (rows > 0 ? rows : 1);
 }
+
+Region matrix(const void *p, long long rows, long long cols, long long ld, long long size) { return {p, rows, cols * size, ld * size}; }
 
 rr_status check_linear(const rr_linear_shape *in, rr_linear_shape *s)
 {
@@ -481,6 +512,12 @@ rr_status rr_linear_fwd(const rr_linear_shape *shape, const void *x, const void 
         !aligned(workspace, 256))
         return RR_ERR_INVALID_ARG;
     if (residual == y && s.ldr != s.ldy) return RR_ERR_INVALID_ARG;
+    const long long ys = s.y_dtype == RR_F32 ? 4 : 2;
+    const Region rx = matrix(x, s.M, s.K, s.ldx, 2), rw = matrix(W, s.N, s.K, s.K, 2), rb = matrix(bias, 1, s.N, s.N, 2),
+                 rres = matrix(residual, s.M, s.N, s.ldr, ys), ry = matrix(y, s.M, s.N, s.ldy, ys), rz = matrix(z, s.M, s.N, s.ldz, 2);
+    if (overlap(ry, rx) || overlap(ry, rw) || overlap(ry, rb) || (residual != y && overlap(ry, rres)) || overlap(rz, rx) || overlap(rz, rw) ||
+        overlap(rz, rb) || overlap(rz, rres) || overlap(rz, ry))
+        return RR_ERR_INVALID_ARG;
     if (rr::linear_fwd_workspace() > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
     return rr::launch_linear_fwd(s, x, W, bias, residual, rng, y, z, workspace, static_cast<cudaStream_t>(stream));
 }
@@ -503,6 +540,15 @@ rr_status rr_linear_bwd(const rr_linear_shape *shape, const void *dy, const void
     }
     if (!dy || !workspace || (dW && !x) || (dx && !W) || (s.act != RR_ACT_NONE && !z)) return RR_ERR_INVALID_ARG;
     if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(W, 16) || !aligned(z, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    // (what a call does not read may lie anywhere)
+    const Region in[4] = {matrix(dy, s.M, s.N, s.lddy, 2), matrix(dW ? x : nullptr, s.M, s.K, s.ldx, 2), matrix(dx ? W : nullptr, s.N, s.K, s.K, 2),
+                          matrix(s.act != RR_ACT_NONE ? z : nullptr, s.M, s.N, s.ldz, 2)};
+    const Region out[3] = {matrix(dx, s.M, s.K, s.lddx, s.dx_dtype == RR_F32 ? 4 : 2), matrix(dW, s.N, s.K, s.K, s.dw_dtype == RR_F32 ? 4 : 2),
+                           matrix(dbias, 1, s.N, s.N, 4)};
+    for (const Region &o : out)
+        for (const Region &i : in)
+            if (overlap(o, i)) return RR_ERR_INVALID_ARG;
+    if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return RR_ERR_INVALID_ARG;
     if (rr::linear_bwd_workspace(s.M, s.N, s.K) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
     return rr::launch_linear_bwd(s, dy, x, W, z, rng, dx, dW, dbias, workspace, st);
 }
