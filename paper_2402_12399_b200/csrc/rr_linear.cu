@@ -92,6 +92,7 @@ struct DenseParams {
     int head;      // rounds of the second job's items that only pairs with fewer items of the first take part in
     BiasGrad bias; // (backward)
     int *status;
+    unsigned long long tfull_limit_ns;  // of the epilogue's waits for accumulators
 };
 
 // The it-th item of this pair (job, index), index -1: no more.  The first job's items are dealt out in rounds; `more` pairs got
@@ -250,7 +251,7 @@ k_dense(const __grid_constant__ DenseParams p)
             if (mine) ew.template fetch<kForward>(j.e, row0 + lane, col00 + eg * 32, j.M, j.N, lane);
             // Every warp waits for itself, asleep: a dozen warps that poll take issue slots from the producers and the MMA issuer (one tile a
             // pair at K = 4096: 39 us instead of 34), and a barrier in front of the tile holds the early ones back.
-            if (!warp_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status)) break;
+            if (!warp_wait_brisk(&sh->tfull[buf], (it >> 1) & 1u, abort_flag, p.status, p.tfull_limit_ns)) break;
             fence_after_sync();
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * TN;
             auto release = [&]() {  // (both CTAs' warps free the accumulator at the leader)
@@ -317,6 +318,7 @@ struct SlimParams {
     __nv_bfloat16 *z;
     long long ldz;
     int *status;
+    unsigned long long done_limit_ns;  // of the wait for the partial tile
 };
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr)
@@ -394,7 +396,7 @@ k_slim(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtenso
             }
             if (ok) mma_commit_one(&sh->done);
         }
-    } else if (warp_wait_brisk(&sh->done, 0, abort_flag, p.status)) {
+    } else if (warp_wait_brisk(&sh->done, 0, abort_flag, p.status, p.done_limit_ns)) {
         // every load has landed and every MMA has read its operands: the ring's memory takes the partial tile,
         // [token][128 features]
         fence_after_sync();
@@ -676,12 +678,16 @@ bool make_job(DenseJob *j, Matrix a, Matrix b, int M, int N, int K, void *y, lon
     return true;
 }
 
+// The limit of the waits that a test may shorten.
+unsigned long long short_wait_ns() { return test_wait_limit_ns() ? test_wait_limit_ns() : kWaitLimitNs; }
+
 // `n` jobs of p, the one with the longer items first
 template <bool kForward>
 rr_status launch_dense(DenseParams &p, int n, cudaStream_t st)
 {
     const int pairs = device_sm_count() / 2;
     if (pairs < 1) return RR_ERR_CUDA;
+    p.tfull_limit_ns = short_wait_ns();
     p.items[0] = p.job[0].items;
     p.items[1] = n > 1 ? p.job[1].items : 0;
     for (int k = 0; k < n; ++k) {
@@ -749,6 +755,7 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
     p.z = static_cast<__nv_bfloat16 *>(z);
     p.ldz = ldz;
     p.status = status;
+    p.done_limit_ns = short_wait_ns();
     // two CTAs on every SM, if each is left four k-blocks (1 x 4096 x 4096: 9.5 us with 256 CTAs, 10.0 with 128; 64 x 4096 x 1024: 6.9 us with
     // 128 CTAs of four k-blocks, 8.1 with 256 of two)
     p.split = 1;

@@ -70,9 +70,10 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     return true;
 }
 
-// As mbar_try_wait, but the thread may sleep in the instruction for up to about a millisecond: a waiting thread then takes no
+// As mbar_try_wait, but the thread may sleep in the instruction for up to about `nap_ns`: a waiting thread then takes no
 // issue slots from the warps that work.
-__device__ __forceinline__ bool mbar_try_sleep(uint64_t *bar, uint32_t parity)
+constexpr uint32_t kNapNs = 1000000;
+__device__ __forceinline__ bool mbar_try_sleep(uint64_t *bar, uint32_t parity, uint32_t nap_ns)
 {
     uint32_t ok;
     asm volatile(
@@ -80,21 +81,24 @@ __device__ __forceinline__ bool mbar_try_sleep(uint64_t *bar, uint32_t parity)
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(nap_ns)
         : "memory");
     return ok != 0;
 }
 
-// mbar_wait for loops that wait once per k-block: sleeping tries, and the clock is read only every sixteenth time one fails.
-__device__ __forceinline__ bool mbar_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status)
+// mbar_wait for loops that wait once per k-block: sleeping tries, and the clock is read only every sixteenth time one fails.  (A limit
+// below a nap is a test's: naps of that length, and a look at the clock after each.)
+__device__ __forceinline__ bool mbar_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status,
+                                                unsigned long long limit_ns = kWaitLimitNs)
 {
+    const uint32_t nap = limit_ns < kNapNs ? (uint32_t)limit_ns : kNapNs;
     unsigned long long t0 = 0;
-    for (uint32_t it = 1; !mbar_try_sleep(bar, parity); ++it) {
-        if ((it & 15u) == 0) {
+    for (uint32_t it = 1; !mbar_try_sleep(bar, parity, nap); ++it) {
+        if ((it & 15u) == 0 || limit_ns < kNapNs) {
             if (*abort_flag) return false;
             const unsigned long long now = globaltimer();
             if (t0 == 0) t0 = now;
-            if (now - t0 > kWaitLimitNs) {
+            if (now - t0 > limit_ns) {
                 *abort_flag = 1;
                 latch_status(status, RR_ERR_TIMEOUT);
                 return false;
@@ -114,10 +118,11 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volati
 }
 
 // Lane 0 waits asleep, the whole warp learns the outcome.
-__device__ __forceinline__ bool warp_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status)
+__device__ __forceinline__ bool warp_wait_brisk(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status,
+                                                unsigned long long limit_ns = kWaitLimitNs)
 {
     int ok = 1;
-    if ((threadIdx.x & 31) == 0) ok = mbar_wait_brisk(bar, parity, abort_flag, status) ? 1 : 0;
+    if ((threadIdx.x & 31) == 0) ok = mbar_wait_brisk(bar, parity, abort_flag, status, limit_ns) ? 1 : 0;
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
