@@ -473,7 +473,7 @@ rr_status rr_linear_bwd(const rr_linear_shape *s /* host */, const void *dy, con
  *     dL/da_ij = scale live_i g_ij ( alpha E / (S' n_s) (f_sj - sum_e f_se g_ie) + 2 beta / n lse_i ),  g_i = softmax(a_i)
  *   count, n_live as rr_balance_fwd wrote them; live, alpha, beta as there; scale a host value
  *   dlogits [T,E] fp32 dev: overwritten (zero where not live) when accumulate == 0, else added to (rows that are not
- *                live are left alone).  One kernel, no workspace.
+ *                live are left alone); may be the same buffer as logits.  One kernel, no workspace.
  */
 rr_status rr_balance_workspace_bytes(int T, int E, int S, size_t *bytes);
 rr_status rr_balance_fwd(int T, int E, int k, int stride, int S, const float *logits, const int32_t *topk_expert,

@@ -27,24 +27,25 @@ constexpr int kBalWarps = kBalThreads / 32;
 constexpr int kBalBlocks = 296;     // blocks wanted: two per SM, all resident at once
 constexpr int kBalFinal = 1024;     // threads of the second forward kernel
 
-// softmax of one row over the group's lanes and its log-sum-exp; a token that is not live takes part in the
-// shuffles with zeros
-template <int GS, int CPL, bool VEC>
-__device__ __forceinline__ void load_row(const float *__restrict__ a, bool in, int E, int gl, float (&g)[CPL])
+// the columns of one row that a lane keeps; minus infinity past E and where there is no row.  kReadOnly: nothing in the launch
+// writes to the scores (the gradient may be written over them, which loads past the coherent path would not be allowed to meet).
+template <int GS, int CPL, bool VEC, bool kReadOnly>
+__device__ __forceinline__ void load_row(const float *a, bool in, int E, int gl, float (&g)[CPL])
 {
+    auto get = [](const auto *p) { return kReadOnly ? __ldg(p) : *p; };
     if constexpr (VEC) {
 #pragma unroll
         for (int q = 0; q < CPL / 4; ++q) {
             const int j = column_of<GS, true>(4 * q, gl);
             float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            if (in && j < E) v = __ldg(reinterpret_cast<const float4 *>(a + j));
+            if (in && j < E) v = get(reinterpret_cast<const float4 *>(a + j));
             g[4 * q] = v.x; g[4 * q + 1] = v.y; g[4 * q + 2] = v.z; g[4 * q + 3] = v.w;
         }
     } else {
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
             const int j = column_of<GS, false>(c, gl);
-            g[c] = (in && j < E) ? __ldg(a + j) : -INFINITY;
+            g[c] = (in && j < E) ? get(a + j) : -INFINITY;
         }
     }
 }
@@ -307,8 +308,8 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
         const bool ina = ta < t1, inb = tb < t1;
         // rows, marks and choices are requested together, whatever the marks will say
         float ga[CPL], gb[CPL];
-        load_row<GS, CPL, VEC>(logits + (ina ? ta : 0) * E, ina, E, gl, ga);
-        load_row<GS, CPL, VEC>(logits + (inb ? tb : 0) * E, inb, E, gl, gb);
+        load_row<GS, CPL, VEC, true>(logits + (ina ? ta : 0) * E, ina, E, gl, ga);
+        load_row<GS, CPL, VEC, true>(logits + (inb ? tb : 0) * E, inb, E, gl, gb);
         const bool la = is_live(live, ina, ta), lb = is_live(live, inb, tb);
         const int ea = ina && gl < b.k ? __ldg(topk + ta * b.stride + gl) : 0, eb = inb && gl < b.k ? __ldg(topk + tb * b.stride + gl) : 0;
         if (la && gl < b.k) count_choice(ea);
@@ -382,7 +383,7 @@ k_balance_partial(const BalShape b, const float *__restrict__ logits, const int3
 // Backward: items of up to `slab` tokens of one segment, dealt to the blocks in turn.
 template <int GS, int CPL, bool VEC>
 __global__ void __launch_bounds__(kBalThreads)
-k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__restrict__ count, const int *__restrict__ n_live,
+k_balance_bwd(const BalShape b, const float *logits, const int *__restrict__ count, const int *__restrict__ n_live,
               const uint8_t *__restrict__ live, float coef_b, float coef_z, int accumulate, float *dlogits)
 {
     constexpr int TPW = 32 / GS;
@@ -413,7 +414,7 @@ k_balance_bwd(const BalShape b, const float *__restrict__ logits, const int *__r
             const long long t = base + grp;
             const bool in = t < t1;
             float g[CPL];
-            load_row<GS, CPL, VEC>(logits + (in ? t : 0) * E, in, E, gl, g);
+            load_row<GS, CPL, VEC, false>(logits + (in ? t : 0) * E, in, E, gl, g);
             const bool l = is_live(live, in, t);
             float inv, dot = 0.f;
             const float lse = softmax_lse<GS, CPL>(g, inv);
@@ -465,9 +466,10 @@ BalShape balance_shape(int T, int E, int k, int stride, int S, int want, int pas
     if (b.slab < 1) b.slab = 1;
     b.cps = (int)((b.L + b.slab - 1) / b.slab);
     if (b.cps < 1) b.cps = 1;
-    // One launch where the header has a counter for every segment and a block adds up a segment's parts in about the time that the second
-    // kernel takes to start: the device takes as long (four segments of 16 tokens: 6.7 us, 7.5 with two launches; 32 of 2048: 10.8 and
-    // 10.4), the caller 2 us less.  A segment in hundreds of parts keeps the second kernel, whose blocks are twice as large.
+    // One launch where the header has a counter for every segment (32 words were spare) and a block adds up a segment's parts in about the
+    // time that the second kernel takes to start.  The device takes as long, the caller 2 us less (with a mask, E = 64; in brackets with two launches:
+    // four segments of 16 tokens 6.2 us [7.8], 32 of 256 8.4 [8.9], 32 of 2048 11.0 [11.3], 4 of 4096 in 32 parts each 9.5 [9.3]).  A segment in
+    // more parts keeps the second kernel, whose blocks are twice as large (one of 16384 in 128 parts: 8.5 [7.6]).
     b.one = S <= 32 && b.cps <= 32;
     return b;
 }
