@@ -17,9 +17,9 @@ namespace {
 
 constexpr int kDropThreads = 256;
 
-// Blocks per SM, all resident at once.  Where every element moves 8 bytes or more HBM is the bound and fewer streams of reads and writes
+// Blocks per SM, all resident at once.  Where every element moves 6 bytes or more HBM is the bound and fewer streams of reads and writes
 // suit it better (2^26 elements, fp32 + bf16 residual -> bf16: 81.8 us with three, 84.7 with four, 95 with five; bf16 -> fp32: 69 and 78);
-// with 4 to 6 bytes the generator's integer work is as long and wants the warps (bf16 -> bf16: 52.2 and 48.0).
+// with 4 bytes the generator's integer work is as long and wants the warps (bf16 -> bf16: 52.2 with three, 48.0 with four).
 template <class TX, class TY>
 constexpr int drop_blocks() { return sizeof(TX) + sizeof(TY) == 4 ? 4 : 3; }
 

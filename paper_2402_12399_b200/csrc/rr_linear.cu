@@ -22,8 +22,9 @@ constexpr int kStageA = 128 * 128;       // this CTA's 128 rows of A, one k-bloc
 constexpr int kPanel = 64 * 128;         // MN-major panel: 64 k-rows x 64 columns
 // Warps: 0-2 TMA producers, 3 MMA issuer and TMEM owner, 4-15 epilogue.  The epilogue of a forward tile with everything in it is some
 // thirty instructions an element with long dependent chains (generator, activation): at K = 1024 longer than the main loop.  Three warps
-// per scheduler hide them best against the registers they leave each other (2048 x 4096 x 1024 with a residual: 20.7 us with twelve,
-// 21.4 with eight, 22.2 with sixteen; with GELU, dropout and z as well 30.2, 29.5, 30.7; K = 128: 105, 121, 100).
+// per scheduler hide them best against the registers they leave each other (with twelve, eight, sixteen: 2048 x 4096 x 1024 with a
+// residual 21.4, 21.8, 22.8 us, with GELU, dropout and z as well 30.8, 29.8, 31.2; 16384 x 4096 x 128 with everything 129, 140, 140,
+// without the residual 111, 127, 105).
 constexpr int kDenseProducers = 3, kDenseMma = 3, kDenseEpi0 = 4, kDenseEpiWarps = 12;
 constexpr int kDenseThreads = 32 * (kDenseEpi0 + kDenseEpiWarps);
 constexpr int kEpiBytes = 2048;          // staging of one epilogue warp
@@ -290,8 +291,9 @@ k_dense(const __grid_constant__ DenseParams p)
 // of a cluster (`split` = 1, 2, 4, 8), which keeps all SMs reading when there are few weight tiles.  The fp32 partial
 // tiles meet in shared memory: each CTA of the cluster adds up its share of the tokens, in the order of the
 // ranks (the result repeats bit for bit), and finishes them.  About 110 KB of shared memory a CTA: two share an SM.
-// 1 x 4096 x 4096: 8.8 us, 3.8 TB/s (256 CTAs; the read alone takes 5.1); 37 x 14336 x 4096: 23.2 us, 5.1 TB/s (0.79 of the measured copy
-// rate).  With more tokens the parts' way through the SM-to-SM network counts, at about 4 TB/s over all SMs (128 x 4096 x 4096: 13.0 us).
+// 1 x 4096 x 4096: 8.3 us, 4.0 TB/s (256 CTAs; the read alone takes 5.1), 9.2 with bias and residual; 37 x 14336 x 4096: 23.2 us, 5.1 TB/s (0.79 of the measured copy
+// rate).  With more tokens the parts' way through the SM-to-SM network counts, at about 4 TB/s over all SMs (128 x 4096 x 4096: 13.0 to 13.5 us;
+// the library's product 9.6 to 10).
 //   kWmn: the weights are MN-major (dx = dz W: the features are the columns of W, the contraction runs over its rows).
 constexpr int kSlimTokens = 128;   // up to here always
 constexpr int kSlimThreads = 320;  // warp 0: TMA, warp 1: MMA, warps 2-9: TMEM; all of them finish
@@ -756,7 +758,7 @@ rr_status launch_slim(Operand w, Operand x, int tokens, int features, int K, voi
     p.ldz = ldz;
     p.status = status;
     p.done_limit_ns = short_wait_ns();
-    // two CTAs on every SM, if each is left four k-blocks (1 x 4096 x 4096: 9.5 us with 256 CTAs, 10.0 with 128; 64 x 4096 x 1024: 6.9 us with
+    // two CTAs on every SM, if each is left four k-blocks (1 x 4096 x 4096 with bias and residual: 9.5 us with 256 CTAs, 10.0 with 128; 64 x 4096 x 1024: 6.9 us with
     // 128 CTAs of four k-blocks, 8.1 with 256 of two)
     p.split = 1;
     while (p.split < 8 && (long long)f_tiles * p.t_tiles * p.split * 2 <= 2 * 148 && p.kblocks >= 8 * p.split) p.split *= 2;
