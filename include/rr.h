@@ -6,8 +6,9 @@
  *  - "dev" pointers are CUDA device pointers of the current device, "host"
  *    pointers are ordinary host memory.  All dev pointers must be 16-byte
  *    aligned; hidden / weight / dout tensors must be 128-byte aligned (they are
- *    read through TMA).  Everything is row-major and densely packed (rr_linear_* ask for 16 bytes
- *    and take pitches).
+ *    read through TMA).  Everything is row-major and densely packed (rr_linear_*, rr_norm_* and
+ *    rr_embed_* ask for 16 bytes and take pitches; ids and the gradients of a clip need only the
+ *    alignment of their type).
  *  - The caller owns and allocates every buffer, including the workspace.  The
  *    library allocates no device memory and keeps no state between calls other
  *    than lazily resolved driver entry points.
@@ -41,7 +42,7 @@ enum {
     RR_ERR_UNSUPPORTED = 2,        /* valid request this build has no kernel for            */
     RR_ERR_WORKSPACE_TOO_SMALL = 3,
     RR_ERR_CUDA = 4,               /* a CUDA runtime / driver call failed                   */
-    RR_ERR_NONFINITE = 5,          /* device: a logit was NaN or Inf (tables are undefined) */
+    RR_ERR_NONFINITE = 5,          /* device: a logit (tables are undefined) or a gradient was NaN or Inf */
     RR_ERR_TIMEOUT = 6,            /* device: a bounded wait inside a kernel ran out        */
     RR_ERR_STATIC_SCRATCH_EXCEEDED = 7 /* rr_route_noalloc: shape needs more than its fixed scratch */
 };
@@ -484,6 +485,123 @@ rr_status rr_balance_fwd(int T, int E, int k, int stride, int S, const float *lo
 rr_status rr_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
                          const uint8_t *live, float alpha, float beta, float scale, int accumulate, float *dlogits,
                          void *stream);
+
+/*
+ * ---- The rest of a training step around the layer ----------------------------------------------------------
+ * (no counterpart in the paper either: the norm in front of a branch with the residual add of the branch before it, the embedding in front of
+ * the first block, and the clip of all gradients behind the last.)
+ */
+
+/* kinds of norm */
+#define RR_NORM_LAYER 0 /* mean taken off */
+#define RR_NORM_RMS 1   /* divided by the root of the mean square only */
+
+/* Shape of one norm call.  Pitches count elements between rows; 0 means densely packed. */
+typedef struct rr_norm_shape {
+    int32_t M, N;              /* rows (tokens, >= 0) and columns, 1 <= N <= 32768               */
+    int32_t kind;              /* RR_NORM_*                                                      */
+    int32_t x_dtype;           /* RR_BF16 or RR_F32: type of x (forward)                         */
+    int32_t h_dtype;           /* type of residual and h                                         */
+    int32_t w_dtype;           /* type of w and b                                                */
+    int32_t y_dtype;           /* type of y (forward), dy (backward)                             */
+    int32_t dx_dtype;          /* type of dx and dh (backward)                                   */
+    uint32_t flags;            /* RR_ADD_DW (backward): add to dw and db instead of overwriting  */
+    float eps;                 /* >= 0, finite                                                   */
+    int64_t ldx, ldr, ldh, ldy; /* pitches of x, residual, h, y: at least N, less than 2^40 bytes */
+    int64_t lddy, lddh, lddx;  /* of dy, dh, dx                                                  */
+} rr_norm_shape;
+
+/*
+ * rr_norm_fwd:  h = residual + x, rounded to h's type (h = x where residual is NULL),
+ *     mu = mean of the row of h (0 with RR_NORM_RMS),  rstd = 1 / sqrt(mean((h - mu)^2) + eps),  y = (h - mu) rstd w + b
+ *   x [M,N], residual [M,N] or NULL        dev, read only
+ *   w [N], b [N]                           dev; w NULL is 1, b NULL is 0
+ *   h [M,N] dev: the new residual stream; NULL when it is not wanted, and without a residual
+ *   y [M,N] dev;  mean [M], rstd [M] fp32 dev, each NULL when not wanted (rr_norm_bwd takes them; no mean with RR_NORM_RMS)
+ *   h may be the same buffer as residual or x, y the same as x or residual (same type and pitch)
+ * rr_norm_bwd, for given dy [M,N], xh = (h - mu) rstd, g = dy w:
+ *     dx = dh + rstd (g - mean(g) - xh mean(g xh))   (no mean(g) with RR_NORM_RMS)
+ *     dw = sum over the rows of dy xh,   db = sum over the rows of dy
+ *   h, w, mean, rstd as in the forward pass (h is x where that had no residual)
+ *   dh [M,N] or NULL: gradient that reaches h along the residual stream, type dx_dtype
+ *   dx [M,N]: the gradient of h, which is that of x and of residual;  dw [N], db [N] fp32.  Each of the three may be NULL.
+ *   dx may be the same buffer as dy, h or dh (same type and pitch)
+ *   workspace dev, >= rr_norm_workspace_bytes, 256-byte aligned
+ * The arithmetic is fp32 with one rounding to the type of each result; a row is held on the chip, so the variance is a mean of squared
+ * differences, and all sums have a fixed order: results repeat bit for bit.  Matrices are read 16 bytes at a time where N is a multiple of 8 and
+ * pitches are multiples of 16 bytes, and element by element otherwise; any pitch of at least N is taken.  M == 0 does nothing
+ * forward and sets dw and db to zero backward (or leaves them under RR_ADD_DW).  An output that overlaps what the call reads, or another
+ * output, in any other way than named is refused, as for rr_linear_*.  Calls that share a workspace must not overlap on the GPU.
+ */
+rr_status rr_norm_workspace_bytes(int M, int N, size_t *bwd_bytes);
+rr_status rr_norm_fwd(const rr_norm_shape *s /* host */, const void *x, const void *residual, const void *w, const void *b, void *h, void *y,
+                      float *mean, float *rstd, void *stream);
+rr_status rr_norm_bwd(const rr_norm_shape *s /* host */, const void *dy, const void *h, const void *w, const float *mean, const float *rstd,
+                      const void *dh, void *dx, float *dw, float *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Shape of one embedding call. */
+typedef struct rr_embed_shape {
+    int32_t n, V, d;           /* tokens (0 <= n <= 2^30), rows of the table, width; 1 <= V, d <= 2^30, V d < 2^40 */
+    int32_t wide_ids;          /* 0: ids are i32, 1: i64                                         */
+    int32_t table_dtype;       /* RR_BF16 or RR_F32: type of table / dtable                      */
+    int32_t y_dtype;           /* type of y / dy                                                 */
+    uint32_t flags;            /* RR_ADD_DW (backward)                                           */
+    float scale;               /* finite                                                         */
+    int64_t ldy;               /* pitch of y / dy in elements, at least d and less than 2^40 bytes; 0: densely packed */
+} rr_embed_shape;
+
+/*
+ * rr_embed_fwd:  y_i = scale table[id_i];  id -1 stands for no token (padding) and gives a row of zeros
+ * rr_embed_bwd:  dtable_v = scale (sum over the tokens i with id_i = v of dy_i), rows without a token 0; under RR_ADD_DW added to what
+ *                dtable holds (rows without a token are not touched).  What dy holds for id -1 does not matter.
+ *   ids [n] dev, i32 or i64, aligned to their size;  an id outside -1..V-1 counts as -1 and latches RR_ERR_INVALID_ARG in the workspace header
+ *   table, dtable [V,d] dev, 16-byte aligned, dense;  y, dy [n,d] dev, 16-byte aligned
+ *   workspace dev, >= fwd_bytes / bwd_bytes, 256-byte aligned; its first 256 bytes are zero when first used (the status word)
+ * fp32 arithmetic, one rounding to the result's type (under RR_ADD_DW of the sum with what was there).  The gradient's sums follow the order
+ * of the tokens, in pieces that depend on n and the ids alone: results repeat bit for bit.  n == 0 does nothing forward; backward
+ * it sets dtable to zero, or leaves it under RR_ADD_DW.  An output that overlaps what the call reads is refused.  Calls that share a
+ * workspace must not overlap on the GPU.
+ */
+rr_status rr_embed_workspace_bytes(int n, int V, int d, size_t *fwd_bytes, size_t *bwd_bytes);
+rr_status rr_embed_fwd(const rr_embed_shape *s /* host */, const void *ids, const void *table, void *y, void *workspace,
+                       size_t workspace_bytes, void *stream);
+rr_status rr_embed_bwd(const rr_embed_shape *s /* host */, const void *ids, const void *dy, void *dtable, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* One gradient of a list: n elements, densely packed, each address aligned to its element. */
+typedef struct rr_grad {
+    const void *src;
+    void *dst;                 /* where the clipped gradient goes: src itself (same type), another buffer, or NULL: only in the norm */
+    int64_t n;                 /* >= 0 */
+    int32_t src_dtype, dst_dtype; /* RR_BF16 or RR_F32 (dst_dtype is ignored without dst) */
+} rr_grad;
+
+/* A list made ready for rr_clip_grads (filled in by rr_grad_plan; host). */
+typedef struct rr_grad_set {
+    void *plan;                /* the caller's device buffer, which now describes the list */
+    int32_t tensors, chunk;
+    int64_t chunks;
+} rr_grad_set;
+
+/*
+ * rr_grad_plan -- describe a list of up to 2^20 gradients to the device, once per program: the addresses stay those of the list until it
+ * is made anew.  `plan` is a device buffer of >= rr_grad_plan_bytes, 16-byte aligned; it is written by small kernels on `stream` (nothing is
+ * copied from host memory, so `list` may go at once and the call may be captured).  Returns RR_ERR_INVALID_ARG for a missing or misaligned
+ * address, for 2^42 elements or more in all, and where two of the buffers overlap (other than src and dst of one entry that are the same).
+ * rr_clip_grads -- clipping by the global norm:
+ *     norm = sqrt(sum of the squares of all elements of all src),  f = min(1, bound / (norm + 1e-6)),  dst = f src
+ *   bound >= 0, infinity for the norm alone;  norm [2] fp32 dev: norm and f
+ *   workspace dev, >= rr_clip_workspace_bytes, 256-byte aligned; its first 256 bytes are zero when first used
+ * Squares of fp32 are added eight at a time in fp32 and those sums in 64 bits (or all in 64 bits where fp32 would overflow or lose them), in a
+ * fixed order; the results repeat bit for bit.  In place with f = 1 nothing is written.  If an element is not finite, norm is not either: f is
+ * 1 (other buffers get unscaled copies) and RR_ERR_NONFINITE is latched.  No tensors, or none with elements: norm is 0.
+ * Calls that share a workspace, or buffers, must not overlap on the GPU.
+ */
+rr_status rr_grad_plan_bytes(int tensors, size_t *bytes);
+rr_status rr_grad_plan(int tensors, const rr_grad *list /* host */, void *plan /* dev */, size_t plan_bytes, rr_grad_set *set /* host */,
+                       void *stream);
+rr_status rr_clip_workspace_bytes(size_t *bytes);
+rr_status rr_clip_grads(const rr_grad_set *set /* host */, float bound, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * rr_check -- synchronise `stream`, then return the status word latched in `workspace`

@@ -27,6 +27,8 @@ ACT_GELU_TANH = 3
 ACT_SILU = 4
 ADD_DX = 1
 ADD_DW = 2
+NORM_LAYER = 0
+NORM_RMS = 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librr.so")
@@ -50,6 +52,24 @@ class _CLinear(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "act", "y_dtype", "dx_dtype", "dw_dtype")] + \
         [("flags", C.c_uint32), ("p", C.c_float)] + \
         [(n, C.c_int64) for n in ("ldx", "ldr", "ldy", "ldz", "lddy", "lddx")]
+
+
+class _CNorm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "kind", "x_dtype", "h_dtype", "w_dtype", "y_dtype", "dx_dtype")] + \
+        [("flags", C.c_uint32), ("eps", C.c_float)] + [(n, C.c_int64) for n in ("ldx", "ldr", "ldh", "ldy", "lddy", "lddh", "lddx")]
+
+
+class _CEmbed(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "V", "d", "wide_ids", "table_dtype", "y_dtype")] + \
+        [("flags", C.c_uint32), ("scale", C.c_float), ("ldy", C.c_int64)]
+
+
+class _CGrad(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("src_dtype", C.c_int32), ("dst_dtype", C.c_int32)]
+
+
+class _CGradSet(C.Structure):
+    _fields_ = [("plan", C.c_void_p), ("tensors", C.c_int32), ("chunk", C.c_int32), ("chunks", C.c_int64)]
 
 
 class RRError(RuntimeError):
@@ -106,6 +126,16 @@ def lib():
         L.rr_balance_workspace_bytes.argtypes = [C.c_int] * 3 + [C.POINTER(C.c_size_t)]
         L.rr_balance_fwd.argtypes = [C.c_int] * 5 + [C.c_void_p] * 3 + [C.c_float] * 2 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
         L.rr_balance_bwd.argtypes = [C.c_int] * 4 + [C.c_void_p] * 4 + [C.c_float] * 3 + [C.c_int, C.c_void_p, C.c_void_p]
+        L.rr_norm_workspace_bytes.argtypes = [C.c_int] * 2 + [C.POINTER(C.c_size_t)]
+        L.rr_norm_fwd.argtypes = [C.POINTER(_CNorm)] + [C.c_void_p] * 9
+        L.rr_norm_bwd.argtypes = [C.POINTER(_CNorm)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
+        L.rr_embed_workspace_bytes.argtypes = [C.c_int] * 3 + [C.POINTER(C.c_size_t)] * 2
+        L.rr_embed_fwd.argtypes = [C.POINTER(_CEmbed)] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        L.rr_embed_bwd.argtypes = [C.POINTER(_CEmbed)] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        L.rr_grad_plan_bytes.argtypes = [C.c_int, C.POINTER(C.c_size_t)]
+        L.rr_grad_plan.argtypes = [C.c_int, C.POINTER(_CGrad), C.c_void_p, C.c_size_t, C.POINTER(_CGradSet), C.c_void_p]
+        L.rr_clip_workspace_bytes.argtypes = [C.POINTER(C.c_size_t)]
+        L.rr_clip_grads.argtypes = [C.POINTER(_CGradSet), C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -716,3 +746,197 @@ def balance_bwd(logits: torch.Tensor, count: torch.Tensor, n_live: torch.Tensor,
     if code:
         raise RRError(code, "rr_balance_bwd")
     return dlogits
+
+
+# ---- the rest of a training step around the layer ------------------------------------------------------
+
+def norm_workspace_bytes(M: int, N: int) -> int:
+    """Workspace bytes of norm_bwd."""
+    a = C.c_size_t(0)
+    _ok(lib().rr_norm_workspace_bytes(M, N, C.byref(a)), "rr_norm_workspace_bytes")
+    return a.value
+
+
+def _vector(t, n: int, dtype, what: str):
+    if t is None:
+        return None
+    if t.shape != (n,) or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        _same_shape(t, (n,), what)
+        raise TypeError(f"{what} must be contiguous" + ("" if dtype is None else f" {dtype}") + f", got {t.dtype}")
+    return t.data_ptr()
+
+
+def _parameters(weight, bias, N: int) -> int:
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError(f"weight is {weight.dtype}, bias {bias.dtype}")
+    t = weight if weight is not None else bias
+    return BF16 if t is None else _code(t, "weight" if t is weight else "bias")
+
+
+def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+             kind: int = NORM_LAYER, eps: float = 1e-5, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+             h: torch.Tensor | None = None, mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None) -> torch.Tensor:
+    """rr_norm_fwd; returns y [M,N] = norm(residual + x) * weight + bias (type: out's, else out_dtype, else the residual's, else x's).
+    Pass `h`, of the residual's type, to receive residual + x (it may be the residual itself), and `mean`, `rstd` [M] fp32 to keep the
+    statistics for norm_bwd (no mean with NORM_RMS).  x, residual, h and out may be views whose rows lie apart."""
+    M, N = x.shape
+    if out is None:
+        out = torch.empty(M, N, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
+    here = _here()
+    _elsewhere(here, x, weight, bias, residual, h, out, mean, rstd)
+    if h is not None:
+        if residual is None:
+            raise ValueError("h is residual + x: it needs a residual")
+        if h.dtype != residual.dtype:
+            raise TypeError(f"residual is {residual.dtype}, h {h.dtype}")
+    s = _CNorm(M, N, kind, _code(x, "x"), 0 if residual is None else _code(residual, "residual"), _parameters(weight, bias, N), _code(out, "out"), 0, 0, eps,
+               _pitch(x, M, N, "x"), _pitch(residual, M, N, "residual"), _pitch(h, M, N, "h"), _pitch(out, M, N, "out"), 0, 0, 0)
+    code = (_lib or lib()).rr_norm_fwd(C.byref(s), x.data_ptr(), None if residual is None else residual.data_ptr(), _vector(weight, N, None, "weight"),
+                                       _vector(bias, N, None, "bias"), None if h is None else h.data_ptr(), out.data_ptr(), _vector(mean, M, _F32, "mean"),
+                                       _vector(rstd, M, _F32, "rstd"), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_norm_fwd")
+    return out
+
+
+def norm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor | None, rstd: torch.Tensor, kind: int = NORM_LAYER,
+             dh: torch.Tensor | None = None, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, dbias: torch.Tensor | None = None,
+             add_dw: bool = False, workspace: torch.Tensor | None = None):
+    """rr_norm_bwd; writes the gradients whose buffers are given -- dx [M,N] (bf16 or fp32; the gradient of h, so that of x and of the
+    residual), dw [N] and dbias [N] fp32 -- and returns (dx, dw, dbias).  `h` is what the norm was taken of (x where there was no residual);
+    `dh`, of dx's type, is the gradient that reaches it along the residual stream.  With add_dw, dw and dbias are added to."""
+    M, N = dy.shape
+    if workspace is None:
+        workspace = alloc_workspace(norm_workspace_bytes(M, N), dy.device)
+    here = _here()
+    _elsewhere(here, dy, h, weight, mean, rstd, dh, dx, dw, dbias, workspace)
+    if dh is not None and dx is not None and dh.dtype != dx.dtype:
+        raise TypeError(f"dh is {dh.dtype}, dx {dx.dtype}")
+    t = dx if dx is not None else dh
+    s = _CNorm(M, N, kind, 0, _code(h, "h"), _parameters(weight, None, N), _code(dy, "dy"), 0 if t is None else _code(t, "dx"),
+               ADD_DW if add_dw else 0, 0.0, 0, 0, _pitch(h, M, N, "h"), 0, _pitch(dy, M, N, "dy"), _pitch(dh, M, N, "dh"), _pitch(dx, M, N, "dx"))
+    code = (_lib or lib()).rr_norm_bwd(C.byref(s), dy.data_ptr(), h.data_ptr(), _vector(weight, N, None, "weight"), _vector(mean, M, _F32, "mean"),
+                                       _vector(rstd, M, _F32, "rstd"), None if dh is None else dh.data_ptr(), None if dx is None else dx.data_ptr(),
+                                       _vector(dw, N, _F32, "dw"), _vector(dbias, N, _F32, "dbias"), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_norm_bwd")
+    for t in (dx, dw, dbias):
+        if t is not None:
+            t._workspace = workspace
+    return dx, dw, dbias
+
+
+def embed_workspace_bytes(n: int, V: int, d: int):
+    """(fwd workspace bytes, bwd workspace bytes) of the embedding of n tokens."""
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _ok(lib().rr_embed_workspace_bytes(n, V, d, C.byref(a), C.byref(b)), "rr_embed_workspace_bytes")
+    return a.value, b.value
+
+
+def _token_ids(ids) -> int:
+    if ids.dtype not in (_I32, torch.int64) or not ids.is_contiguous():
+        raise TypeError(f"ids are contiguous int32 or int64, got {ids.dtype}")
+    return 1 if ids.dtype == torch.int64 else 0
+
+
+def embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+              workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """rr_embed_fwd; returns y [n,d] = scale * table[ids] (type: out's, else out_dtype, else the table's).  `ids` may have any shape, n is
+    their number; -1 gives a row of zeros, any other id outside the table too and latches an error that check(out._workspace) raises.  out
+    may be a view whose rows lie apart."""
+    V, d = table.shape
+    n = ids.numel()
+    if out is None:
+        out = torch.empty(n, d, dtype=out_dtype or table.dtype, device=table.device)
+    if workspace is None:
+        workspace = alloc_workspace(embed_workspace_bytes(n, V, d)[0], table.device)
+    here = _here()
+    _elsewhere(here, ids, table, out, workspace)
+    if not table.is_contiguous():
+        raise ValueError("table must be contiguous")
+    s = _CEmbed(n, V, d, _token_ids(ids), _code(table, "table"), _code(out, "out"), 0, scale, _pitch(out, n, d, "out"))
+    code = (_lib or lib()).rr_embed_fwd(C.byref(s), ids.data_ptr(), table.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_embed_fwd")
+    out._workspace = workspace
+    return out
+
+
+def embed_bwd(ids: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+              workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """rr_embed_bwd; writes (or, with accumulate, adds to) the gradient of the table [V,d], bf16 or fp32, and returns it.  dy [n,d] may be a
+    view whose rows lie apart."""
+    V, d = dtable.shape
+    n = ids.numel()
+    if workspace is None:
+        workspace = alloc_workspace(embed_workspace_bytes(n, V, d)[1], dtable.device)
+    here = _here()
+    _elsewhere(here, ids, dy, dtable, workspace)
+    if not dtable.is_contiguous():
+        raise ValueError("dtable must be contiguous")
+    s = _CEmbed(n, V, d, _token_ids(ids), _code(dtable, "dtable"), _code(dy, "dy"), ADD_DW if accumulate else 0, scale, _pitch(dy, n, d, "dy"))
+    code = (_lib or lib()).rr_embed_bwd(C.byref(s), ids.data_ptr(), dy.data_ptr(), dtable.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_embed_bwd")
+    dtable._workspace = workspace
+    return dtable
+
+
+class GradPlan:
+    """A list of gradients as clip_grads takes it (see grad_plan).  It keeps the tensors alive; the addresses are those they had when it
+    was made."""
+
+    def __init__(self, grads, out, set_, buffer):
+        self.grads, self.out, self.set, self.buffer = grads, out, set_, buffer
+
+
+def grad_plan(grads, out=None) -> GradPlan:
+    """rr_grad_plan; describes a list of gradients (contiguous, bf16 or fp32) to the device, once per program.  They are clipped in place, or
+    into `out`: as many contiguous tensors of the same shapes, or None for one that only counts for the norm."""
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads):
+        raise ValueError(f"{len(grads)} gradients, but {len(out)} outputs")
+    here = _here()
+    _elsewhere(here, *grads, *out)
+    items = (_CGrad * max(1, len(grads)))()
+    for g, o, c in zip(grads, out, items):
+        if not g.is_contiguous() or (o is not None and not o.is_contiguous()):
+            raise ValueError("gradients and their outputs must be contiguous")
+        if o is not None:
+            _same_shape(o, g.shape, "out")
+        c.src, c.n, c.src_dtype = g.data_ptr(), g.numel(), _code(g, "a gradient")
+        if o is not None:
+            c.dst, c.dst_dtype = o.data_ptr(), _code(o, "an output")
+    n = C.c_size_t(0)
+    _ok(lib().rr_grad_plan_bytes(len(grads), C.byref(n)), "rr_grad_plan_bytes")
+    buffer = torch.empty(n.value, dtype=torch.uint8, device=torch.device("cuda", here))
+    s = _CGradSet()
+    _ok(lib().rr_grad_plan(len(grads), items, buffer.data_ptr(), buffer.numel(), C.byref(s), _stream_of(here)), "rr_grad_plan")
+    return GradPlan(grads, out, s, buffer)
+
+
+def clip_workspace_bytes() -> int:
+    """Workspace bytes of clip_grads."""
+    a = C.c_size_t(0)
+    _ok(lib().rr_clip_workspace_bytes(C.byref(a)), "rr_clip_workspace_bytes")
+    return a.value
+
+
+def clip_grads(plan, bound: float, norm: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """rr_clip_grads; scales the gradients of `plan` (a GradPlan, or a list of tensors to be clipped in place) by
+    min(1, bound / (norm + 1e-6)) and returns norm [2] fp32: the global norm and that factor.  bound = inf: the norm alone."""
+    if not isinstance(plan, GradPlan):
+        plan = grad_plan(plan)
+    buffer = plan.buffer
+    if norm is None:
+        norm = torch.empty(2, dtype=_F32, device=buffer.device)
+    if workspace is None:
+        workspace = alloc_workspace(clip_workspace_bytes(), buffer.device)
+    here = _here()
+    _elsewhere(here, buffer, norm, workspace)
+    code = (_lib or lib()).rr_clip_grads(C.byref(plan.set), bound, _vector(norm, 2, _F32, "norm"), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    if code:
+        raise RRError(code, "rr_clip_grads")
+    norm._workspace, norm._plan = workspace, plan
+    return norm

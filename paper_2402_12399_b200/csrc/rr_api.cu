@@ -1,5 +1,9 @@
 // C-ABI entry points of librr (declared and documented in include/rr.h):
 // argument checks, workspace layout, launches.  No device memory is allocated here.
+#include <stdlib.h>
+
+#include <algorithm>
+
 #include "rr_common.cuh"
 #include "rr_ffn.cuh"
 
@@ -601,6 +605,252 @@ rr_status rr_balance_bwd(int T, int E, int k, int S, const float *logits, const 
                                   static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+
+int bytes_of(int dtype) { return dtype == RR_F32 ? 4 : 2; }
+
+// a pitch of `width` elements of `size` bytes that nothing asks to be aligned: 0 becomes the width; the limits of fill_pitch
+bool fill_loose_pitch(int64_t *ld, int width, int size, int rows)
+{
+    if (*ld == 0) *ld = width;
+    return *ld >= width && *ld < (1ll << 40) / size && *ld <= (1ll << 62) / size / (rows > 0 ? rows : 1);
+}
+
+rr_status check_norm(const rr_norm_shape *in, rr_norm_shape *s)
+{
+    if (!in) return RR_ERR_INVALID_ARG;
+    *s = *in;
+    if (s->M < 0 || s->N < 1 || s->N > 32768 || (s->kind != RR_NORM_LAYER && s->kind != RR_NORM_RMS)) return RR_ERR_INVALID_ARG;
+    if (!is_dtype(s->x_dtype) || !is_dtype(s->h_dtype) || !is_dtype(s->w_dtype) || !is_dtype(s->y_dtype) || !is_dtype(s->dx_dtype)) return RR_ERR_INVALID_ARG;
+    if ((s->flags & ~RR_ADD_DW) || !(s->eps >= 0.0f && s->eps <= 3.0e38f)) return RR_ERR_INVALID_ARG;
+    const int hs = bytes_of(s->h_dtype), ys = bytes_of(s->y_dtype), ds = bytes_of(s->dx_dtype);
+    if (!fill_loose_pitch(&s->ldx, s->N, bytes_of(s->x_dtype), s->M) || !fill_loose_pitch(&s->ldr, s->N, hs, s->M) ||
+        !fill_loose_pitch(&s->ldh, s->N, hs, s->M) || !fill_loose_pitch(&s->ldy, s->N, ys, s->M) || !fill_loose_pitch(&s->lddy, s->N, ys, s->M) ||
+        !fill_loose_pitch(&s->lddh, s->N, ds, s->M) || !fill_loose_pitch(&s->lddx, s->N, ds, s->M))
+        return RR_ERR_INVALID_ARG;
+    return RR_OK;
+}
+
+// An output against something that is read: apart, or (where `same` allows it) the very same matrix of the same type.
+bool in_the_way(const Region &out, int out_dtype, const Region &in, int in_dtype, bool same)
+{
+    if (same && out.p == in.p && out_dtype == in_dtype && (out.rows == 1 || out.pitch == in.pitch)) return false;
+    return overlap(out, in);
+}
+
+}  // namespace
+
+rr_status rr_norm_workspace_bytes(int M, int N, size_t *bwd_bytes)
+{
+    if (M < 0 || N < 1 || N > 32768 || !bwd_bytes) return RR_ERR_INVALID_ARG;
+    *bwd_bytes = rr::norm_workspace(M, N);
+    return RR_OK;
+}
+
+rr_status rr_norm_fwd(const rr_norm_shape *shape, const void *x, const void *residual, const void *w, const void *b, void *h, void *y, float *mean,
+                      float *rstd, void *stream)
+{
+    rr_norm_shape s;
+    rr_status rc = check_norm(shape, &s);
+    if (rc) return rc;
+    if (s.M == 0) return RR_OK;
+    if (!x || !y || (h && !residual) || (mean && s.kind != RR_NORM_LAYER)) return RR_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(w, 16) || !aligned(b, 16) || !aligned(h, 16) || !aligned(y, 16) || !aligned(mean, 16) ||
+        !aligned(rstd, 16))
+        return RR_ERR_INVALID_ARG;
+    const int xs = bytes_of(s.x_dtype), hs = bytes_of(s.h_dtype), ys = bytes_of(s.y_dtype), ps = bytes_of(s.w_dtype);
+    const Region rx = matrix(x, s.M, s.N, s.ldx, xs), rres = matrix(residual, s.M, s.N, s.ldr, hs), rw = matrix(w, 1, s.N, s.N, ps),
+                 rb = matrix(b, 1, s.N, s.N, ps);
+    const Region out[4] = {matrix(h, s.M, s.N, s.ldh, hs), matrix(y, s.M, s.N, s.ldy, ys), matrix(mean, 1, s.M, s.M, 4), matrix(rstd, 1, s.M, s.M, 4)};
+    const int type[4] = {s.h_dtype, s.y_dtype, RR_F32, RR_F32};
+    for (int i = 0; i < 4; ++i) {
+        if (in_the_way(out[i], type[i], rx, s.x_dtype, i < 2) || in_the_way(out[i], type[i], rres, s.h_dtype, i < 2) || overlap(out[i], rw) || overlap(out[i], rb))
+            return RR_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return RR_ERR_INVALID_ARG;
+    }
+    return rr::launch_norm_fwd(s, x, residual, w, b, h, y, mean, rstd, static_cast<cudaStream_t>(stream));
+}
+
+rr_status rr_norm_bwd(const rr_norm_shape *shape, const void *dy, const void *h, const void *w, const float *mean, const float *rstd, const void *dh,
+                      void *dx, float *dw, float *db, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rr_norm_shape s;
+    rr_status rc = check_norm(shape, &s);
+    if (rc) return rc;
+    if (!aligned(dx, 16) || !aligned(dw, 16) || !aligned(db, 16)) return RR_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.M == 0) {  // no rows: the gradients of the parameters are zero
+        if (!(s.flags & RR_ADD_DW) && ((dw && cudaMemsetAsync(dw, 0, (size_t)s.N * 4, st) != cudaSuccess) ||
+                                       (db && cudaMemsetAsync(db, 0, (size_t)s.N * 4, st) != cudaSuccess)))
+            return RR_ERR_CUDA;
+        return RR_OK;
+    }
+    if (!dy || !h || !rstd || !workspace || (s.kind == RR_NORM_LAYER && !mean)) return RR_ERR_INVALID_ARG;
+    if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(w, 16) || !aligned(mean, 16) || !aligned(rstd, 16) || !aligned(dh, 16) || !aligned(workspace, 256))
+        return RR_ERR_INVALID_ARG;
+    const int hs = bytes_of(s.h_dtype), ys = bytes_of(s.y_dtype), ds = bytes_of(s.dx_dtype);
+    const Region rin[3] = {matrix(dy, s.M, s.N, s.lddy, ys), matrix(h, s.M, s.N, s.ldh, hs), matrix(dh, s.M, s.N, s.lddh, ds)};
+    const int tin[3] = {s.y_dtype, s.h_dtype, s.dx_dtype};
+    const Region vin[3] = {matrix(w, 1, s.N, s.N, bytes_of(s.w_dtype)), matrix(s.kind == RR_NORM_LAYER ? mean : nullptr, 1, s.M, s.M, 4),
+                           matrix(rstd, 1, s.M, s.M, 4)};
+    const Region out[3] = {matrix(dx, s.M, s.N, s.lddx, ds), matrix(dw, 1, s.N, s.N, 4), matrix(db, 1, s.N, s.N, 4)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 3; ++j)
+            if (in_the_way(out[i], s.dx_dtype, rin[j], tin[j], i == 0) || overlap(out[i], vin[j])) return RR_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return RR_ERR_INVALID_ARG;
+    }
+    if (!dx && !dw && !db) return RR_OK;
+    if (rr::norm_workspace(s.M, s.N) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_norm_bwd(s, dy, h, w, mean, rstd, dh, dx, dw, db, workspace, st);
+}
+
+namespace {
+
+rr_status check_embed_sizes(long long n, long long V, long long d)
+{
+    constexpr long long kMost = 1ll << 30;
+    return n < 0 || n > kMost || V < 1 || V > kMost || d < 1 || d > kMost || V * d >= 1ll << 40 ? RR_ERR_INVALID_ARG : RR_OK;
+}
+
+rr_status check_embed(const rr_embed_shape *in, rr_embed_shape *s)
+{
+    if (!in) return RR_ERR_INVALID_ARG;
+    *s = *in;
+    rr_status rc = check_embed_sizes(s->n, s->V, s->d);
+    if (rc) return rc;
+    if ((s->wide_ids != 0 && s->wide_ids != 1) || !is_dtype(s->table_dtype) || !is_dtype(s->y_dtype) || (s->flags & ~RR_ADD_DW)) return RR_ERR_INVALID_ARG;
+    if (!(s->scale >= -3.4e38f && s->scale <= 3.4e38f)) return RR_ERR_INVALID_ARG;
+    return fill_loose_pitch(&s->ldy, s->d, bytes_of(s->y_dtype), s->n) ? RR_OK : RR_ERR_INVALID_ARG;
+}
+
+rr_status check_embed_call(const rr_embed_shape &s, const void *ids, const void *in, const void *out, const void *workspace, bool back)
+{
+    if (!ids || !in || !out || !workspace) return RR_ERR_INVALID_ARG;
+    if (!aligned(ids, s.wide_ids ? 8 : 4) || !aligned(in, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    const Region rows = matrix(back ? in : out, s.n, s.d, s.ldy, bytes_of(s.y_dtype)), tab = matrix(back ? out : in, 1, (long long)s.V * s.d, (long long)s.V * s.d, bytes_of(s.table_dtype)),
+                 rid = matrix(ids, 1, s.n, s.n, s.wide_ids ? 8 : 4);
+    return overlap(rows, tab) || overlap(back ? tab : rows, rid) ? RR_ERR_INVALID_ARG : RR_OK;
+}
+
+}  // namespace
+
+rr_status rr_embed_workspace_bytes(int n, int V, int d, size_t *fwd_bytes, size_t *bwd_bytes)
+{
+    rr_status rc = check_embed_sizes(n, V, d);
+    if (rc) return rc;
+    if (fwd_bytes) *fwd_bytes = rr::kHeaderBytes;
+    if (bwd_bytes) *bwd_bytes = rr::embed_bwd_workspace(n, d);
+    return RR_OK;
+}
+
+rr_status rr_embed_fwd(const rr_embed_shape *shape, const void *ids, const void *table, void *y, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rr_embed_shape s;
+    rr_status rc = check_embed(shape, &s);
+    if (rc || s.n == 0) return rc;
+    rc = check_embed_call(s, ids, table, y, workspace, false);
+    if (rc) return rc;
+    if (workspace_bytes < (size_t)rr::kHeaderBytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_embed_fwd(s, ids, table, y, workspace, static_cast<cudaStream_t>(stream));
+}
+
+rr_status rr_embed_bwd(const rr_embed_shape *shape, const void *ids, const void *dy, void *dtable, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rr_embed_shape s;
+    rr_status rc = check_embed(shape, &s);
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.n == 0) {  // no tokens: the gradient is zero
+        if (s.flags & RR_ADD_DW) return RR_OK;
+        if (!dtable || !aligned(dtable, 16)) return RR_ERR_INVALID_ARG;
+        return cudaMemsetAsync(dtable, 0, (size_t)s.V * s.d * bytes_of(s.table_dtype), st) == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    }
+    rc = check_embed_call(s, ids, dy, dtable, workspace, true);
+    if (rc) return rc;
+    if (rr::embed_bwd_workspace(s.n, s.d) > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_embed_bwd(s, ids, dy, dtable, workspace, st);
+}
+
+namespace {
+
+constexpr int kMostGrads = 1 << 20;
+
+struct Span {
+    uintptr_t at, end;
+};
+
+// one buffer of a list: addressable, aligned to its elements
+bool grad_span(const void *p, long long n, int dtype, Span *s)
+{
+    if (!is_dtype(dtype) || !p || !aligned(p, bytes_of(dtype))) return false;
+    s->at = (uintptr_t)p;
+    s->end = s->at + (uintptr_t)n * bytes_of(dtype);
+    return s->end >= s->at;
+}
+
+// does any two of the buffers share a byte?
+bool spans_meet(Span *s, int n)
+{
+    std::sort(s, s + n, [](const Span &a, const Span &b) { return a.at < b.at; });
+    for (int i = 1; i < n; ++i)
+        if (s[i].at < s[i - 1].end) return true;
+    return false;
+}
+
+rr_status check_grads(int tensors, const rr_grad *list, Span *spans)
+{
+    long long total = 0;
+    int n = 0;
+    for (int i = 0; i < tensors; ++i) {
+        const rr_grad &g = list[i];
+        if (g.n < 0 || g.n >= 1ll << 42 || (total += g.n) >= 1ll << 42) return RR_ERR_INVALID_ARG;
+        if (g.n == 0) continue;
+        if (!grad_span(g.src, g.n, g.src_dtype, &spans[n++])) return RR_ERR_INVALID_ARG;
+        if (!g.dst || (g.dst == g.src && g.dst_dtype == g.src_dtype)) continue;
+        if (!grad_span(g.dst, g.n, g.dst_dtype, &spans[n++])) return RR_ERR_INVALID_ARG;
+    }
+    return spans_meet(spans, n) ? RR_ERR_INVALID_ARG : RR_OK;
+}
+
+}  // namespace
+
+rr_status rr_grad_plan_bytes(int tensors, size_t *bytes)
+{
+    if (tensors < 0 || tensors > kMostGrads || !bytes) return RR_ERR_INVALID_ARG;
+    *bytes = rr::grad_plan_size(tensors);
+    return RR_OK;
+}
+
+rr_status rr_grad_plan(int tensors, const rr_grad *list, void *plan, size_t plan_bytes, rr_grad_set *set, void *stream)
+{
+    if (tensors < 0 || tensors > kMostGrads || (tensors && !list) || !plan || !set || !aligned(plan, 16)) return RR_ERR_INVALID_ARG;
+    Span *spans = static_cast<Span *>(malloc(((size_t)tensors * 2 + 1) * sizeof(Span)));
+    if (!spans) return RR_ERR_CUDA;
+    const rr_status rc = check_grads(tensors, list, spans);
+    free(spans);
+    if (rc) return rc;
+    if (rr::grad_plan_size(tensors) > plan_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_grad_plan(tensors, list, plan, set, static_cast<cudaStream_t>(stream));
+}
+
+rr_status rr_clip_workspace_bytes(size_t *bytes)
+{
+    if (!bytes) return RR_ERR_INVALID_ARG;
+    *bytes = rr::clip_workspace();
+    return RR_OK;
+}
+
+rr_status rr_clip_grads(const rr_grad_set *set, float bound, float *norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!set || !set->plan || !aligned(set->plan, 16) || set->tensors < 0 || set->tensors > kMostGrads || set->chunk < 8 || set->chunk % 8 || set->chunks < 0)
+        return RR_ERR_INVALID_ARG;
+    if (!(bound >= 0.0f) || !norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    if (rr::clip_workspace() > workspace_bytes) return RR_ERR_WORKSPACE_TOO_SMALL;
+    return rr::launch_clip_grads(*set, bound, norm, workspace, static_cast<cudaStream_t>(stream));
+}
+
 rr_status rr_check(const void *workspace, void *stream)
 {
     if (!workspace) return RR_ERR_INVALID_ARG;
@@ -628,7 +878,7 @@ const char *rr_status_string(rr_status s)
     case RR_ERR_UNSUPPORTED: return "unsupported request";
     case RR_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
     case RR_ERR_CUDA: return "CUDA call failed";
-    case RR_ERR_NONFINITE: return "non-finite logit";
+    case RR_ERR_NONFINITE: return "non-finite logit or gradient";
     case RR_ERR_TIMEOUT: return "bounded wait ran out on the device";
     case RR_ERR_STATIC_SCRATCH_EXCEEDED: return "shape needs more scratch than the fixed in-library array holds";
     default: return "unknown status";

@@ -1,0 +1,338 @@
+// Clipping by the global norm of many gradients:
+//     norm = sqrt(sum of the squares of all elements of all tensors),  f = min(1, bound / (norm + 1e-6)),  dst = f src
+// in place or into other buffers.  The tensors are cut into chunks of equal length; a first kernel adds up squares, a second takes the
+// factor from the blocks' sums and scales.  The factor needs every element, so gradients that exceed the L2 cache are read twice: both
+// kernels deal the same chunks to the same blocks, the second backwards, so that what was read last is found in the cache.  In place with
+// f = 1 nothing is written.  Squares are added in fp32 eight at a time and these sums in 64 bits in a fixed order, so that neither the length nor the
+// order costs anything; eights whose squares leave the range of fp32 are squared in 64 bits, so finite gradients never overflow or vanish.
+#include "rr_ffn.cuh"
+#include "rr_vec.cuh"
+
+namespace rr {
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kClipThreads = 256;
+constexpr int kClipBlocks = 8;       // an SM, all resident at once
+constexpr int kClipMost = 2048;      // parts in the workspace
+constexpr int kClipUnroll = 4;
+
+struct GradEntry {
+    const void *src;
+    void *dst;           // null: only in the norm
+    long long n;
+    long long first;     // its first chunk; the entry behind the last tensor holds the number of chunks
+    int src_f32, dst_f32;
+    int head;            // elements up to the first that both src and dst hold at a 16-byte boundary; -1: there is none
+    int pad;
+};
+
+constexpr int kPlanEntries = 64;     // written by one launch (3 KB of parameters)
+struct PlanPiece {
+    GradEntry e[kPlanEntries];
+};
+__global__ void k_grad_plan(const __grid_constant__ PlanPiece piece, int count, GradEntry *plan)
+{
+    if ((int)threadIdx.x < count) plan[threadIdx.x] = piece.e[threadIdx.x];
+}
+
+// The chunks of a block: [lo, hi) of all, in tensors that are looked up once and then walked.
+struct Walk {
+    const GradEntry *plan;
+    long long lo, hi;
+};
+__device__ __forceinline__ Walk my_chunks(const GradEntry *plan, long long chunks)
+{
+    return {plan, chunks * blockIdx.x / gridDim.x, chunks * (blockIdx.x + 1) / gridDim.x};
+}
+__device__ __forceinline__ int tensor_of(const GradEntry *plan, int tensors, long long chunk)
+{
+    int lo = 0, hi = tensors - 1;  // the last tensor whose first chunk is not behind it (tensors without chunks lie before one with)
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(&plan[mid].first) <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+__device__ __forceinline__ GradEntry entry(const GradEntry *plan, int i)
+{
+    GradEntry e;
+    const longlong2 *p = reinterpret_cast<const longlong2 *>(plan + i);
+    longlong2 *q = reinterpret_cast<longlong2 *>(&e);
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(GradEntry) / 16; ++j) q[j] = __ldg(p + j);
+    return e;
+}
+static_assert(sizeof(GradEntry) == 48, "read in pieces of 16 bytes");
+
+// Range of chunk `c` of a tensor: elements [lo, hi), of which [body, body + 8 eights) lie at 16-byte boundaries.
+struct Range {
+    long long lo, hi, body;
+    int eights;
+};
+__device__ __forceinline__ Range range_of(const GradEntry &e, long long c, int chunk)
+{
+    Range r;
+    if (e.head < 0) {
+        r.lo = c * chunk;
+        r.hi = min(e.n, r.lo + chunk);
+        r.body = r.hi;
+        r.eights = 0;
+    } else {
+        r.body = min(e.n, e.head + c * chunk);
+        r.lo = c ? r.body : 0;
+        r.hi = min(e.n, e.head + (c + 1) * chunk);
+        r.eights = (int)((r.hi - r.body) >> 3);
+    }
+    return r;
+}
+
+// sum of the squares of eight values
+__device__ __forceinline__ double squares(const float (&v)[8])
+{
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(v[j], v[j], s);
+    // in range: no overflow, and what an underflowing square loses is below 2^-126 / 2^-80 of the sum
+    if (s >= 0x1p-80f && s <= 0x1p120f) return s;
+    double d = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d = fma((double)v[j], (double)v[j], d);
+    return d;
+}
+__device__ __forceinline__ double block_sum(double v, double *buf)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int q = 0; q < kClipThreads / 32; ++q) v += buf[q];
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
+{
+    double sum = 0;
+    const T *p = src + r.body;
+    int i = threadIdx.x;
+    for (; i + (kClipUnroll - 1) * kClipThreads < r.eights; i += kClipUnroll * kClipThreads) {
+        Eight<T, true> e[kClipUnroll];
+#pragma unroll
+        for (int u = 0; u < kClipUnroll; ++u) e[u].template load<kConst>(p + (long long)(i + u * kClipThreads) * 8, 1, 8);
+#pragma unroll
+        for (int u = 0; u < kClipUnroll; ++u) {
+            float v[8];
+            e[u].get(v);
+            sum += squares(v);
+        }
+    }
+    for (; i < r.eights; i += kClipThreads) {
+        Eight<T, true> e;
+        e.template load<kConst>(p + (long long)i * 8, 1, 8);
+        float v[8];
+        e.get(v);
+        sum += squares(v);
+    }
+    for (long long k = r.lo + threadIdx.x; k < r.body; k += 8 * kClipThreads) {  // in front of the body, or all of it
+        Eight<T, false> e;
+        const long long left = r.body - k;
+        e.template load<kConst>(src + k, kClipThreads, (int)(left < 8 * kClipThreads ? left : 8 * kClipThreads));
+        float v[8];
+        e.get(v);
+        sum += squares(v);
+    }
+    const long long k = r.body + 8ll * r.eights + threadIdx.x;
+    if (k < r.hi) {
+        const double v = as_f32(src[k]);
+        sum += v * v;
+    }
+    return sum;
+}
+
+__global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *plan, int tensors, long long chunks, int chunk, double *part)
+{
+    __shared__ double buf[kClipThreads / 32];
+    dependent_start();
+    const Walk w = my_chunks(plan, chunks);
+    double sum = 0;
+    if (w.lo < w.hi) {
+        int i = tensor_of(plan, tensors, w.lo);
+        GradEntry e = entry(plan, i);
+        long long next = __ldg(&plan[i + 1].first);
+        for (long long c = w.lo; c < w.hi; ++c) {
+            while (c >= next) {
+                e = entry(plan, ++i);
+                next = __ldg(&plan[i + 1].first);
+            }
+            const Range r = range_of(e, c - e.first, chunk);
+            sum += e.src_f32 ? chunk_squares(static_cast<const float *>(e.src), r) : chunk_squares(static_cast<const bf16 *>(e.src), r);
+        }
+    }
+    sum = block_sum(sum, buf);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+template <class TS, class TD>
+__device__ __forceinline__ void chunk_scale(const TS *src, TD *dst, const Range &r, float f)
+{
+    auto scaled = [f](float (&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f;
+    };
+    int i = threadIdx.x;
+    for (; i + (kClipUnroll - 1) * kClipThreads < r.eights; i += kClipUnroll * kClipThreads) {
+        Eight<TS, true> e[kClipUnroll];
+#pragma unroll
+        for (int u = 0; u < kClipUnroll; ++u) e[u].load(src + r.body + (long long)(i + u * kClipThreads) * 8, 1, 8);
+#pragma unroll
+        for (int u = 0; u < kClipUnroll; ++u) {
+            float v[8];
+            e[u].get(v);
+            scaled(v);
+            Eight<TD, true> o;
+            o.set(v);
+            o.store(dst + r.body + (long long)(i + u * kClipThreads) * 8, 1, 8);
+        }
+    }
+    for (; i < r.eights; i += kClipThreads) {
+        Eight<TS, true> e;
+        e.load(src + r.body + (long long)i * 8, 1, 8);
+        float v[8];
+        e.get(v);
+        scaled(v);
+        Eight<TD, true> o;
+        o.set(v);
+        o.store(dst + r.body + (long long)i * 8, 1, 8);
+    }
+    for (long long k = r.lo + threadIdx.x; k < r.body; k += 8 * kClipThreads) {
+        Eight<TS, false> e;
+        const long long left = r.body - k;
+        const int here = (int)(left < 8 * kClipThreads ? left : 8 * kClipThreads);
+        e.load(src + k, kClipThreads, here);
+        float v[8];
+        e.get(v);
+        scaled(v);
+        Eight<TD, false> o;
+        o.set(v);
+        o.store(dst + k, kClipThreads, here);
+    }
+    const long long k = r.body + 8ll * r.eights + threadIdx.x;
+    if (k < r.hi) dst[k] = from_f32<TD>(as_f32(src[k]) * f);
+}
+
+__global__ void __launch_bounds__(kClipThreads)
+k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, const double *part, int parts, float bound, float *norm, int *status)
+{
+    __shared__ double buf[kClipThreads / 32];
+    dependent_start();
+    double sum = 0;
+    for (int i = threadIdx.x; i < parts; i += kClipThreads) sum += __ldg(part + i);
+    sum = block_sum(sum, buf);
+    const double root = sqrt(sum);
+    const bool finite = isfinite(sum);
+    // (gradients that are not finite are left as they are)
+    const float f = finite ? (float)fmin(1.0, (double)bound / (root + 1e-6)) : 1.0f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        norm[0] = (float)root;
+        norm[1] = f;
+        if (!finite) latch_status(status, RR_ERR_NONFINITE);
+    }
+    const Walk w = my_chunks(plan, chunks);
+    if (w.lo >= w.hi) return;
+    int i = tensor_of(plan, tensors, w.hi - 1);
+    GradEntry e = entry(plan, i);
+    for (long long c = w.hi - 1; c >= w.lo; --c) {
+        while (c < e.first) e = entry(plan, --i);
+        if (!e.dst || (e.dst == e.src && f == 1.0f)) continue;
+        const Range r = range_of(e, c - e.first, chunk);
+        if (e.src_f32) {
+            if (e.dst_f32) chunk_scale(static_cast<const float *>(e.src), static_cast<float *>(e.dst), r, f);
+            else chunk_scale(static_cast<const float *>(e.src), static_cast<bf16 *>(e.dst), r, f);
+        } else {
+            if (e.dst_f32) chunk_scale(static_cast<const bf16 *>(e.src), static_cast<float *>(e.dst), r, f);
+            else chunk_scale(static_cast<const bf16 *>(e.src), static_cast<bf16 *>(e.dst), r, f);
+        }
+    }
+}
+
+int size_of(int dtype) { return dtype == RR_F32 ? 4 : 2; }
+
+// elements up to the first at which both addresses are multiples of 16 bytes, -1 if there is none
+int common_head(const rr_grad &g)
+{
+    const uintptr_t s = (uintptr_t)g.src, d = g.dst ? (uintptr_t)g.dst : s;
+    const int ss = size_of(g.src_dtype), ds = g.dst ? size_of(g.dst_dtype) : ss;
+    for (int h = 0; h < 8; ++h)
+        if ((s + (uintptr_t)h * ss) % 16 == 0 && (d + (uintptr_t)h * ds) % 16 == 0) return h;
+    return -1;
+}
+
+}  // namespace
+
+size_t grad_plan_size(int tensors) { return ((size_t)tensors + 1) * sizeof(GradEntry); }
+size_t clip_workspace() { return kHeaderBytes + kClipMost * sizeof(double); }
+
+rr_status launch_grad_plan(int tensors, const rr_grad *list, void *plan, rr_grad_set *set, cudaStream_t st)
+{
+    const int sms = device_sm_count();
+    if (sms < 1) return RR_ERR_CUDA;
+    // Chunks: 8192 elements, fewer where that would leave SMs without one.
+    long long total = 0;
+    for (int i = 0; i < tensors; ++i) total += list[i].n;
+    int chunk = kClipThreads * 8 * kClipUnroll;
+    while (chunk > kClipThreads * 8 && total / chunk < 4ll * sms) chunk >>= 1;
+    long long first = 0;
+    PlanPiece piece;
+    GradEntry *out = static_cast<GradEntry *>(plan);
+    for (int i = 0, k = 0; i <= tensors; ++i) {
+        GradEntry &e = piece.e[k];
+        e = GradEntry{};
+        e.first = first;
+        if (i < tensors) {
+            const rr_grad &g = list[i];
+            e.src = g.src;
+            e.dst = g.dst;
+            e.n = g.n;
+            e.src_f32 = g.src_dtype == RR_F32;
+            e.dst_f32 = g.dst_dtype == RR_F32;
+            e.head = common_head(g);
+            const long long body = e.head < 0 ? g.n : g.n > e.head ? g.n - e.head : 0;
+            first += g.n == 0 ? 0 : body == 0 ? 1 : (body + chunk - 1) / chunk;
+        }
+        if (++k == kPlanEntries || i == tensors) {
+            k_grad_plan<<<1, kPlanEntries, 0, st>>>(piece, k, out);
+            if (cudaGetLastError() != cudaSuccess) return RR_ERR_CUDA;
+            out += k;
+            k = 0;
+        }
+    }
+    set->plan = plan;
+    set->tensors = tensors;
+    set->chunk = chunk;
+    set->chunks = first;
+    return RR_OK;
+}
+
+rr_status launch_clip_grads(const rr_grad_set &set, float bound, float *norm, void *ws, cudaStream_t st)
+{
+    const int sms = device_sm_count();
+    if (sms < 1) return RR_ERR_CUDA;
+    const GradEntry *plan = static_cast<const GradEntry *>(set.plan);
+    double *part = reinterpret_cast<double *>(static_cast<char *>(ws) + kHeaderBytes);
+    long long most = (long long)sms * kClipBlocks;
+    if (most > kClipMost) most = kClipMost;
+    const int grid = set.chunks < 1 ? 1 : (int)(set.chunks < most ? set.chunks : most);
+    cudaError_t err = launch_dependent(k_grad_squares, dim3(grid), kClipThreads, 0, 1, st, plan, (int)set.tensors, (long long)set.chunks, (int)set.chunk, part);
+    if (err == cudaSuccess)
+        err = launch_dependent(k_grad_scale, dim3(grid), kClipThreads, 0, 1, st, plan, (int)set.tensors, (long long)set.chunks, (int)set.chunk, (const double *)part,
+                               grid, bound, norm, static_cast<int *>(ws));
+    return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+}
+
+}  // namespace rr

@@ -81,4 +81,18 @@ rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float
 rr_status launch_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
                              const uint8_t *live, float coef_b, float coef_z, int accumulate, float *dlogits, cudaStream_t st);
 
+// Norm (rr_norm.cu), embedding (rr_embed.cu), clip (rr_clip.cu); the shapes' pitches are filled in
+size_t norm_workspace(int M, int N);
+rr_status launch_norm_fwd(const rr_norm_shape &s, const void *x, const void *residual, const void *w, const void *b, void *h, void *y, float *mean,
+                          float *rstd, cudaStream_t st);
+rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h, const void *w, const float *mean, const float *rstd, const void *dh,
+                          void *dx, float *dw, float *db, void *workspace, cudaStream_t st);
+size_t embed_bwd_workspace(long long n, int d);
+rr_status launch_embed_fwd(const rr_embed_shape &s, const void *ids, const void *table, void *y, void *ws, cudaStream_t st);
+rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void *dy, void *dtable, void *ws, cudaStream_t st);
+size_t grad_plan_size(int tensors);
+size_t clip_workspace();
+rr_status launch_grad_plan(int tensors, const rr_grad *list, void *plan, rr_grad_set *set, cudaStream_t st);
+rr_status launch_clip_grads(const rr_grad_set &set, float bound, float *norm, void *ws, cudaStream_t st);
+
 }  // namespace rr
