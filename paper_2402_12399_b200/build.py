@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librr.so")
 SOURCES = ["rr_api.cu", "rr_route.cu", "rr_route_fused.cu", "rr_route_noalloc.cu", "rr_ffn.cu", "rr_bwd.cu", "rr_gate.cu", "rr_aux.cu", "rr_dropout.cu",
-           "rr_linear.cu", "rr_balance.cu", "rr_norm.cu", "rr_embed.cu", "rr_clip.cu"]
+           "rr_linear.cu", "rr_balance.cu", "rr_norm_fwd.cu", "rr_norm_bwd.cu", "rr_embed.cu", "rr_clip.cu"]
 
 
 def _newest_source() -> float:

@@ -15,7 +15,7 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kClipThreads = 256;
-constexpr int kClipBlocks = 8;       // an SM, all resident at once
+constexpr int kClipBlocks = 4;       // an SM, all resident at once (64 registers a thread)
 constexpr int kClipMost = 2048;      // parts in the workspace
 constexpr int kClipUnroll = 4;
 
@@ -38,25 +38,6 @@ __global__ void k_grad_plan(const __grid_constant__ PlanPiece piece, int count, 
     if ((int)threadIdx.x < count) plan[threadIdx.x] = piece.e[threadIdx.x];
 }
 
-// The chunks of a block: [lo, hi) of all, in tensors that are looked up once and then walked.
-struct Walk {
-    const GradEntry *plan;
-    long long lo, hi;
-};
-__device__ __forceinline__ Walk my_chunks(const GradEntry *plan, long long chunks)
-{
-    return {plan, chunks * blockIdx.x / gridDim.x, chunks * (blockIdx.x + 1) / gridDim.x};
-}
-__device__ __forceinline__ int tensor_of(const GradEntry *plan, int tensors, long long chunk)
-{
-    int lo = 0, hi = tensors - 1;  // the last tensor whose first chunk is not behind it (tensors without chunks lie before one with)
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(&plan[mid].first) <= chunk) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
 __device__ __forceinline__ GradEntry entry(const GradEntry *plan, int i)
 {
     GradEntry e;
@@ -67,6 +48,25 @@ __device__ __forceinline__ GradEntry entry(const GradEntry *plan, int i)
     return e;
 }
 static_assert(sizeof(GradEntry) == 48, "read in pieces of 16 bytes");
+
+// Block b takes the chunks b, b + gridDim, ... (all blocks sweep the memory together).  The tensor of a chunk is looked up by the whole
+// block at once: one round of loads for up to 256 tensors, two for 65536.
+struct Place {
+    GradEntry e;
+    long long end;  // first chunk behind the tensor
+};
+__device__ __forceinline__ void seek(Place &p, const GradEntry *plan, int tensors, long long chunk)
+{
+    int lo = 0, len = tensors;  // the last tensor whose first chunk is not behind this one (those without a chunk lie before one with)
+    while (len > 1) {
+        const int stride = (len + kClipThreads - 1) / kClipThreads, at = (int)threadIdx.x * stride;
+        const int count = __syncthreads_count(at < len && __ldg(&plan[lo + at].first) <= chunk) - 1;  // (the first of the range always is)
+        lo += count * stride;
+        len = min(stride, len - count * stride);
+    }
+    p.e = entry(plan, lo);
+    p.end = __ldg(&plan[lo + 1].first);
+}
 
 // Range of chunk `c` of a tensor: elements [lo, hi), of which [body, body + 8 eights) lie at 16-byte boundaries.
 struct Range {
@@ -90,17 +90,18 @@ __device__ __forceinline__ Range range_of(const GradEntry &e, long long c, int c
     return r;
 }
 
-// sum of the squares of eight values
-__device__ __forceinline__ double squares(const float (&v)[8])
+// sum of the squares of kN values
+template <int kN>
+__device__ __forceinline__ double squares(const float (&v)[kN])
 {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(v[j], v[j], s);
+    for (int j = 0; j < kN; ++j) s = fmaf(v[j], v[j], s);
     // in range: no overflow, and what an underflowing square loses is below 2^-126 / 2^-80 of the sum
     if (s >= 0x1p-80f && s <= 0x1p120f) return s;
     double d = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) d = fma((double)v[j], (double)v[j], d);
+    for (int j = 0; j < kN; ++j) d = fma((double)v[j], (double)v[j], d);
     return d;
 }
 __device__ __forceinline__ double block_sum(double v, double *buf)
@@ -115,64 +116,62 @@ __device__ __forceinline__ double block_sum(double v, double *buf)
     return v;
 }
 
+// f(k) for every element k of the range that the body leaves over, in front of it (all of a tensor without common boundaries) and behind it
+template <class F>
+__device__ __forceinline__ void edges(const Range &r, F f)
+{
+    for (long long k = r.lo + threadIdx.x; k < r.body; k += kClipThreads) f(k);
+    const long long k = r.body + 8ll * r.eights + threadIdx.x;
+    if (k < r.hi) f(k);
+}
+
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
 {
-    double sum = 0;
+    constexpr int kN = 16 / sizeof(T), kAtOnce = 2 * kClipUnroll;  // 16 bytes, and how many of them a thread has in flight
+    const int units = r.eights * (8 / kN);
     const T *p = src + r.body;
+    double sum = 0;
     int i = threadIdx.x;
-    for (; i + (kClipUnroll - 1) * kClipThreads < r.eights; i += kClipUnroll * kClipThreads) {
-        Eight<T, true> e[kClipUnroll];
+    for (; i + (kAtOnce - 1) * kClipThreads < units; i += kAtOnce * kClipThreads) {
+        Unit<T, kN> e[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kClipUnroll; ++u) e[u].template load<kConst>(p + (long long)(i + u * kClipThreads) * 8, 1, 8);
+        for (int u = 0; u < kAtOnce; ++u) e[u].template load<kConst>(p + (long long)(i + u * kClipThreads) * kN);
 #pragma unroll
-        for (int u = 0; u < kClipUnroll; ++u) {
+        for (int u = 0; u < kAtOnce; u += 8 / kN) {  // eight values at a time
             float v[8];
-            e[u].get(v);
-            sum += squares(v);
+#pragma unroll
+            for (int k = 0; k < 8 / kN; ++k) e[u + k].get(reinterpret_cast<float(&)[kN]>(v[k * kN]));
+            sum += squares<8>(v);
         }
     }
-    for (; i < r.eights; i += kClipThreads) {
-        Eight<T, true> e;
-        e.template load<kConst>(p + (long long)i * 8, 1, 8);
-        float v[8];
+    for (; i < units; i += kClipThreads) {
+        Unit<T, kN> e;
+        e.template load<kConst>(p + (long long)i * kN);
+        float v[kN];
         e.get(v);
-        sum += squares(v);
+        sum += squares<kN>(v);
     }
-    for (long long k = r.lo + threadIdx.x; k < r.body; k += 8 * kClipThreads) {  // in front of the body, or all of it
-        Eight<T, false> e;
-        const long long left = r.body - k;
-        e.template load<kConst>(src + k, kClipThreads, (int)(left < 8 * kClipThreads ? left : 8 * kClipThreads));
-        float v[8];
-        e.get(v);
-        sum += squares(v);
-    }
-    const long long k = r.body + 8ll * r.eights + threadIdx.x;
-    if (k < r.hi) {
+    edges(r, [&](long long k) {
         const double v = as_f32(src[k]);
         sum += v * v;
-    }
+    });
     return sum;
 }
 
+// The next kernel may be made ready once this one has seen the plan, so that it can read it without waiting for the sums.
 __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *plan, int tensors, long long chunks, int chunk, double *part)
 {
     __shared__ double buf[kClipThreads / 32];
-    dependent_start();
-    const Walk w = my_chunks(plan, chunks);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double sum = 0;
-    if (w.lo < w.hi) {
-        int i = tensor_of(plan, tensors, w.lo);
-        GradEntry e = entry(plan, i);
-        long long next = __ldg(&plan[i + 1].first);
-        for (long long c = w.lo; c < w.hi; ++c) {
-            while (c >= next) {
-                e = entry(plan, ++i);
-                next = __ldg(&plan[i + 1].first);
-            }
-            const Range r = range_of(e, c - e.first, chunk);
-            sum += e.src_f32 ? chunk_squares(static_cast<const float *>(e.src), r) : chunk_squares(static_cast<const bf16 *>(e.src), r);
-        }
+    Place p;
+    p.end = 0;
+    for (long long c = blockIdx.x; c < chunks; c += gridDim.x) {
+        if (c >= p.end) seek(p, plan, tensors, c);
+        const Range r = range_of(p.e, c - p.e.first, chunk);
+        sum += p.e.src_f32 ? chunk_squares(static_cast<const float *>(p.e.src), r) : chunk_squares(static_cast<const bf16 *>(p.e.src), r);
     }
     sum = block_sum(sum, buf);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -181,56 +180,41 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *
 template <class TS, class TD>
 __device__ __forceinline__ void chunk_scale(const TS *src, TD *dst, const Range &r, float f)
 {
-    auto scaled = [f](float (&v)[8]) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= f;
-    };
+    constexpr int kN = sizeof(TS) + sizeof(TD) == 4 ? 8 : 4, kAtOnce = kClipUnroll * 8 / kN;
+    const int units = r.eights * (8 / kN);
+    const TS *p = src + r.body;
+    TD *q = dst + r.body;
     int i = threadIdx.x;
-    for (; i + (kClipUnroll - 1) * kClipThreads < r.eights; i += kClipUnroll * kClipThreads) {
-        Eight<TS, true> e[kClipUnroll];
+    for (; i + (kAtOnce - 1) * kClipThreads < units; i += kAtOnce * kClipThreads) {
+        Unit<TS, kN> e[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kClipUnroll; ++u) e[u].load(src + r.body + (long long)(i + u * kClipThreads) * 8, 1, 8);
+        for (int u = 0; u < kAtOnce; ++u) e[u].template load<kStream>(p + (long long)(i + u * kClipThreads) * kN);
 #pragma unroll
-        for (int u = 0; u < kClipUnroll; ++u) {
-            float v[8];
-            e[u].get(v);
-            scaled(v);
-            Eight<TD, true> o;
-            o.set(v);
-            o.store(dst + r.body + (long long)(i + u * kClipThreads) * 8, 1, 8);
+        for (int u = 0; u < kAtOnce; ++u) {
+            Unit<TD, kN> o;
+            scaled<kN>(e[u], o, f);
+            o.template store<kStream>(q + (long long)(i + u * kClipThreads) * kN);
         }
     }
-    for (; i < r.eights; i += kClipThreads) {
-        Eight<TS, true> e;
-        e.load(src + r.body + (long long)i * 8, 1, 8);
-        float v[8];
-        e.get(v);
-        scaled(v);
-        Eight<TD, true> o;
-        o.set(v);
-        o.store(dst + r.body + (long long)i * 8, 1, 8);
+    for (; i < units; i += kClipThreads) {
+        Unit<TS, kN> e;
+        Unit<TD, kN> o;
+        e.template load<kStream>(p + (long long)i * kN);
+        scaled<kN>(e, o, f);
+        o.template store<kStream>(q + (long long)i * kN);
     }
-    for (long long k = r.lo + threadIdx.x; k < r.body; k += 8 * kClipThreads) {
-        Eight<TS, false> e;
-        const long long left = r.body - k;
-        const int here = (int)(left < 8 * kClipThreads ? left : 8 * kClipThreads);
-        e.load(src + k, kClipThreads, here);
-        float v[8];
-        e.get(v);
-        scaled(v);
-        Eight<TD, false> o;
-        o.set(v);
-        o.store(dst + k, kClipThreads, here);
-    }
-    const long long k = r.body + 8ll * r.eights + threadIdx.x;
-    if (k < r.hi) dst[k] = from_f32<TD>(as_f32(src[k]) * f);
+    edges(r, [&](long long k) { dst[k] = from_f32<TD>(as_f32(src[k]) * f); });
 }
 
 __global__ void __launch_bounds__(kClipThreads)
 k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, const double *part, int parts, float bound, float *norm, int *status)
 {
     __shared__ double buf[kClipThreads / 32];
-    dependent_start();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    long long c = chunks > blockIdx.x ? blockIdx.x + (chunks - 1 - blockIdx.x) / gridDim.x * gridDim.x : -1;  // the last chunk of the block
+    Place p;
+    if (c >= 0) seek(p, plan, tensors, c);  // (the plan is older than the sums: see above)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0;
     for (int i = threadIdx.x; i < parts; i += kClipThreads) sum += __ldg(part + i);
     sum = block_sum(sum, buf);
@@ -243,12 +227,9 @@ k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, co
         norm[1] = f;
         if (!finite) latch_status(status, RR_ERR_NONFINITE);
     }
-    const Walk w = my_chunks(plan, chunks);
-    if (w.lo >= w.hi) return;
-    int i = tensor_of(plan, tensors, w.hi - 1);
-    GradEntry e = entry(plan, i);
-    for (long long c = w.hi - 1; c >= w.lo; --c) {
-        while (c < e.first) e = entry(plan, --i);
+    for (; c >= 0; c -= gridDim.x) {
+        if (c < p.e.first) seek(p, plan, tensors, c);
+        const GradEntry &e = p.e;
         if (!e.dst || (e.dst == e.src && f == 1.0f)) continue;
         const Range r = range_of(e, c - e.first, chunk);
         if (e.src_f32) {

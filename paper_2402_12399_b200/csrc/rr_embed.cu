@@ -39,11 +39,11 @@ __device__ __forceinline__ int token_id(const EmbArgs &a, long long i)
     return -1;
 }
 
-// A block takes tiles of kTile eights of the result, whatever the width of a row; row and place of each come from one division per
-// tile and a product per eight.
+// A block takes tiles of kTile units of the result (kN elements each), whatever the width of a row; row and place of a unit come from a
+// product, and those of the next tile from those of the last.
 constexpr int kEmbUnroll = 4;
-template <class TX, class TY, bool kVec>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int per_row /* eights, or elements */, unsigned long long magic, long long row_step, unsigned at_step)
+template <class TX, class TY, int kN>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int per_row, unsigned long long magic, long long row_step, unsigned at_step)
 {
     constexpr int kTile = kEmbThreads * kEmbUnroll;
     dependent_start();
@@ -62,32 +62,19 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
             at[u] = w - q * per_row;
             id[u] = tile + l < total ? token_id(a, row[u]) : -2;
         }
-        if constexpr (kVec) {
-            Eight<TX, true> e[kEmbUnroll];
+        Unit<TX, kN> e[kEmbUnroll];
 #pragma unroll
-            for (int u = 0; u < kEmbUnroll; ++u) {
-                e[u].zero();
-                if (id[u] >= 0) e[u].template load<kKeep>(static_cast<const TX *>(a.in) + (long long)id[u] * a.d + at[u] * 8, 1, 8);
-            }
+        for (int u = 0; u < kEmbUnroll; ++u) {
+            e[u].raw = {};
+            if (id[u] >= 0) e[u].template load<kKeep>(static_cast<const TX *>(a.in) + (long long)id[u] * a.d + (long long)at[u] * kN);
+        }
 #pragma unroll
-            for (int u = 0; u < kEmbUnroll; ++u) {
-                if (id[u] == -2) continue;
-                float v[8];
-                e[u].get(v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = id[u] < 0 ? 0.f : v[j] * a.scale;
-                Eight<TY, true> o;
-                o.set(v);
-                o.store(static_cast<TY *>(a.out) + row[u] * a.ld + at[u] * 8, 1, 8);
-            }
-        } else {
-            TX e[kEmbUnroll];
-#pragma unroll
-            for (int u = 0; u < kEmbUnroll; ++u)
-                if (id[u] >= 0) e[u] = static_cast<const TX *>(a.in)[(long long)id[u] * a.d + at[u]];
-#pragma unroll
-            for (int u = 0; u < kEmbUnroll; ++u)
-                if (id[u] != -2) place<kStream>(static_cast<TY *>(a.out) + row[u] * a.ld + at[u], from_f32<TY>(id[u] < 0 ? 0.f : as_f32(e[u]) * a.scale));
+        for (int u = 0; u < kEmbUnroll; ++u) {
+            if (id[u] == -2) continue;
+            Unit<TY, kN> o;
+            scaled<kN>(e[u], o, a.scale);
+            if (id[u] < 0) o.raw = {};  // (not -0)
+            o.template store<kStream>(static_cast<TY *>(a.out) + row[u] * a.ld + (long long)at[u] * kN);
         }
         row0 += row_step;  // gridDim tiles on
         at0 += at_step;
@@ -101,7 +88,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
 // ---- backward: the sort -------------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits; // at most
 constexpr int kSortMost = 16;                            // tokens a thread of a sorting block holds
 constexpr int kSlab = kSortThreads * kSortMost;          // tokens of a sorting block
 constexpr int kMapWords = 8192;                          // bitmap of a zeroing block: 2^18 rows at a time
@@ -109,61 +96,64 @@ constexpr int kMapWords = 8192;                          // bitmap of a zeroing 
 struct SortArgs {
     EmbArgs e;
     int slabs, slab;       // sorting blocks and tokens of each (the last may have fewer)
-    int passes;
+    int passes, bits;      // digits, and bits of each
     int *key, *pos;        // [n] sorted ids (V: no id) and their tokens, slab by slab
-    int fill;              // rows without a token are zeroed
+    int *runs;             // counter of the long runs (k_embed_sum), set to zero here
     int out_f32;
 };
 
-// zeros in `bytes` (512 or more) bytes at p: an even number at an even address
-__device__ __forceinline__ void zero_bytes(char *p, long long bytes, int lane)
-{
-    const int head = (int)(-(uintptr_t)p & 15), tail = (int)((bytes - head) & 15);
-    if (2 * lane < head) *reinterpret_cast<uint16_t *>(p + 2 * lane) = 0;
-    if (2 * lane < tail) *reinterpret_cast<uint16_t *>(p + bytes - tail + 2 * lane) = 0;
-    uint4 *q = reinterpret_cast<uint4 *>(p + head);
-    for (long long i = lane; i < (bytes - head) / 16; i += 32) __stcs(q + i, make_uint4(0u, 0u, 0u, 0u));
-}
-
-// Rows of this zeroing block that no token names.  A warp zeroes a row at a time; rows shorter than 512 bytes, which would leave lanes idle,
-// are shared out by elements.
+// Rows of this zeroing block that no token names.  `lanes` lanes of a warp zero a row, as many as it has 16-byte pieces.
 __device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *map)
 {
     const long long V = a.e.V, lo = V * block / blocks, hi = V * (block + 1) / blocks;
-    const int es = a.out_f32 ? 4 : 2;
-    const long long width = (long long)a.e.d * es;
-    char *out = static_cast<char *>(a.e.out);
+    const long long width = (long long)a.e.d * (a.out_f32 ? 4 : 2);
+    int lanes = 1;
+    while (lanes < 32 && lanes * 16 < width) lanes <<= 1;
+    const int lane = threadIdx.x & (lanes - 1), step = kSortThreads / lanes;
+    constexpr int kAtOnce = 16;
     for (long long r0 = lo; r0 < hi; r0 += kMapWords * 32) {
         const long long r1 = min(hi, r0 + kMapWords * 32);
         const int words = (int)((r1 - r0 + 31) / 32);
         __syncthreads();
         for (int i = threadIdx.x; i < words; i += kSortThreads) map[i] = 0;
         __syncthreads();
-#pragma unroll 4
-        for (long long i = threadIdx.x; i < a.e.n; i += kSortThreads) {
-            const int id = token_id(a.e, i);
-            if (id >= r0 && id < r1) atomicOr(&map[(id - r0) >> 5], 1u << ((id - r0) & 31));
+        for (long long i0 = threadIdx.x; i0 < a.e.n; i0 += kAtOnce * kSortThreads) {
+            int id[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) id[u] = i0 + u * kSortThreads < a.e.n ? token_id(a.e, i0 + u * kSortThreads) : -1;
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+                if (id[u] >= r0 && id[u] < r1) atomicOr(&map[(id[u] - r0) >> 5], 1u << ((id[u] - r0) & 31));
         }
         __syncthreads();
-        if (width >= 512) {
-            for (long long r = r0 + (threadIdx.x >> 5); r < r1; r += kSortWarps)
-                if (!(map[(r - r0) >> 5] >> ((r - r0) & 31) & 1)) zero_bytes(out + r * width, width, threadIdx.x & 31);
-        } else {
-            const int d = a.e.d;
-            const long long elements = (r1 - r0) * d;
-            for (long long i = threadIdx.x; i < elements; i += kSortThreads) {
-                const int r = (int)(i / d);
-                if (map[r >> 5] >> (r & 31) & 1) continue;
-                if (es == 4) reinterpret_cast<float *>(out)[r0 * d + i] = 0.f;
-                else reinterpret_cast<uint16_t *>(out)[r0 * d + i] = 0;
-            }
+        for (long long r = r0 + threadIdx.x / lanes; r < r1; r += step) {
+            if (map[(r - r0) >> 5] >> ((r - r0) & 31) & 1) continue;
+            char *p = static_cast<char *>(a.e.out) + r * width;  // (an even address, an even number of bytes)
+            const int head = (int)min(width, (long long)(-(uintptr_t)p & 15)), tail = (int)((width - head) & 15);
+            for (int i = 2 * lane; i < head; i += 2 * lanes) *reinterpret_cast<uint16_t *>(p + i) = 0;
+            for (int i = 2 * lane; i < tail; i += 2 * lanes) *reinterpret_cast<uint16_t *>(p + width - tail + i) = 0;
+            uint4 *q = reinterpret_cast<uint4 *>(p + head);
+            for (long long i = lane; i < (width - head) / 16; i += lanes) __stcs(q + i, make_uint4(0u, 0u, 0u, 0u));
         }
     }
 }
 
-// Stable sort of a slab by id, least significant digit first.  A thread holds K consecutive-by-warp tokens (token w*32*K + k*32 + lane of
-// the slab): in a pass every warp counts its tokens digit by digit in its own column of the table (`__match_any_sync` gives a token its
-// place among the equal digits of its warp), the table is scanned digit by digit and warp by warp, and the tokens move in shared memory.
+// lanes of the warp with the same digit (`bits` bits) as this one
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits)
+{
+    uint32_t same = 0xffffffffu;
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+        if (b >= bits) break;
+        const uint32_t with = __ballot_sync(0xffffffffu, digit >> b & 1);
+        same &= digit >> b & 1 ? with : ~with;
+    }
+    return same;
+}
+
+// Stable sort of a slab by id, least significant digit first.  A thread holds K tokens (token w 32 K + k 32 + lane of the slab): in a
+// pass every warp counts its tokens digit by digit in its own column of a table, which gives a token its place among the equal digits of the
+// warp; the table is scanned digit by digit and warp by warp, and the tokens move in shared memory.
 // Blocks behind the sorting ones zero the rows that nobody names.
 template <int K>
 __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
@@ -174,15 +164,17 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
         zero_rows(a, blockIdx.x - a.slabs, gridDim.x - a.slabs, shared);
         return;
     }
-    uint32_t *const count = shared;                        // [kDigits][kSortWarps + 1]
-    uint32_t *const sk = count + kDigits * (kSortWarps + 1);  // [1024 K]
+    constexpr int kRow = kSortWarps + 1;                   // (a column of the table in every bank)
+    uint32_t *const count = shared;                        // [kDigits][kRow]
+    uint32_t *const total = count + kDigits * kRow;        // [kDigits] tokens of a digit, then those of lower ones
+    uint32_t *const sk = total + kDigits;                  // [1024 K]
     uint16_t *const sp = reinterpret_cast<uint16_t *>(sk + kSortThreads * K);
     __shared__ uint32_t warp_total[kSortWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, digits = 1 << a.bits;
     const long long base = (long long)blockIdx.x * a.slab;
     const int n = (int)min((long long)a.slab, a.e.n - base);
-    uint32_t key[K];
-    uint32_t pos[K];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.runs = 0;
+    uint32_t key[K], pos[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int i = warp * 32 * K + k * 32 + lane;
@@ -192,15 +184,14 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
         pos[k] = i;
     }
     for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * kDigitBits;
-        for (int i = threadIdx.x; i < kDigits * (kSortWarps + 1); i += kSortThreads) count[i] = 0;
+        const int shift = pass * a.bits;
+        for (int i = threadIdx.x; i < digits * kRow; i += kSortThreads) count[i] = 0;
         __syncthreads();
         uint32_t rank[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const uint32_t digit = key[k] >> shift & (kDigits - 1);
-            const uint32_t same = __match_any_sync(0xffffffffu, digit), below = same & ((1u << lane) - 1);
-            uint32_t *c = &count[digit * (kSortWarps + 1) + warp];
+            const uint32_t digit = key[k] >> shift & (digits - 1), same = same_digit(digit, a.bits), below = same & ((1u << lane) - 1);
+            uint32_t *c = &count[digit * kRow + warp];
             const uint32_t before = *c;
             __syncwarp();
             if (below == 0) *c = before + __popc(same);
@@ -208,32 +199,37 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
             rank[k] = before + __popc(below);
         }
         __syncthreads();
-        // exclusive scan over (digit, warp): thread t owns eight warps of digit t / 4
-        uint32_t v[8], sum = 0;
-        uint32_t *c = &count[(threadIdx.x >> 2) * (kSortWarps + 1) + (threadIdx.x & 3) * 8];
+        for (int d = warp; d < digits; d += kSortWarps) {  // a digit's tokens in the warps before
+            const uint32_t own = count[d * kRow + lane];
+            uint32_t sum = own;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = sum;
-            sum += c[j];
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += up;
+            }
+            count[d * kRow + lane] = sum - own;
+            if (lane == 31) total[d] = sum;
         }
-        uint32_t inclusive = sum;
+        __syncthreads();
+        uint32_t own = 0, sum = 0;  // lower digits' tokens
+        if ((int)threadIdx.x < digits) sum = own = total[threadIdx.x];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t up = __shfl_up_sync(0xffffffffu, inclusive, o);
-            if (lane >= o) inclusive += up;
+            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
         }
-        if (lane == 31) warp_total[warp] = inclusive;
+        if (lane == 31) warp_total[warp] = sum;
         __syncthreads();
-        uint32_t before = lane < warp ? warp_total[lane] : 0;
+        if (warp < digits / 32 || warp == 0) {
+            uint32_t before = lane < warp ? warp_total[lane] : 0;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-        before += inclusive - sum;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = before + v[j];
+            for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+            if ((int)threadIdx.x < digits) total[threadIdx.x] = before + sum - own;
+        }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const uint32_t to = rank[k] + count[(key[k] >> shift & (kDigits - 1)) * (kSortWarps + 1) + warp];
+            const uint32_t digit = key[k] >> shift & (digits - 1), to = rank[k] + total[digit] + count[digit * kRow + warp];
             sk[to] = key[k];
             sp[to] = (uint16_t)pos[k];
         }
@@ -244,7 +240,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
             key[k] = sk[i];
             pos[k] = sp[i];
         }
-        // (the next pass writes to sk and sp behind two barriers)
+        // (the next pass writes to sk and sp behind further barriers)
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -257,156 +253,204 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
 }
 
 // Sorted slabs into one order: a token's place is the number of tokens in front of it in every slab (equal ids: earlier slabs only).
+// Four slabs are searched side by side.
 __global__ void __launch_bounds__(kEmbThreads) k_embed_merge(long long n, int slabs, int slab, const int *__restrict__ key, const int *__restrict__ pos, int *out_key,
                                                              int *out_pos)
 {
+    constexpr int kSide = 4;
     dependent_start();
     const long long i = (long long)blockIdx.x * kEmbThreads + threadIdx.x;
     if (i >= n) return;
     const int mine = (int)(i / slab), id = __ldg(key + i);
+    const int token = __ldg(pos + i);
     long long to = i - (long long)mine * slab;
-    for (int s = 0; s < slabs; ++s) {
-        if (s == mine) continue;
-        const long long base = (long long)s * slab;
-        int lo = 0, hi = (int)min((long long)slab, n - base);
-        while (lo < hi) {  // tokens of slab s below id, or in earlier slabs not above it
-            const int mid = (lo + hi) >> 1, k = __ldg(key + base + mid);
-            if (k < id || (k == id && s < mine)) lo = mid + 1;
-            else hi = mid;
+    int steps = 1;
+    while (1 << steps <= slab) ++steps;
+    for (int s0 = 0; s0 < slabs; s0 += kSide) {
+        int lo[kSide], hi[kSide];
+#pragma unroll
+        for (int u = 0; u < kSide; ++u) {
+            const int s = s0 + u;
+            lo[u] = 0;
+            hi[u] = s < slabs && s != mine ? (int)min((long long)slab, n - (long long)s * slab) : 0;
         }
-        to += lo;
+        for (int step = 0; step < steps; ++step) {
+#pragma unroll
+            for (int u = 0; u < kSide; ++u) {  // tokens of slab s below id, or in earlier slabs not above it
+                if (lo[u] >= hi[u]) continue;
+                const int mid = (lo[u] + hi[u]) >> 1, k = __ldg(key + (long long)(s0 + u) * slab + mid);
+                if (k < id || (k == id && s0 + u < mine)) lo[u] = mid + 1;
+                else hi[u] = mid;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSide; ++u) to += lo[u];
     }
     out_key[to] = id;
-    out_pos[to] = __ldg(pos + i);
+    out_pos[to] = token;
 }
 
 // ---- backward: the sums -------------------------------------------------------------------------------------------
+// A run is all the tokens of one id.  A block takes a chunk of sorted tokens, and of the runs that begin in it those of up to kLong tokens
+// to their end: most runs are short, and need no second look.  Of a longer run every chunk adds up its own piece (the first piece is part 1
+// of its chunk, every other the part 0), and k_embed_join adds up the pieces in order.
 struct SumArgs {
     EmbArgs e;
     const int *key, *pos;  // [n] sorted
-    float *part;           // [chunks][2][d]: the first and the last run of a chunk where they go on beyond it
-    long long chunks;
+    float *part;           // [chunks][2][d]
+    int *runs, *list;      // long runs: how many, and the chunks in which they begin (in any order)
     int add;
 };
 
-constexpr int kChunk = 32;    // sorted tokens of a chunk
-constexpr int kAhead = 8;     // rows in flight
+constexpr int kChunk = 32;             // sorted tokens of a chunk
+constexpr int kLong = 64;
+constexpr int kReach = kChunk + kLong; // tokens that a block may have to look at from the start of its chunk on
+constexpr int kAhead = 8;              // rows in flight
 
-template <class TO, bool kVec>
-__device__ __forceinline__ void write_row(const SumArgs &a, int id, int at, int step, float (&v)[8])
+template <class TO, Layout L>
+__device__ __forceinline__ void write_row(const SumArgs &a, int id, int at, int step, f32x2 (&v)[4])
 {
     TO *p = static_cast<TO *>(a.e.out) + (long long)id * a.e.d + at;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= a.e.scale;
+    const f32x2 scale = tc::pack2(a.e.scale, a.e.scale);
     if (a.add) {
-        Eight<TO, kVec> old;
-        old.load(p, step, a.e.d - at);
-        float o[8];
+        Eight<TO, L> old;
+        old.template load<kKeep>(p, step, a.e.d - at);
+        f32x2 o[4];
         old.get(o);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += o[j];
+        for (int j = 0; j < 4; ++j) v[j] = tc::add2(tc::mul2(v[j], scale), o[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = tc::mul2(v[j], scale);
     }
-    Eight<TO, kVec> e;
+    Eight<TO, L> e;
     e.set(v);
     e.store(p, step, a.e.d - at);
 }
-template <bool kVec>
-__device__ __forceinline__ void write_part(const SumArgs &a, long long chunk, int which, int at, int step, const float (&v)[8])
+
+// the number of lanes from lane 0 on without a gap
+__device__ __forceinline__ int leading(bool p)
 {
-    Eight<float, kVec> e;
-    e.set(v);
-    e.template store<kKeep>(a.part + (chunk * 2 + which) * a.e.d + at, step, a.e.d - at);
+    const int gap = __ffs(~__ballot_sync(0xffffffffu, p));
+    return gap ? gap - 1 : 32;
 }
 
 // One chunk of sorted tokens and 8 blockDim columns
-template <class TY, class TO, bool kVec>
+template <class TY, class TO, Layout L>
 __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
 {
-    __shared__ int sk[kChunk + 2], sp[kChunk];
+    __shared__ int sk[kLong + kReach];  // ids of the tokens from kLong before the chunk on; -1 where there is none
+    __shared__ int sp[kReach];
     dependent_start();
     const long long chunk = blockIdx.x, i0 = chunk * kChunk;
-    const int n = (int)min((long long)kChunk, a.e.n - i0);
-    for (int i = threadIdx.x; i < kChunk + 2; i += blockDim.x) {
-        const long long at = i0 + i - 1;
-        sk[i] = at >= 0 && at < a.e.n && i <= n + 1 ? __ldg(a.key + at) : -1;
-        if (i < n) sp[i] = __ldg(a.pos + i0 + i);
+    for (int i = threadIdx.x; i < kLong + kReach; i += blockDim.x) {
+        const long long at = i0 + i - kLong;
+        sk[i] = at >= 0 && at < a.e.n ? __ldg(a.key + at) : -1;
+        if (i >= kLong) sp[i - kLong] = at < a.e.n ? __ldg(a.pos + at) : 0;
     }
     __syncthreads();
-    const int step = kVec ? 1 : blockDim.x, at = (kVec ? (blockIdx.y * blockDim.x + threadIdx.x) * 8 : blockIdx.y * blockDim.x * 8 + threadIdx.x);
+    const int *const id = sk + kLong;
+    const int lane = threadIdx.x & 31, n = (int)min((long long)kChunk, a.e.n - i0), V = a.e.V;
+    int begin = 0, end = n;
+    bool head = false, tail = false;  // the first, the last run is a piece of a long one that began before, that begins here
+    if (id[0] == V) return;           // (tokens without an id are the last)
+    if (id[-1] == id[0]) {
+        int back = leading(id[-1 - lane] == id[0]), on = leading(id[lane] == id[0]);
+        if (back == 32) back += leading(id[-33 - lane] == id[0]);
+        if (on == 32) on += leading(id[32 + lane] == id[0]);
+        if (on == 64) on += leading(id[64 + lane] == id[0]);
+        head = back + on > kLong;
+        if (!head) begin = on;        // (the chunk in which it began takes all of it)
+        if (begin >= n) return;
+    }
+    const int last = id[n - 1];
+    if (last != V && id[n] == last && !(head && last == id[0])) {
+        const int back = leading(id[n - 1 - lane] == last);  // (it begins in this chunk)
+        int on = leading(id[n + lane] == last);
+        if (on == 32) on += leading(id[n + 32 + lane] == last);
+        tail = back + on > kLong;
+        if (!tail) end = n + on;
+        else if (threadIdx.x == 0 && blockIdx.y == 0) a.list[atomicAdd(a.runs, 1)] = (int)chunk;
+    }
+    const int threads = blockDim.x, step = L == kQuads ? 4 * threads : threads, block = blockIdx.y * threads * 8,
+              at = block + (int)threadIdx.x * (L == kEights ? 8 : L == kQuads ? 4 : 1);
     if (at >= a.e.d) return;
     const TY *dy = static_cast<const TY *>(a.e.in) + at;
-    float acc[8] = {};
-    bool started = sk[0] != sk[1];  // the run of ids at hand began in this chunk
-    for (int i = 0; i < n; i += kAhead) {
-        if (sk[i + 1] == a.e.V) return;  // (tokens without an id are the last)
-        Eight<TY, kVec> row[kAhead];
+    f32x2 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(0.f, 0.f);
+    for (int i = begin; i < end; i += kAhead) {
+        Eight<TY, L> row[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (i + u < n && sk[i + u + 1] != a.e.V) row[u].load(dy + (long long)sp[i + u] * a.e.ld, step, a.e.d - at);
+            if (i + u < end && id[i + u] != V) row[u].load(dy + (long long)sp[i + u] * a.e.ld, step, a.e.d - at);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (i + u >= n) break;
-            const int id = sk[i + u + 1];
-            if (id == a.e.V) return;
-            float v[8];
+            if (i + u >= end) break;
+            const int now = id[i + u];
+            if (now == V) return;
+            f32x2 v[4];
             row[u].get(v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += v[j];
-            const bool ends = sk[i + u + 2] != id;
-            if (!ends && i + u + 1 < n) continue;
-            if (started && ends) write_row<TO, kVec>(a, id, at, step, acc);
-            else write_part<kVec>(a, chunk, started ? 1 : 0, at, step, acc);
-            started = true;
+            for (int j = 0; j < 4; ++j) acc[j] = tc::add2(acc[j], v[j]);
+            if (i + u + 1 < end && id[i + u + 1] == now) continue;
+            const bool piece = (head && now == id[0]) || (tail && now == last);
+            if (piece) {
+                Eight<float, L> e;
+                e.set(acc);
+                e.template store<kKeep>(a.part + (chunk * 2 + (head && now == id[0] ? 0 : 1)) * a.e.d + at, step, a.e.d - at);
+            } else {
+                write_row<TO, L>(a, now, at, step, acc);
+            }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+            for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(0.f, 0.f);
         }
     }
 }
 
-// Runs across chunks: the block of the chunk in which one begins adds up its parts, every kJoin-th by one row of threads, those in order.
+// Long runs: a block adds up the pieces of kJoinCols 8 columns of one, every kJoin-th piece by a row of threads, those in order.
 constexpr int kJoin = 8, kJoinCols = 32;
-template <class TO, bool kVec>
-__global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a)
+template <class TO, Layout L>
+__global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a, int tiles)
 {
     __shared__ float red[kJoin][8][kJoinCols + 1];
     dependent_start();
-    const long long chunk = blockIdx.x, last = (chunk + 1) * kChunk - 1;  // (the last chunk is not in the grid)
-    const int id = __ldg(a.key + last);
-    if (id == a.e.V || __ldg(a.key + last + 1) != id) return;             // no run goes on from this chunk
-    if (__ldg(a.key + chunk * kChunk) == id && chunk > 0 && __ldg(a.key + chunk * kChunk - 1) == id) return;  // it began earlier
-    long long lo = last + 1, hi = a.e.n;  // end of the run
-    while (lo < hi) {
-        const long long mid = (lo + hi) >> 1;
-        if (__ldg(a.key + mid) == id) lo = mid + 1;
-        else hi = mid;
-    }
-    const long long end = (lo - 1) / kChunk;  // its last chunk
-    const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols;
-    const int step = kVec ? 1 : kJoinCols;
-    for (int tile = blockIdx.y * kJoinCols * 8; tile < a.e.d; tile += gridDim.y * kJoinCols * 8) {
-        const int at = tile + (kVec ? c * 8 : c);
-        float acc[8] = {};
+    const long long items = (long long)*a.runs * tiles;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long chunk = __ldg(a.list + item / tiles);
+        const int id = __ldg(a.key + (chunk + 1) * kChunk - 1);
+        long long end = chunk;  // its last chunk: those behind the first that begin with it
+        for (int more = kJoin * kJoinCols; more == kJoin * kJoinCols; end += more) {
+            const long long at = (end + 1 + threadIdx.x) * kChunk;
+            more = __syncthreads_count(at < a.e.n && __ldg(a.key + at) == id);
+        }
+        const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols, step = L == kQuads ? 4 * kJoinCols : kJoinCols;
+        const int at = (int)(item % tiles) * kJoinCols * 8 + c * (L == kEights ? 8 : L == kQuads ? 4 : 1);
+        f32x2 acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(0.f, 0.f);
         if (at < a.e.d) {
 #pragma unroll 4
             for (long long k = chunk + q; k <= end; k += kJoin) {
-                Eight<float, kVec> e;
+                Eight<float, L> e;
                 e.template load<kKeep>(a.part + (k * 2 + (k == chunk ? 1 : 0)) * a.e.d + at, step, a.e.d - at);
-                float v[8];
+                f32x2 v[4];
                 e.get(v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += v[j];
+                for (int j = 0; j < 4; ++j) acc[j] = tc::add2(acc[j], v[j]);
             }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tc::unpack2(acc[j], red[q][2 * j][c], red[q][2 * j + 1][c]);
         __syncthreads();
+        if (q == 0 && at < a.e.d) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) red[q][j][c] = acc[j];
-        __syncthreads();
-        if (q || at >= a.e.d) continue;
+            for (int i = 1; i < kJoin; ++i)
 #pragma unroll
-        for (int i = 1; i < kJoin; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += red[i][j][c];
-        write_row<TO, kVec>(a, id, at, step, acc);
+                for (int j = 0; j < 4; ++j) acc[j] = tc::add2(acc[j], tc::pack2(red[i][2 * j][c], red[i][2 * j + 1][c]));
+            write_row<TO, L>(a, id, at, step, acc);
+        }
+        // (the next item writes to red behind the barrier in its search)
     }
 }
 
@@ -417,12 +461,10 @@ struct Type {
 };
 template <class F>
 cudaError_t with_type(int dtype, F f) { return dtype == RR_F32 ? f(Type<float>{}) : f(Type<bf16>{}); }
-template <class F>
-cudaError_t with_vec(bool vec, F f) { return vec ? f(std::integral_constant<bool, true>{}) : f(std::integral_constant<bool, false>{}); }
 
 struct BwdLayout {
     Header *hdr;
-    int *key, *pos, *key2, *pos2;
+    int *key, *pos, *key2, *pos2, *runs, *list;
     float *part;
     long long chunks;
     int slabs, slab;
@@ -439,7 +481,9 @@ size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
     l.pos = c.take<int>(n);
     l.key2 = l.slabs > 1 ? c.take<int>(n) : l.key;
     l.pos2 = l.slabs > 1 ? c.take<int>(n) : l.pos;
-    l.part = c.take<float>(l.chunks > 1 ? (size_t)l.chunks * 2 * d : 0);
+    l.runs = c.take<int>(1);
+    l.list = c.take<int>(n / kLong + 1);
+    l.part = c.take<float>(n > kLong ? (size_t)l.chunks * 2 * d : 0);
     if (out) *out = l;
     return align_up(c.off, 256);
 }
@@ -460,11 +504,18 @@ EmbArgs emb_args(const rr_embed_shape &s, const void *ids, const void *in, void 
     return a;
 }
 
+// bf16 alone goes eight at a time, with fp32 four: 16-byte accesses of the wider type
+Layout layout_of(const rr_embed_shape &s)
+{
+    if (s.table_dtype == RR_BF16 && s.y_dtype == RR_BF16 && s.d % 8 == 0 && s.ldy % 8 == 0) return kEights;
+    return s.d % 4 == 0 && s.ldy % 4 == 0 ? kQuads : kOne;
+}
+
 template <int K>
 cudaError_t launch_sort(const SortArgs &a, int blocks, cudaStream_t st)
 {
-    const size_t tables = (size_t)kDigits * (kSortWarps + 1) * 4 + (size_t)kSortThreads * K * 6, map = (size_t)kMapWords * 4;
-    const size_t smem = tables > map ? tables : map;
+    constexpr size_t smem = (size_t)kDigits * (kSortWarps + 2) * 4 + (size_t)kSortThreads * K * 6;
+    static_assert(smem >= kMapWords * 4 && smem <= 227 << 10, "a zeroing block's bitmap lies in the same memory");
     const cudaError_t err = cudaFuncSetAttribute(k_embed_sort<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
     return launch_dependent(k_embed_sort<K>, dim3(blocks), kSortThreads, smem, 1, st, a);
@@ -477,21 +528,25 @@ size_t embed_bwd_workspace(long long n, int d) { return bwd_layout(nullptr, n, d
 rr_status launch_embed_fwd(const rr_embed_shape &s, const void *ids, const void *table, void *y, void *ws, cudaStream_t st)
 {
     const EmbArgs a = emb_args(s, ids, table, y, ws);
-    const bool vec = s.d % 8 == 0 && s.ldy % (s.y_dtype == RR_F32 ? 4 : 8) == 0;
-    const int per_row = vec ? s.d / 8 : s.d, sms = device_sm_count();
+    const Layout L = layout_of(s);
+    const int per_row = L == kEights ? s.d / 8 : L == kQuads ? s.d / 4 : s.d, sms = device_sm_count();
     if (sms < 1) return RR_ERR_CUDA;
     // w / per_row is the high word of w * magic, magic = ceil(2^64 / per_row): what the rounding up adds to the quotient is below
     // w / 2^64 < 2^-32, less than the 1 / per_row that would be missing to the next whole number.  (A divisor of one has no such factor.)
     const unsigned long long magic = per_row == 1 ? 0 : ~0ull / (unsigned)per_row + 1;
-    const long long tiles = (s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll), most = (long long)sms * 8;
+    const long long tiles = ((long long)s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll), most = (long long)sms * 8;
     const dim3 grid((unsigned)(tiles < most ? tiles : most));
     const long long step = (long long)grid.x * kEmbThreads * kEmbUnroll, row_step = step / per_row;
     const unsigned at_step = (unsigned)(step % per_row);
     const cudaError_t err = with_type(s.table_dtype, [&](auto tx) {
         return with_type(s.y_dtype, [&](auto ty) {
-            return with_vec(vec, [&](auto v) {
-                return launch_dependent(k_embed_fwd<typename decltype(tx)::type, typename decltype(ty)::type, v()>, grid, kEmbThreads, 0, 1, st, a, per_row, magic, row_step, at_step);
-            });
+            using TX = typename decltype(tx)::type;
+            using TY = typename decltype(ty)::type;
+            auto go = [&](auto kernel) { return launch_dependent(kernel, grid, kEmbThreads, 0, 1, st, a, per_row, magic, row_step, at_step); };
+            if constexpr (sizeof(TX) + sizeof(TY) == 4) {
+                if (L == kEights) return go(k_embed_fwd<TX, TY, 8>);
+            }
+            return L == kOne ? go(k_embed_fwd<TX, TY, 1>) : go(k_embed_fwd<TX, TY, 4>);
         });
     });
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
@@ -508,11 +563,13 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     a.e = emb_args(s, ids, dy, dtable, ws);
     a.slabs = l.slabs;
     a.slab = l.slab;
-    a.passes = 1;
-    while (a.passes < 4 && ((unsigned long long)s.V >> (kDigitBits * a.passes)) != 0) ++a.passes;  // (V itself is a key)
+    int bits = 1;
+    while (bits < 31 && s.V >> bits) ++bits;  // (V itself is a key)
+    a.passes = (bits + kDigitBits - 1) / kDigitBits;
+    a.bits = (bits + a.passes - 1) / a.passes;
     a.key = l.key;
     a.pos = l.pos;
-    a.fill = !add;
+    a.runs = l.runs;
     a.out_f32 = s.table_dtype == RR_F32;
     int fillers = 0;
     if (!add) {  // zeroing blocks: one an SM, but none with less than 64 KB
@@ -521,9 +578,9 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
         fillers = (int)(want < most ? want : most);
         if (fillers > s.V) fillers = s.V;
     }
-    cudaError_t err = l.slab <= kSortThreads * 2 ? launch_sort<2>(a, l.slabs + fillers, st)
-                      : l.slab <= kSortThreads * 4 ? launch_sort<4>(a, l.slabs + fillers, st)
-                                                   : launch_sort<kSortMost>(a, l.slabs + fillers, st);
+    const int blocks = l.slabs + fillers, K = (l.slab + kSortThreads - 1) / kSortThreads;
+    cudaError_t err = K <= 2 ? launch_sort<2>(a, blocks, st) : K <= 4 ? launch_sort<4>(a, blocks, st) : K <= 8 ? launch_sort<8>(a, blocks, st)
+                                                                                                                : launch_sort<kSortMost>(a, blocks, st);
     if (err == cudaSuccess && l.slabs > 1)
         err = launch_dependent(k_embed_merge, dim3((unsigned)((s.n + kEmbThreads - 1) / kEmbThreads)), kEmbThreads, 0, 1, st, (long long)s.n, l.slabs, l.slab,
                                (const int *)l.key, (const int *)l.pos, l.key2, l.pos2);
@@ -533,27 +590,33 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     b.key = l.key2;
     b.pos = l.pos2;
     b.part = l.part;
-    b.chunks = l.chunks;
+    b.runs = l.runs;
+    b.list = l.list;
     b.add = add;
-    const bool vec = s.d % 8 == 0 && s.ldy % (s.y_dtype == RR_F32 ? 4 : 8) == 0;
+    const Layout L = layout_of(s);
     int threads = 32;
     while (threads < kEmbThreads && threads * 8 < s.d) threads <<= 1;
     const dim3 grid((unsigned)l.chunks, (unsigned)((s.d + threads * 8 - 1) / (threads * 8)));
-    err = with_type(s.y_dtype, [&](auto ty) {
-        return with_type(s.table_dtype, [&](auto to) {
-            return with_vec(vec, [&](auto v) {
-                return launch_dependent(k_embed_sum<typename decltype(ty)::type, typename decltype(to)::type, v()>, grid, threads, 0, 1, st, b);
-            });
+    const int tiles = (s.d + kJoinCols * 8 - 1) / (kJoinCols * 8);
+    const long long most_items = (long long)(s.n / kLong + 1) * tiles;
+    const dim3 join((unsigned)(most_items < 2 * sms ? most_items : 2 * sms));
+    err = with_type(s.table_dtype, [&](auto to) {
+        using TO = typename decltype(to)::type;
+        cudaError_t e = with_type(s.y_dtype, [&](auto ty) {
+            using TY = typename decltype(ty)::type;
+            auto go = [&](auto kernel) { return launch_dependent(kernel, grid, threads, 0, 1, st, b); };
+            if constexpr (sizeof(TY) + sizeof(TO) == 4) {
+                if (L == kEights) return go(k_embed_sum<TY, TO, kEights>);
+            }
+            return L == kOne ? go(k_embed_sum<TY, TO, kOne>) : go(k_embed_sum<TY, TO, kQuads>);
         });
+        if (e != cudaSuccess || s.n <= kLong) return e;  // (no run is long)
+        auto go = [&](auto kernel) { return launch_dependent(kernel, join, kJoin * kJoinCols, 0, 1, st, b, tiles); };
+        if constexpr (sizeof(TO) == 2) {
+            if (L == kEights) return go(k_embed_join<TO, kEights>);
+        }
+        return L == kOne ? go(k_embed_join<TO, kOne>) : go(k_embed_join<TO, kQuads>);
     });
-    if (err == cudaSuccess && l.chunks > 1) {
-        const int tiles = (s.d + kJoinCols * 8 - 1) / (kJoinCols * 8);
-        err = with_type(s.table_dtype, [&](auto to) {
-            return with_vec(vec, [&](auto v) {
-                return launch_dependent(k_embed_join<typename decltype(to)::type, v()>, dim3((unsigned)(l.chunks - 1), tiles < 16 ? tiles : 16), kJoin * kJoinCols, 0, 1, st, b);
-            });
-        });
-    }
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 

@@ -81,7 +81,7 @@ rr_status launch_balance_fwd(int T, int E, int k, int stride, int S, const float
 rr_status launch_balance_bwd(int T, int E, int k, int S, const float *logits, const int32_t *count, const int32_t *n_live,
                              const uint8_t *live, float coef_b, float coef_z, int accumulate, float *dlogits, cudaStream_t st);
 
-// Norm (rr_norm.cu), embedding (rr_embed.cu), clip (rr_clip.cu); the shapes' pitches are filled in
+// Norm (rr_norm_fwd.cu, rr_norm_bwd.cu), embedding (rr_embed.cu), clip (rr_clip.cu); the shapes' pitches are filled in
 size_t norm_workspace(int M, int N);
 rr_status launch_norm_fwd(const rr_norm_shape &s, const void *x, const void *residual, const void *w, const void *b, void *h, void *y, float *mean,
                           float *rstd, cudaStream_t st);

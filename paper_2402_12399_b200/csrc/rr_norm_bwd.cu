@@ -1,0 +1,304 @@
+// Gradients of the norm (rr_norm.cuh has the mathematics).
+#include "rr_norm.cuh"
+
+namespace rr {
+
+namespace {
+
+constexpr int bwd_blocks(int threads) { return threads == 256 ? 2 : 1; }  // an SM
+
+// A block takes every gridDim-th set of rows and keeps the sums of its columns over them in registers.  With four eights a thread there are no
+// registers left to keep a row's numbers: they are worked out a second time.  TD: type of dx and dh.
+template <class TY, class TH, class TD, Layout L, int kSlots, int kThreads>
+__global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(const NormArgs a)
+{
+    constexpr bool kHold = kSlots == 2;
+    extern __shared__ __align__(16) char ring[];  // [2] dy, h, dh; afterwards the sums of the block's rows side by side
+    __shared__ float2 buf[2][32];
+    dependent_start();
+    const int t = threadIdx.x & (a.group - 1), step = step_of<L>(a.group), rows = kThreads / a.group;
+    const long long stride = (long long)gridDim.x * rows;
+    long long row = (long long)blockIdx.x * rows + threadIdx.x / a.group;
+    const int h_at = tensor_bytes(L, sizeof(TY), kSlots, kThreads, rows, a.N), d_at = h_at + tensor_bytes(L, sizeof(TH), kSlots, kThreads, rows, a.N);
+    const int stage_bytes = d_at + (a.dh ? tensor_bytes(L, sizeof(TD), kSlots, kThreads, rows, a.N) : 0);
+    auto request = [&](long long r, char *to) {
+        if (r < a.M) {
+            copy_row<TY, L, kSlots, kThreads>(to, static_cast<const TY *>(a.dy) + r * a.lddy, t, a.group, a.N);
+            copy_row<TH, L, kSlots, kThreads>(to + h_at, static_cast<const TH *>(a.h) + r * a.ldh, t, a.group, a.N);
+            if (a.dh) copy_row<TD, L, kSlots, kThreads>(to + d_at, static_cast<const TD *>(a.dh) + r * a.lddh, t, a.group, a.N);
+        }
+        copies_asked();
+    };
+    if (a.ahead) request(row, ring);
+    f32x2 aw[kSlots][4], ab[kSlots][4];
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) aw[s][j] = ab[s][j] = pack2(0.f, 0.f);
+    int turn = 0, stage = 0;
+    for (long long first = (long long)blockIdx.x * rows; first < a.M; first += stride, row += stride) {
+        const bool in = row < a.M;
+        const float mean = in && a.layer ? __ldg(a.mean + row) : 0.f, rstd = in ? __ldg(a.rstd + row) : 0.f;
+        const char *here = ring + stage * stage_bytes;
+        if (a.ahead) {
+            stage ^= 1;
+            if (L == kOne) {  // (the rows of the other buffer have been read by all, these have come for all)
+                copies_arrived<0>();
+                row_barrier(a.group);
+                request(row + stride, ring + stage * stage_bytes);
+            } else {
+                request(row + stride, ring + stage * stage_bytes);
+                copies_arrived<1>();
+            }
+        }
+        const TY *py = static_cast<const TY *>(a.dy) + row * a.lddy;
+        const TH *ph = static_cast<const TH *>(a.h) + row * a.ldh;
+        const TD *pd = static_cast<const TD *>(a.dh) + row * a.lddh;
+        const f32x2 centre = pack2(-mean, -mean), factor = pack2(rstd, rstd);
+        // the numbers of slot s: dy, xh and the weight (behind the row: dy is 0, and so is all that is made of it)
+        auto numbers = [&](int s, int at, f32x2 (&y)[4], f32x2 (&x)[4], f32x2 (&w)[4]) {
+            Eight<TY, L> ey;
+            Eight<TH, L> eh;
+            if (a.ahead) {
+                take<TY, L, kThreads>(here, py, s, t, a.group, a.N, ey);
+                take<TH, L, kThreads>(here + h_at, ph, s, t, a.group, a.N, eh);
+            } else {
+                ey.load(py + at, step, a.N - at);
+                eh.load(ph + at, step, a.N - at);
+            }
+            parameter<L>(a.w, a.w_f32, at, step, a.N - at, 1.f, w);
+            ey.get(y);
+            eh.get(x);
+            if (a.layer) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = add2(x[j], centre);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = mul2(x[j], factor);
+        };
+        f32x2 g[kHold ? kSlots : 1][4], xh[kHold ? kSlots : 1][4], p1 = pack2(0.f, 0.f), p2 = p1;
+        if (in) {
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                const int at = first_column<L>(s, t, a.group), k = kHold ? s : 0;
+                if (at >= a.N) break;
+                f32x2 w[4];
+                numbers(s, at, g[k], xh[k], w);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    aw[s][j] = fma2(g[k][j], xh[k][j], aw[s][j]);
+                    if (a.db) ab[s][j] = add2(ab[s][j], g[k][j]);
+                    g[k][j] = mul2(g[k][j], w[j]);
+                    if (a.layer) p1 = add2(p1, g[k][j]);
+                    p2 = fma2(g[k][j], xh[k][j], p2);
+                }
+            }
+        }
+        if (!a.dx) continue;  // (not wanted)
+        float s1 = both(p1), s2 = both(p2);
+        row_sums(s1, s2, a.group, buf, turn);
+        if (!in) continue;
+        const f32x2 c1 = pack2(-s1 * a.inv_n, -s1 * a.inv_n), c2 = pack2(-s2 * a.inv_n, -s2 * a.inv_n);
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            const int at = first_column<L>(s, t, a.group), k = kHold ? s : 0;
+            if (at >= a.N) break;
+            if constexpr (!kHold) {
+                f32x2 w[4];
+                numbers(s, at, g[0], xh[0], w);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], w[j]);
+            }
+            Eight<TD, L> e;
+            f32x2 o[4];
+            if (a.dh) {
+                if (a.ahead) take<TD, L, kThreads>(here + d_at, pd, s, t, a.group, a.N, e);
+                else e.load(pd + at, step, a.N - at);
+                e.get(o);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f32x2 d = fma2(xh[k][j], c2, g[k][j]);
+                if (a.layer) d = add2(d, c1);
+                o[j] = a.dh ? fma2(d, factor, o[j]) : mul2(d, factor);
+            }
+            e.set(o);
+            e.store(static_cast<TD *>(a.dx) + row * a.lddx + at, step, a.N - at);
+        }
+    }
+    if (!a.dw && !a.db) return;
+    // The sums of the rows side by side: of a warp by exchange (every lane adds the same pairs in the same order), of the block through shared memory
+    for (int o = a.group; o < 32; o <<= 1) {
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                aw[s][j] = add2(aw[s][j], __shfl_xor_sync(0xffffffffu, aw[s][j], o));
+                ab[s][j] = add2(ab[s][j], __shfl_xor_sync(0xffffffffu, ab[s][j], o));
+            }
+    }
+    const size_t part = (size_t)blockIdx.x * a.N;
+    const int sets = kThreads / (a.group < 32 ? 32 : a.group);
+    if (sets == 1) {
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            const int at = first_column<L>(s, t, a.group);
+            if (at >= a.N) break;
+            float *const out[2] = {a.dw, a.db};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (!out[k]) continue;
+                f32x2 o[4];
+                Eight<float, L> e;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = k ? ab[s][j] : aw[s][j];
+                if (a.add) {
+                    f32x2 old[4];
+                    e.load(out[k] + part + at, step, a.N - at);
+                    e.get(old);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = add2(old[j], o[j]);
+                }
+                e.set(o);
+                e.template store<kKeep>(out[k] + part + at, step, a.N - at);
+            }
+        }
+        return;
+    }
+    copies_arrived<0>();
+    __syncthreads();  // (nobody reads rows any more)
+    float *const sums = reinterpret_cast<float *>(ring);  // [sets][2][N]
+    const int set = threadIdx.x / (a.group < 32 ? 32 : a.group);
+    if ((threadIdx.x & 31) < a.group) {
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            const int at = first_column<L>(s, t, a.group);
+            if (at >= a.N) break;
+            Eight<float, kOne> e;  // (element by element: a row of sums starts anywhere)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float *out = sums + (2 * set + k) * a.N;
+                e.set(k ? ab[s] : aw[s]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = L == kEights ? at + j : L == kQuads ? at + (j >> 2) * step + (j & 3) : at + j * step;
+                    if (c < a.N) out[c] = e.e[j];
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.N; c += kThreads) {
+        float *out = c < a.N ? a.dw : a.db;
+        if (!out) continue;
+        float sum = sums[c];
+        for (int q = 1; q < sets; ++q) sum += sums[2 * q * a.N + c];
+        float *o = out + part + (c < a.N ? c : c - a.N);
+        *o = a.add ? *o + sum : sum;
+    }
+}
+
+// out[c] (+)= sum of the blocks' parts of column c, in a fixed order: a thread adds up every kLanes-th part, then the lanes are added in turn
+constexpr int kFoldLanes = 16;
+__global__ void __launch_bounds__(32 * kFoldLanes) k_norm_fold(int blocks, int N, const float *pw, const float *pb, float *dw, float *db, int add)
+{
+    __shared__ float red[kFoldLanes][33];
+    const float *p = blockIdx.y ? pb : pw;
+    float *out = blockIdx.y ? db : dw;
+    const int lane = threadIdx.x & 31, q = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    dependent_start();
+    if (!out) return;
+    float sum = 0.f;
+    if (c < N) {
+#pragma unroll 8
+        for (int b = q; b < blocks; b += kFoldLanes) sum += __ldg(p + (size_t)b * N + c);
+    }
+    red[q][lane] = sum;
+    __syncthreads();
+    if (q || c >= N) return;
+    sum = red[0][lane];
+#pragma unroll
+    for (int i = 1; i < kFoldLanes; ++i) sum += red[i][lane];
+    out[c] = add ? out[c] + sum : sum;
+}
+
+// Two eights a thread beside the sums of as many columns; four from 8192 columns on, where two would take a block of 1024.
+NormLayout bwd_layout(int N) { return norm_layout(N, N > 8192 ? 4 : 2, 256); }
+
+int bwd_parts(int M, int N)
+{
+    const NormLayout l = bwd_layout(N);
+    const int sms = device_sm_count();
+    const long long sets = ((long long)M + l.rows - 1) / l.rows, most = (long long)(sms > 0 ? sms : 148) * bwd_blocks(l.threads);
+    return (int)(sets < most ? sets : most);
+}
+
+template <Layout L, class F>
+cudaError_t with_layout(const NormLayout &l, F f)
+{
+    if (l.threads == 256) return call<L, 2, 256>(f);
+    if (l.threads == 1024) return call<L, 4, 1024>(f);
+    return l.slots == 2 ? call<L, 2, 512>(f) : call<L, 4, 512>(f);
+}
+
+}  // namespace
+
+size_t norm_workspace(int M, int N) { return kHeaderBytes + align_up((size_t)bwd_parts(M, N) * N * 4, 256) * 2; }
+
+rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h, const void *w, const float *mean, const float *rstd, const void *dh,
+                          void *dx, float *dw, float *db, void *workspace, cudaStream_t st)
+{
+    Access access(s.N);
+    access.matrix(dy, s.y_dtype, s.lddy);
+    access.matrix(h, s.h_dtype, s.ldh);
+    access.matrix(dh, s.dx_dtype, s.lddh);
+    access.matrix(dx, s.dx_dtype, s.lddx);
+    if (!dh && !dx) access.all_bf16 = access.all_bf16 && s.dx_dtype == RR_BF16;  // (its kernels are of that type all the same)
+    const Layout L = access.layout();
+    const NormLayout l = bwd_layout(s.N);
+    NormArgs a = norm_args(s, l);
+    a.dy = dy;
+    a.h = const_cast<void *>(h);
+    a.w = w;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    a.dh = dh;
+    a.dx = dx;
+    const int parts = bwd_parts(s.M, s.N), add = (s.flags & RR_ADD_DW) != 0;
+    const bool fold = parts > 1 && (dw || db);
+    Carver c(workspace);
+    c.take<Header>(1);
+    float *pw = c.take<float>((size_t)parts * s.N), *pb = c.take<float>((size_t)parts * s.N);
+    a.dw = dw ? (fold ? pw : dw) : nullptr;
+    a.db = db ? (fold ? pb : db) : nullptr;
+    a.add = fold ? 0 : add;
+    auto bytes = [&](int dtype) { return tensor_bytes(L, dtype == RR_F32 ? 4 : 2, l.slots, l.threads, l.rows, s.N); };
+    int smem = 2 * (bytes(s.y_dtype) + bytes(s.h_dtype) + (dh ? bytes(s.dx_dtype) : 0));
+    a.ahead = (long long)s.M > (long long)parts * l.rows && smem <= kMostShared / bwd_blocks(l.threads);  // (a block with one set of rows has nothing to fetch ahead)
+    if (!a.ahead) smem = 0;
+    const int sets = l.threads / (l.group < 32 ? 32 : l.group), sums = sets > 1 ? sets * 2 * s.N * 4 : 0;  // (32 KB at most)
+    if (smem < sums) smem = sums;
+    cudaError_t err = with_type(s.y_dtype, [&](auto ty) {
+        return with_type(s.h_dtype, [&](auto th) {
+            return with_type(s.dx_dtype, [&](auto td) {
+                using TY = typename decltype(ty)::type;
+                using TH = typename decltype(th)::type;
+                using TD = typename decltype(td)::type;
+                auto go = [&](auto layout, auto slots, auto threads) {
+                    auto kernel = k_norm_bwd<TY, TH, TD, layout(), slots(), threads()>;
+                    const cudaError_t e = allow(kernel, smem);
+                    return e != cudaSuccess ? e : launch_dependent(kernel, dim3(parts), threads(), (size_t)smem, 1, st, a);
+                };
+                if constexpr (sizeof(TY) + sizeof(TH) + sizeof(TD) == 6) {
+                    if (L == kEights) return with_layout<kEights>(l, go);
+                }
+                return L == kOne ? with_layout<kOne>(l, go) : with_layout<kQuads>(l, go);
+            });
+        });
+    });
+    if (err == cudaSuccess && fold)
+        err = launch_dependent(k_norm_fold, dim3((s.N + 31) / 32, 2), 32 * kFoldLanes, 0, 1, st, parts, s.N, (const float *)pw, (const float *)pb, dw, db, add);
+    return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+}
+
+}  // namespace rr

@@ -1,12 +1,12 @@
 // Eight elements of a row per thread and step, bf16 or fp32, as they lie in memory: the access shared by the memory-bound operators of a
-// training step (norm, embedding, clip).  kVec: eight consecutive elements at a 16-byte aligned address.  Otherwise any alignment and any
-// width: elements `step` apart, so that the threads of a group still read and write next to each other.
+// training step (norm, embedding, clip).
 #pragma once
 #include <cuda_bf16.h>
 
 #include <type_traits>
 
 #include "rr_common.cuh"
+#include "rr_tc.cuh"
 
 namespace rr {
 
@@ -18,9 +18,6 @@ __device__ __forceinline__ T from_f32(float v)
     if constexpr (sizeof(T) == 4) return v;
     else return __float2bfloat16_rn(v);
 }
-// v as a value of T holds it
-template <class T>
-__device__ __forceinline__ float rounded(float v) { return as_f32(from_f32<T>(v)); }
 
 // How a load or store treats the caches: kStream for what is touched once, kKeep for what comes again, kConst for what comes again and
 // what nothing in the launch writes to.
@@ -43,68 +40,158 @@ __device__ __forceinline__ void place(V *p, V v)
     else *p = v;
 }
 
-template <class T, bool kVec>
+using tc::f32x2;
+
+// two bf16 of a word as an fp32 pair, and back
+__device__ __forceinline__ f32x2 pair_of(uint32_t w) { return tc::pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t word_of(f32x2 v) { return tc::pack_bf16x2(v); }
+
+// kN consecutive elements at an address that is a multiple of their size: 16 bytes, or the four bf16 beside four fp32; or one element
+template <class T, int kN>
+struct Unit {
+    using Raw = std::conditional_t<kN == 1, std::conditional_t<sizeof(T) == 4, float, unsigned short>,
+                                   std::conditional_t<sizeof(T) * kN == 8, uint2, std::conditional_t<sizeof(T) == 4, float4, uint4>>>;
+    Raw raw;
+    template <Cache C>
+    __device__ __forceinline__ void load(const T *p) { raw = fetch<C>(reinterpret_cast<const Raw *>(p)); }
+    template <Cache C>
+    __device__ __forceinline__ void store(T *p) const { place<C>(reinterpret_cast<Raw *>(p), raw); }
+    __device__ __forceinline__ void get(float (&v)[kN]) const
+    {
+        if constexpr (kN == 1) {
+            if constexpr (sizeof(T) == 4) v[0] = raw;
+            else v[0] = __uint_as_float((uint32_t)raw << 16);
+        } else if constexpr (sizeof(T) == 4) {
+            v[0] = raw.x; v[1] = raw.y; v[2] = raw.z; v[3] = raw.w;
+        } else {
+            tc::unpack2(pair_of(raw.x), v[0], v[1]);
+            tc::unpack2(pair_of(raw.y), v[2], v[3]);
+            if constexpr (kN == 8) {
+                tc::unpack2(pair_of(raw.z), v[4], v[5]);
+                tc::unpack2(pair_of(raw.w), v[6], v[7]);
+            }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[kN])
+    {
+        if constexpr (kN == 1) {
+            if constexpr (sizeof(T) == 4) raw = v[0];
+            else raw = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+        } else if constexpr (sizeof(T) == 4) {
+            raw = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            raw.x = word_of(tc::pack2(v[0], v[1]));
+            raw.y = word_of(tc::pack2(v[2], v[3]));
+            if constexpr (kN == 8) {
+                raw.z = word_of(tc::pack2(v[4], v[5]));
+                raw.w = word_of(tc::pack2(v[6], v[7]));
+            }
+        }
+    }
+};
+template <int kN, class A, class B>
+__device__ __forceinline__ void scaled(const Unit<A, kN> &from, Unit<B, kN> &to, float f)
+{
+    float v[kN];
+    from.get(v);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] *= f;
+    to.set(v);
+}
+
+// Where the eight elements of a thread lie, so that the threads of a group read and write whole 32-byte sectors side by side:
+//   kEights  eight next to each other, 16 bytes of bf16 (in fp32 a warp would touch every sector twice)
+//   kQuads   four next to each other and four more `step` elements on: 16 bytes of fp32, 8 of bf16
+//   kOne     eight elements `step` apart: any width, any alignment
+enum Layout { kOne, kQuads, kEights };
+
+__device__ __forceinline__ void quad_of(const float4 &q, f32x2 &a, f32x2 &b) { a = tc::pack2(q.x, q.y); b = tc::pack2(q.z, q.w); }
+__device__ __forceinline__ void quad_of(const uint2 &q, f32x2 &a, f32x2 &b) { a = pair_of(q.x); b = pair_of(q.y); }
+__device__ __forceinline__ void quad_from(float4 &q, f32x2 a, f32x2 b) { tc::unpack2(a, q.x, q.y); tc::unpack2(b, q.z, q.w); }
+__device__ __forceinline__ void quad_from(uint2 &q, f32x2 a, f32x2 b) { q = make_uint2(word_of(a), word_of(b)); }
+
+// p points at the thread's first element; `left` elements of the row are there from it on.  What lies behind the row is read as zero and not
+// written (with kEights the width is a multiple of eight, with kQuads of four).
+template <class T, Layout L>
 struct Eight;
 
-template <>
-struct Eight<float, true> {
-    float4 a, b;
-    template <Cache C = kStream>
-    __device__ __forceinline__ void load(const float *p, int, int)
-    {
-        a = fetch<C>(reinterpret_cast<const float4 *>(p));
-        b = fetch<C>(reinterpret_cast<const float4 *>(p) + 1);
-    }
-    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-    __device__ __forceinline__ void get(float (&v)[8]) const
-    {
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-    __device__ __forceinline__ void set(const float (&v)[8])
-    {
-        a = make_float4(v[0], v[1], v[2], v[3]);
-        b = make_float4(v[4], v[5], v[6], v[7]);
-    }
-    template <Cache C = kStream>
-    __device__ __forceinline__ void store(float *p, int, int) const
-    {
-        place<C>(reinterpret_cast<float4 *>(p), a);
-        place<C>(reinterpret_cast<float4 *>(p) + 1, b);
-    }
-};
-
-template <>
-struct Eight<__nv_bfloat16, true> {
-    uint4 u;
-    template <Cache C = kStream>
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p, int, int) { u = fetch<C>(reinterpret_cast<const uint4 *>(p)); }
-    __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void get(float (&v)[8]) const
-    {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-    __device__ __forceinline__ void set(const float (&v)[8])
-    {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        u = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    template <Cache C = kStream>
-    __device__ __forceinline__ void store(__nv_bfloat16 *p, int, int) const { place<C>(reinterpret_cast<uint4 *>(p), u); }
-};
-
-// p points at the thread's first element, `left` elements of the row are there from it on (elements behind are read as zero and not written)
 template <class T>
-struct Eight<T, false> {
+struct Eight<T, kEights> {
+    uint4 q[sizeof(T) / 2];
+    template <Cache C = kStream>
+    __device__ __forceinline__ void load(const T *p, int, int)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = fetch<C>(reinterpret_cast<const uint4 *>(p) + i);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void get(f32x2 (&v)[4]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            v[0] = pair_of(q[0].x); v[1] = pair_of(q[0].y); v[2] = pair_of(q[0].z); v[3] = pair_of(q[0].w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                quad_of(make_float4(__uint_as_float(q[i].x), __uint_as_float(q[i].y), __uint_as_float(q[i].z), __uint_as_float(q[i].w)), v[2 * i], v[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void set(const f32x2 (&v)[4])
+    {
+        if constexpr (sizeof(T) == 2) {
+            q[0] = make_uint4(word_of(v[0]), word_of(v[1]), word_of(v[2]), word_of(v[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                float4 f;
+                quad_from(f, v[2 * i], v[2 * i + 1]);
+                q[i] = make_uint4(__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w));
+            }
+        }
+    }
+    template <Cache C = kStream>
+    __device__ __forceinline__ void store(T *p, int, int) const
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) place<C>(reinterpret_cast<uint4 *>(p) + i, q[i]);
+    }
+};
+
+template <class T>
+struct Eight<T, kQuads> {
+    using Quad = std::conditional_t<sizeof(T) == 4, float4, uint2>;
+    Quad a, b;
+    template <Cache C = kStream>
+    __device__ __forceinline__ void load(const T *p, int step, int left)
+    {
+        a = fetch<C>(reinterpret_cast<const Quad *>(p));
+        b = Quad{};
+        if (step < left) b = fetch<C>(reinterpret_cast<const Quad *>(p + step));
+    }
+    __device__ __forceinline__ void zero() { a = b = Quad{}; }
+    __device__ __forceinline__ void get(f32x2 (&v)[4]) const
+    {
+        quad_of(a, v[0], v[1]);
+        quad_of(b, v[2], v[3]);
+    }
+    __device__ __forceinline__ void set(const f32x2 (&v)[4])
+    {
+        quad_from(a, v[0], v[1]);
+        quad_from(b, v[2], v[3]);
+    }
+    template <Cache C = kStream>
+    __device__ __forceinline__ void store(T *p, int step, int left) const
+    {
+        place<C>(reinterpret_cast<Quad *>(p), a);
+        if (step < left) place<C>(reinterpret_cast<Quad *>(p + step), b);
+    }
+};
+
+template <class T>
+struct Eight<T, kOne> {
     T e[8];
     template <Cache C = kStream>
     __device__ __forceinline__ void load(const T *p, int step, int left)
@@ -117,15 +204,20 @@ struct Eight<T, false> {
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(0.f);
     }
-    __device__ __forceinline__ void get(float (&v)[8]) const
+    __device__ __forceinline__ void get(f32x2 (&v)[4]) const
     {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = as_f32(e[j]);
+        for (int j = 0; j < 4; ++j) v[j] = tc::pack2(as_f32(e[2 * j]), as_f32(e[2 * j + 1]));
     }
-    __device__ __forceinline__ void set(const float (&v)[8])
+    __device__ __forceinline__ void set(const f32x2 (&v)[4])
     {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
+        for (int j = 0; j < 4; ++j) {
+            float x, y;
+            tc::unpack2(v[j], x, y);
+            e[2 * j] = from_f32<T>(x);
+            e[2 * j + 1] = from_f32<T>(y);
+        }
     }
     template <Cache C = kStream>
     __device__ __forceinline__ void store(T *p, int step, int left) const
