@@ -558,7 +558,7 @@ typedef struct rr_embed_shape {
  *   table, dtable [V,d] dev, 16-byte aligned, dense;  y, dy [n,d] dev, 16-byte aligned
  *   workspace dev, >= fwd_bytes / bwd_bytes, 256-byte aligned; its first 256 bytes are zero when first used (the status word)
  * fp32 arithmetic, one rounding to the result's type (under RR_ADD_DW of the sum with what was there).  The gradient's sums follow the order
- * of the tokens, in pieces that depend on n and the ids alone: results repeat bit for bit.  n == 0 does nothing forward; backward
+ * of the tokens, in pieces that depend on n, d and the ids alone: results repeat bit for bit.  n == 0 does nothing forward; backward
  * it sets dtable to zero, or leaves it under RR_ADD_DW.  An output that overlaps what the call reads is refused.  Calls that share a
  * workspace must not overlap on the GPU.
  */

@@ -758,6 +758,7 @@ def norm_workspace_bytes(M: int, N: int) -> int:
 
 
 def _vector(t, n: int, dtype, what: str):
+    """Address of a vector of n elements (None: not given)."""
     if t is None:
         return None
     if t.shape != (n,) or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
@@ -766,11 +767,25 @@ def _vector(t, n: int, dtype, what: str):
     return t.data_ptr()
 
 
-def _parameters(weight, bias, N: int) -> int:
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise TypeError(f"weight is {weight.dtype}, bias {bias.dtype}")
+def _matrix(t, shape, what: str):
+    """(address, pitch, type) of a matrix whose rows may lie apart; zeros when it is not given."""
+    if t is None:
+        return None, 0, 0
+    code = _TYPE_CODE.get(t.dtype)
+    if code is None:
+        _code(t, what)
+    if t.shape == shape and t.is_contiguous():
+        return t.data_ptr(), 0, code
+    return t.data_ptr(), _pitch(t, shape[0], shape[1], what), code
+
+
+def _parameters(weight, bias) -> int:
     t = weight if weight is not None else bias
-    return BF16 if t is None else _code(t, "weight" if t is weight else "bias")
+    if t is None:
+        return BF16
+    if bias is not None and bias.dtype != t.dtype:
+        raise TypeError(f"weight is {t.dtype}, bias {bias.dtype}")
+    return _code(t, "weight and bias")
 
 
 def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
@@ -779,21 +794,24 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Te
     """rr_norm_fwd; returns y [M,N] = norm(residual + x) * weight + bias (type: out's, else out_dtype, else the residual's, else x's).
     Pass `h`, of the residual's type, to receive residual + x (it may be the residual itself), and `mean`, `rstd` [M] fp32 to keep the
     statistics for norm_bwd (no mean with NORM_RMS).  x, residual, h and out may be views whose rows lie apart."""
-    M, N = x.shape
+    shape = x.shape
+    M, N = shape
     if out is None:
-        out = torch.empty(M, N, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
+        out = torch.empty(shape, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
     here = _here()
     _elsewhere(here, x, weight, bias, residual, h, out, mean, rstd)
+    px, ldx, xt = _matrix(x, shape, "x")
+    pr, ldr, ht = _matrix(residual, shape, "residual")
+    ph, ldh, t = _matrix(h, shape, "h")
+    py, ldy, yt = _matrix(out, shape, "out")
     if h is not None:
         if residual is None:
             raise ValueError("h is residual + x: it needs a residual")
-        if h.dtype != residual.dtype:
+        if t != ht:
             raise TypeError(f"residual is {residual.dtype}, h {h.dtype}")
-    s = _CNorm(M, N, kind, _code(x, "x"), 0 if residual is None else _code(residual, "residual"), _parameters(weight, bias, N), _code(out, "out"), 0, 0, eps,
-               _pitch(x, M, N, "x"), _pitch(residual, M, N, "residual"), _pitch(h, M, N, "h"), _pitch(out, M, N, "out"), 0, 0, 0)
-    code = (_lib or lib()).rr_norm_fwd(C.byref(s), x.data_ptr(), None if residual is None else residual.data_ptr(), _vector(weight, N, None, "weight"),
-                                       _vector(bias, N, None, "bias"), None if h is None else h.data_ptr(), out.data_ptr(), _vector(mean, M, _F32, "mean"),
-                                       _vector(rstd, M, _F32, "rstd"), _stream_of(here))
+    s = _CNorm(M, N, kind, xt, ht, _parameters(weight, bias), yt, 0, 0, eps, ldx, ldr, ldh, ldy)
+    code = (_lib or lib()).rr_norm_fwd(C.byref(s), px, pr, _vector(weight, N, None, "weight"), _vector(bias, N, None, "bias"), ph, py,
+                                       _vector(mean, M, _F32, "mean"), _vector(rstd, M, _F32, "rstd"), _stream_of(here))
     if code:
         raise RRError(code, "rr_norm_fwd")
     return out
@@ -805,19 +823,24 @@ def norm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mea
     """rr_norm_bwd; writes the gradients whose buffers are given -- dx [M,N] (bf16 or fp32; the gradient of h, so that of x and of the
     residual), dw [N] and dbias [N] fp32 -- and returns (dx, dw, dbias).  `h` is what the norm was taken of (x where there was no residual);
     `dh`, of dx's type, is the gradient that reaches it along the residual stream.  With add_dw, dw and dbias are added to."""
-    M, N = dy.shape
+    shape = dy.shape
+    M, N = shape
     if workspace is None:
         workspace = alloc_workspace(norm_workspace_bytes(M, N), dy.device)
     here = _here()
     _elsewhere(here, dy, h, weight, mean, rstd, dh, dx, dw, dbias, workspace)
-    if dh is not None and dx is not None and dh.dtype != dx.dtype:
-        raise TypeError(f"dh is {dh.dtype}, dx {dx.dtype}")
-    t = dx if dx is not None else dh
-    s = _CNorm(M, N, kind, 0, _code(h, "h"), _parameters(weight, None, N), _code(dy, "dy"), 0 if t is None else _code(t, "dx"),
-               ADD_DW if add_dw else 0, 0.0, 0, 0, _pitch(h, M, N, "h"), 0, _pitch(dy, M, N, "dy"), _pitch(dh, M, N, "dh"), _pitch(dx, M, N, "dx"))
-    code = (_lib or lib()).rr_norm_bwd(C.byref(s), dy.data_ptr(), h.data_ptr(), _vector(weight, N, None, "weight"), _vector(mean, M, _F32, "mean"),
-                                       _vector(rstd, M, _F32, "rstd"), None if dh is None else dh.data_ptr(), None if dx is None else dx.data_ptr(),
-                                       _vector(dw, N, _F32, "dw"), _vector(dbias, N, _F32, "dbias"), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    py, lddy, yt = _matrix(dy, shape, "dy")
+    ph, ldh, ht = _matrix(h, shape, "h")
+    pd, lddh, dt = _matrix(dh, shape, "dh")
+    px, lddx, t = _matrix(dx, shape, "dx")
+    if dx is not None:
+        if dh is not None and dt != t:
+            raise TypeError(f"dh is {dh.dtype}, dx {dx.dtype}")
+        dt = t
+    s = _CNorm(M, N, kind, 0, ht, _parameters(weight, None), yt, dt, ADD_DW if add_dw else 0, 0.0, 0, 0, ldh, 0, lddy, lddh, lddx)
+    code = (_lib or lib()).rr_norm_bwd(C.byref(s), py, ph, _vector(weight, N, None, "weight"), _vector(mean, M, _F32, "mean"), _vector(rstd, M, _F32, "rstd"),
+                                       pd, px, _vector(dw, N, _F32, "dw"), _vector(dbias, N, _F32, "dbias"), workspace.data_ptr(), workspace.numel(),
+                                       _stream_of(here))
     if code:
         raise RRError(code, "rr_norm_bwd")
     for t in (dx, dw, dbias):
@@ -854,8 +877,9 @@ def embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: t
     _elsewhere(here, ids, table, out, workspace)
     if not table.is_contiguous():
         raise ValueError("table must be contiguous")
-    s = _CEmbed(n, V, d, _token_ids(ids), _code(table, "table"), _code(out, "out"), 0, scale, _pitch(out, n, d, "out"))
-    code = (_lib or lib()).rr_embed_fwd(C.byref(s), ids.data_ptr(), table.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    py, ldy, yt = _matrix(out, (n, d), "out")
+    s = _CEmbed(n, V, d, _token_ids(ids), _code(table, "table"), yt, 0, scale, ldy)
+    code = (_lib or lib()).rr_embed_fwd(C.byref(s), ids.data_ptr(), table.data_ptr(), py, workspace.data_ptr(), workspace.numel(), _stream_of(here))
     if code:
         raise RRError(code, "rr_embed_fwd")
     out._workspace = workspace
@@ -874,8 +898,9 @@ def embed_bwd(ids: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, scale: 
     _elsewhere(here, ids, dy, dtable, workspace)
     if not dtable.is_contiguous():
         raise ValueError("dtable must be contiguous")
-    s = _CEmbed(n, V, d, _token_ids(ids), _code(dtable, "dtable"), _code(dy, "dy"), ADD_DW if accumulate else 0, scale, _pitch(dy, n, d, "dy"))
-    code = (_lib or lib()).rr_embed_bwd(C.byref(s), ids.data_ptr(), dy.data_ptr(), dtable.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    py, ldy, yt = _matrix(dy, (n, d), "dy")
+    s = _CEmbed(n, V, d, _token_ids(ids), _code(dtable, "dtable"), yt, ADD_DW if accumulate else 0, scale, ldy)
+    code = (_lib or lib()).rr_embed_bwd(C.byref(s), ids.data_ptr(), py, dtable.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
     if code:
         raise RRError(code, "rr_embed_bwd")
     dtable._workspace = workspace

@@ -81,6 +81,25 @@ inline int device_sm_count()
     return n;
 }
 
+// The shared memory that a kernel may be launched with, beyond the 48 KB of every kernel: asked for once per device and size that is larger than
+// before (the question costs a launch half a microsecond).  One static object per kernel.
+struct SharedAllowance {
+    std::atomic<int> known[64] = {};
+    template <class K>
+    cudaError_t ask(K kernel, int bytes)
+    {
+        if (bytes <= 40 << 10) return cudaSuccess;
+        int dev = 0;
+        cudaError_t err = cudaGetDevice(&dev);
+        if (err != cudaSuccess) return err;
+        const bool keep = dev >= 0 && dev < 64;
+        if (keep && known[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (err == cudaSuccess && keep) known[dev].store(bytes, std::memory_order_relaxed);
+        return err;
+    }
+};
+
 // Carves aligned sub-buffers out of one workspace allocation (base may be null to size only).
 struct Carver {
     char *base;

@@ -30,13 +30,27 @@ struct EmbArgs {
     int *status;
 };
 
-// id of token i: 0..V-1, or -1 for none (and, with the error latched, for one out of range)
-__device__ __forceinline__ int token_id(const EmbArgs &a, long long i)
+// Ids of the kN tokens first, first + step, ...: 0..V-1, or -1 for none (and, with the error latched, for one out of range); -2 from token
+// `end` on.  All are asked for before the first is looked at.
+template <int kN>
+__device__ __forceinline__ void token_ids(const EmbArgs &a, const long long (&token)[kN], long long end, int (&id)[kN])
 {
-    const long long id = a.wide ? __ldg(static_cast<const long long *>(a.ids) + i) : (long long)__ldg(static_cast<const int *>(a.ids) + i);
-    if (id >= 0 && id < a.V) return (int)id;
-    if (id != -1) latch_status(a.status, RR_ERR_INVALID_ARG);
-    return -1;
+    long long raw[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+        raw[k] = -1;
+        if (token[k] >= end) continue;
+        if (a.wide) raw[k] = __ldg(static_cast<const long long *>(a.ids) + token[k]);
+        else raw[k] = __ldg(static_cast<const int *>(a.ids) + token[k]);
+    }
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+        const bool fits = raw[k] >= 0 && raw[k] < a.V;
+        bad |= !fits && raw[k] != -1;
+        id[k] = token[k] >= end ? -2 : fits ? (int)raw[k] : -1;
+    }
+    if (bad) latch_status(a.status, RR_ERR_INVALID_ARG);
 }
 
 // A block takes tiles of kTile units of the result (kN elements each), whatever the width of a row; row and place of a unit come from a
@@ -47,7 +61,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
 {
     constexpr int kTile = kEmbThreads * kEmbUnroll;
     dependent_start();
-    const long long total = a.n * per_row;
+    const long long total = a.n * per_row;  // (a unit behind the last has a row behind the last)
     long long row0 = (long long)blockIdx.x * kTile / per_row;
     unsigned at0 = (unsigned)((long long)blockIdx.x * kTile - row0 * per_row);
     for (long long tile = (long long)blockIdx.x * kTile; tile < total; tile += (long long)gridDim.x * kTile) {
@@ -60,8 +74,8 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
             const unsigned q = magic ? (unsigned)__umul64hi(w, magic) : w;  // w / per_row (the host says why)
             row[u] = row0 + q;
             at[u] = w - q * per_row;
-            id[u] = tile + l < total ? token_id(a, row[u]) : -2;
         }
+        token_ids(a, row, a.n, id);
         Unit<TX, kN> e[kEmbUnroll];
 #pragma unroll
         for (int u = 0; u < kEmbUnroll; ++u) {
@@ -88,9 +102,12 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
 // ---- backward: the sort -------------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits; // at most
+constexpr int kDigitBits = 5, kDigits = 1 << kDigitBits; // at most
 constexpr int kSortMost = 16;                            // tokens a thread of a sorting block holds
 constexpr int kSlab = kSortThreads * kSortMost;          // tokens of a sorting block
+constexpr int kPlaceBits = 14;                           // a token's place in its slab
+static_assert(kSlab <= 1 << kPlaceBits && kSortMost <= 16, "a place fits into its bits, a thread's count of a digit into four");
+constexpr int kTableWords = kDigits * (kSortThreads / 2 / 16 * 17);
 constexpr int kMapWords = 8192;                          // bitmap of a zeroing block: 2^18 rows at a time
 
 struct SortArgs {
@@ -110,7 +127,7 @@ __device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *ma
     int lanes = 1;
     while (lanes < 32 && lanes * 16 < width) lanes <<= 1;
     const int lane = threadIdx.x & (lanes - 1), step = kSortThreads / lanes;
-    constexpr int kAtOnce = 16;
+    constexpr int kAtOnce = 8;
     for (long long r0 = lo; r0 < hi; r0 += kMapWords * 32) {
         const long long r1 = min(hi, r0 + kMapWords * 32);
         const int words = (int)((r1 - r0 + 31) / 32);
@@ -118,9 +135,11 @@ __device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *ma
         for (int i = threadIdx.x; i < words; i += kSortThreads) map[i] = 0;
         __syncthreads();
         for (long long i0 = threadIdx.x; i0 < a.e.n; i0 += kAtOnce * kSortThreads) {
+            long long token[kAtOnce];
             int id[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) id[u] = i0 + u * kSortThreads < a.e.n ? token_id(a.e, i0 + u * kSortThreads) : -1;
+            for (int u = 0; u < kAtOnce; ++u) token[u] = i0 + u * kSortThreads;
+            token_ids(a.e, token, a.e.n, id);
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u)
                 if (id[u] >= r0 && id[u] < r1) atomicOr(&map[(id[u] - r0) >> 5], 1u << ((id[u] - r0) & 31));
@@ -138,24 +157,12 @@ __device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *ma
     }
 }
 
-// lanes of the warp with the same digit (`bits` bits) as this one
-__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits)
-{
-    uint32_t same = 0xffffffffu;
-#pragma unroll
-    for (int b = 0; b < kDigitBits; ++b) {
-        if (b >= bits) break;
-        const uint32_t with = __ballot_sync(0xffffffffu, digit >> b & 1);
-        same &= digit >> b & 1 ? with : ~with;
-    }
-    return same;
-}
-
-// Stable sort of a slab by id, least significant digit first.  A thread holds K tokens (token w 32 K + k 32 + lane of the slab): in a
-// pass every warp counts its tokens digit by digit in its own column of a table, which gives a token its place among the equal digits of the
-// warp; the table is scanned digit by digit and warp by warp, and the tokens move in shared memory.
+// Stable sort of a slab by id, least significant digit first, of words T that hold an id and below it the token's place in the slab.  Thread t
+// holds the K words t K, t K + 1, ...: in a pass it counts them digit by digit in its own column of a table (32 digits of 1024 threads, 16 bits
+// each) and remembers how many of a word's digit it had before; the table is scanned digit by digit and thread by thread, and the words
+// move in shared memory.  (Counted by warps with ballots instead, a token cost 150 instructions a pass: 16384 tokens 40 us.)
 // Blocks behind the sorting ones zero the rows that nobody names.
-template <int K>
+template <int K, class T>
 __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
 {
     extern __shared__ __align__(16) uint32_t shared[];
@@ -164,91 +171,85 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
         zero_rows(a, blockIdx.x - a.slabs, gridDim.x - a.slabs, shared);
         return;
     }
-    constexpr int kRow = kSortWarps + 1;                   // (a column of the table in every bank)
-    uint32_t *const count = shared;                        // [kDigits][kRow]
-    uint32_t *const total = count + kDigits * kRow;        // [kDigits] tokens of a digit, then those of lower ones
-    uint32_t *const sk = total + kDigits;                  // [1024 K]
-    uint16_t *const sp = reinterpret_cast<uint16_t *>(sk + kSortThreads * K);
+    // Table and words have gaps, so that threads next to each other meet in different banks: two entries after every 32, one word after every K.
+    uint16_t *const count = reinterpret_cast<uint16_t *>(shared);  // [digits][kSortThreads]
+    T *const words = reinterpret_cast<T *>(shared + kTableWords);
+    auto entry = [](uint32_t digit, int thread) { return digit * (kSortThreads / 16 * 17) + thread + (thread >> 5) * 2; };
     __shared__ uint32_t warp_total[kSortWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, digits = 1 << a.bits;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, digits = 1 << a.bits;
     const long long base = (long long)blockIdx.x * a.slab;
     const int n = (int)min((long long)a.slab, a.e.n - base);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.runs = 0;
-    uint32_t key[K], pos[K];
+    if (blockIdx.x == 0 && t == 0) *a.runs = 0;
+    constexpr int kAtOnce = K < 8 ? K : 8;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int i = warp * 32 * K + k * 32 + lane;
-        int id = -1;
-        if (i < n) id = token_id(a.e, base + i);
-        key[k] = i >= n ? 0xffffffffu : id < 0 ? (uint32_t)a.e.V : (uint32_t)id;  // (places behind the end stay behind all others)
-        pos[k] = i;
+    for (int k0 = 0; k0 < K; k0 += kAtOnce) {
+        long long token[kAtOnce];
+        int id[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) token[k] = base + (k0 + k) * kSortThreads + t;
+        token_ids(a.e, token, base + n, id);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int i = (k0 + k) * kSortThreads + t;  // (places behind the end stay behind all others)
+            words[i + i / K] = (id[k] == -2 ? ~(T)0 << kPlaceBits : (T)(id[k] < 0 ? a.e.V : id[k]) << kPlaceBits) | (T)i;
+        }
     }
     for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * a.bits;
-        for (int i = threadIdx.x; i < digits * kRow; i += kSortThreads) count[i] = 0;
+        const int shift = kPlaceBits + pass * a.bits;
+        uint4 *const table = reinterpret_cast<uint4 *>(count);
+        for (int i = t; i < digits * (kSortThreads / 128 * 17); i += kSortThreads) table[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
-        uint32_t rank[K];
+        T e[K];
+        uint32_t at[K];  // a word's entry in the table, and below it how many of its digit the thread had before
+#pragma unroll
+        for (int k = 0; k < K; ++k) e[k] = words[t * (K + 1) + k];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const uint32_t digit = key[k] >> shift & (digits - 1), same = same_digit(digit, a.bits), below = same & ((1u << lane) - 1);
-            uint32_t *c = &count[digit * kRow + warp];
-            const uint32_t before = *c;
-            __syncwarp();
-            if (below == 0) *c = before + __popc(same);
-            __syncwarp();
-            rank[k] = before + __popc(below);
+            const uint32_t c = entry((uint32_t)(e[k] >> shift) & (digits - 1), t), before = count[c];
+            count[c] = (uint16_t)(before + 1);
+            at[k] = c << 4 | before;
         }
         __syncthreads();
-        for (int d = warp; d < digits; d += kSortWarps) {  // a digit's tokens in the warps before
-            const uint32_t own = count[d * kRow + lane];
-            uint32_t sum = own;
+        // exclusive scan: thread t owns `digits` entries next to each other, pairs of 16 bits in a word
+        uint32_t *const own = shared + t * (digits / 2) + t * (digits / 2) / 16;
+        uint32_t pairs = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += up;
-            }
-            count[d * kRow + lane] = sum - own;
-            if (lane == 31) total[d] = sum;
-        }
-        __syncthreads();
-        uint32_t own = 0, sum = 0;  // lower digits' tokens
-        if ((int)threadIdx.x < digits) sum = own = total[threadIdx.x];
+        for (int i = 0; i < kDigits / 2; ++i)
+            if (i < digits / 2) pairs += own[i];  // (no half leaves 16 bits: there are no more tokens)
+        uint32_t sum = (pairs & 0xffff) + (pairs >> 16), upto = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += up;
+            const uint32_t up = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += up;
         }
-        if (lane == 31) warp_total[warp] = sum;
+        if (lane == 31) warp_total[warp] = upto;
         __syncthreads();
-        if (warp < digits / 32 || warp == 0) {
-            uint32_t before = lane < warp ? warp_total[lane] : 0;
+        uint32_t run = lane < warp ? warp_total[lane] : 0;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-            if ((int)threadIdx.x < digits) total[threadIdx.x] = before + sum - own;
-        }
-        __syncthreads();
+        for (int o = 16; o > 0; o >>= 1) run += __shfl_xor_sync(0xffffffffu, run, o);
+        run += upto - sum;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const uint32_t digit = key[k] >> shift & (digits - 1), to = rank[k] + total[digit] + count[digit * kRow + warp];
-            sk[to] = key[k];
-            sp[to] = (uint16_t)pos[k];
+        for (int i = 0; i < kDigits / 2; ++i) {
+            if (i >= digits / 2) break;
+            const uint32_t two = own[i], low = two & 0xffff;
+            own[i] = run | (run + low) << 16;
+            run += low + (two >> 16);
         }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int i = warp * 32 * K + k * 32 + lane;
-            key[k] = sk[i];
-            pos[k] = sp[i];
+            const uint32_t to = count[at[k] >> 4] + (at[k] & 15);
+            words[to + to / K] = e[k];
         }
-        // (the next pass writes to sk and sp behind further barriers)
+        __syncthreads();
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = warp * 32 * K + k * 32 + lane;
-        if (i < n) {
-            a.key[base + i] = (int)key[k];
-            a.pos[base + i] = (int)(base + pos[k]);
-        }
+        const int i = k * kSortThreads + t;
+        if (i >= n) break;
+        const T e = words[i + i / K];
+        a.key[base + i] = (int)(e >> kPlaceBits);
+        a.pos[base + i] = (int)(base + (long long)(e & ((1 << kPlaceBits) - 1)));
     }
 }
 
@@ -291,21 +292,21 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_merge(long long n, int sl
 }
 
 // ---- backward: the sums -------------------------------------------------------------------------------------------
-// A run is all the tokens of one id.  A block takes a chunk of sorted tokens, and of the runs that begin in it those of up to kLong tokens
-// to their end: most runs are short, and need no second look.  Of a longer run every chunk adds up its own piece (the first piece is part 1
-// of its chunk, every other the part 0), and k_embed_join adds up the pieces in order.
+// A run is all the tokens of one id.  A block takes a chunk of sorted tokens, and of the runs that begin in it those of up to two chunks'
+// length to their end: most runs are short, and need no second look.  Of a longer run every chunk adds up its own piece (the first piece is
+// part 1 of its chunk, every other the part 0), and k_embed_join adds up the pieces in order.
 struct SumArgs {
     EmbArgs e;
     const int *key, *pos;  // [n] sorted
     float *part;           // [chunks][2][d]
     int *runs, *list;      // long runs: how many, and the chunks in which they begin (in any order)
+    int chunk;             // sorted tokens of a chunk, kLeastChunk to kMostChunk
     int add;
 };
 
-constexpr int kChunk = 32;             // sorted tokens of a chunk
-constexpr int kLong = 64;
-constexpr int kReach = kChunk + kLong; // tokens that a block may have to look at from the start of its chunk on
-constexpr int kAhead = 8;              // rows in flight
+constexpr int kLeastChunk = 8, kMostChunk = 32;
+constexpr int kBefore = 2 * kMostChunk, kReach = 3 * kMostChunk;  // tokens that a block looks at before its chunk, and from its start on
+constexpr int kAhead = 8;                                         // rows in flight
 
 template <class TO, Layout L>
 __device__ __forceinline__ void write_row(const SumArgs &a, int id, int at, int step, f32x2 (&v)[4])
@@ -339,18 +340,32 @@ __device__ __forceinline__ int leading(bool p)
 template <class TY, class TO, Layout L>
 __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
 {
-    __shared__ int sk[kLong + kReach];  // ids of the tokens from kLong before the chunk on; -1 where there is none
+    __shared__ int sk[kBefore + kReach];  // ids of the tokens from kBefore before the chunk on; -1 where there is none
     __shared__ int sp[kReach];
     dependent_start();
-    const long long chunk = blockIdx.x, i0 = chunk * kChunk;
-    for (int i = threadIdx.x; i < kLong + kReach; i += blockDim.x) {
-        const long long at = i0 + i - kLong;
-        sk[i] = at >= 0 && at < a.e.n ? __ldg(a.key + at) : -1;
-        if (i >= kLong) sp[i - kLong] = at < a.e.n ? __ldg(a.pos + at) : 0;
+    const long long chunk = blockIdx.x, i0 = chunk * a.chunk;
+    constexpr int kLooks = (kBefore + kReach) / 32;  // (of a block of 32; all asked for at once)
+    int k[kLooks], p[kLooks];
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) {
+        const int i = threadIdx.x + u * blockDim.x;
+        const long long at = i0 + i - kBefore;
+        k[u] = -1;
+        p[u] = 0;
+        if (i >= kBefore + kReach || at < 0 || at >= a.e.n) continue;
+        k[u] = __ldg(a.key + at);
+        if (i >= kBefore) p[u] = __ldg(a.pos + at);
+    }
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) {
+        const int i = threadIdx.x + u * blockDim.x;
+        if (i >= kBefore + kReach) break;
+        sk[i] = k[u];
+        if (i >= kBefore) sp[i - kBefore] = p[u];
     }
     __syncthreads();
-    const int *const id = sk + kLong;
-    const int lane = threadIdx.x & 31, n = (int)min((long long)kChunk, a.e.n - i0), V = a.e.V;
+    const int *const id = sk + kBefore;
+    const int lane = threadIdx.x & 31, n = (int)min((long long)a.chunk, a.e.n - i0), V = a.e.V, longest = 2 * a.chunk;
     int begin = 0, end = n;
     bool head = false, tail = false;  // the first, the last run is a piece of a long one that began before, that begins here
     if (id[0] == V) return;           // (tokens without an id are the last)
@@ -359,7 +374,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
         if (back == 32) back += leading(id[-33 - lane] == id[0]);
         if (on == 32) on += leading(id[32 + lane] == id[0]);
         if (on == 64) on += leading(id[64 + lane] == id[0]);
-        head = back + on > kLong;
+        head = back + on > longest;
         if (!head) begin = on;        // (the chunk in which it began takes all of it)
         if (begin >= n) return;
     }
@@ -368,7 +383,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
         const int back = leading(id[n - 1 - lane] == last);  // (it begins in this chunk)
         int on = leading(id[n + lane] == last);
         if (on == 32) on += leading(id[n + 32 + lane] == last);
-        tail = back + on > kLong;
+        tail = back + on > longest;
         if (!tail) end = n + on;
         else if (threadIdx.x == 0 && blockIdx.y == 0) a.list[atomicAdd(a.runs, 1)] = (int)chunk;
     }
@@ -418,10 +433,10 @@ __global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a
     const long long items = (long long)*a.runs * tiles;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         const long long chunk = __ldg(a.list + item / tiles);
-        const int id = __ldg(a.key + (chunk + 1) * kChunk - 1);
+        const int id = __ldg(a.key + (chunk + 1) * a.chunk - 1);
         long long end = chunk;  // its last chunk: those behind the first that begin with it
         for (int more = kJoin * kJoinCols; more == kJoin * kJoinCols; end += more) {
-            const long long at = (end + 1 + threadIdx.x) * kChunk;
+            const long long at = (end + 1 + threadIdx.x) * a.chunk;
             more = __syncthreads_count(at < a.e.n && __ldg(a.key + at) == id);
         }
         const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols, step = L == kQuads ? 4 * kJoinCols : kJoinCols;
@@ -467,12 +482,16 @@ struct BwdLayout {
     int *key, *pos, *key2, *pos2, *runs, *list;
     float *part;
     long long chunks;
-    int slabs, slab;
+    int slabs, slab, chunk;
 };
 size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
 {
     BwdLayout l;
-    l.chunks = (n + kChunk - 1) / kChunk;
+    // chunks: shorter ones where the SMs would be short of warps
+    const long long warps = (d + 255) / 256;
+    l.chunk = kMostChunk;
+    while (l.chunk > kLeastChunk && n * warps < 16384ll * l.chunk) l.chunk >>= 1;
+    l.chunks = (n + l.chunk - 1) / l.chunk;
     l.slabs = (int)((n + kSlab - 1) / kSlab);
     l.slab = l.slabs ? (int)((n + l.slabs - 1) / l.slabs) : 0;
     Carver c(ws);
@@ -482,8 +501,8 @@ size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
     l.key2 = l.slabs > 1 ? c.take<int>(n) : l.key;
     l.pos2 = l.slabs > 1 ? c.take<int>(n) : l.pos;
     l.runs = c.take<int>(1);
-    l.list = c.take<int>(n / kLong + 1);
-    l.part = c.take<float>(n > kLong ? (size_t)l.chunks * 2 * d : 0);
+    l.list = c.take<int>(n / (2 * l.chunk) + 1);
+    l.part = c.take<float>(n > 2 * l.chunk ? (size_t)l.chunks * 2 * d : 0);
     if (out) *out = l;
     return align_up(c.off, 256);
 }
@@ -511,14 +530,22 @@ Layout layout_of(const rr_embed_shape &s)
     return s.d % 4 == 0 && s.ldy % 4 == 0 ? kQuads : kOne;
 }
 
-template <int K>
+template <int K, class T>
 cudaError_t launch_sort(const SortArgs &a, int blocks, cudaStream_t st)
 {
-    constexpr size_t smem = (size_t)kDigits * (kSortWarps + 2) * 4 + (size_t)kSortThreads * K * 6;
+    constexpr size_t smem = (size_t)kTableWords * 4 + (size_t)kSortThreads * (K + 1) * sizeof(T);
     static_assert(smem >= kMapWords * 4 && smem <= 227 << 10, "a zeroing block's bitmap lies in the same memory");
-    const cudaError_t err = cudaFuncSetAttribute(k_embed_sort<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static SharedAllowance allowance;
+    const cudaError_t err = allowance.ask(k_embed_sort<K, T>, (int)smem);
     if (err != cudaSuccess) return err;
-    return launch_dependent(k_embed_sort<K>, dim3(blocks), kSortThreads, smem, 1, st, a);
+    return launch_dependent(k_embed_sort<K, T>, dim3(blocks), kSortThreads, smem, 1, st, a);
+}
+template <class T>
+cudaError_t launch_sort(const SortArgs &a, int blocks, cudaStream_t st)
+{
+    const int K = (a.slab + kSortThreads - 1) / kSortThreads;
+    return K <= 2 ? launch_sort<2, T>(a, blocks, st) : K <= 4 ? launch_sort<4, T>(a, blocks, st) : K <= 8 ? launch_sort<8, T>(a, blocks, st)
+                                                                                                          : launch_sort<kSortMost, T>(a, blocks, st);
 }
 
 }  // namespace
@@ -534,7 +561,7 @@ rr_status launch_embed_fwd(const rr_embed_shape &s, const void *ids, const void 
     // w / per_row is the high word of w * magic, magic = ceil(2^64 / per_row): what the rounding up adds to the quotient is below
     // w / 2^64 < 2^-32, less than the 1 / per_row that would be missing to the next whole number.  (A divisor of one has no such factor.)
     const unsigned long long magic = per_row == 1 ? 0 : ~0ull / (unsigned)per_row + 1;
-    const long long tiles = ((long long)s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll), most = (long long)sms * 8;
+    const long long tiles = ((long long)s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll), most = (long long)sms * 16;
     const dim3 grid((unsigned)(tiles < most ? tiles : most));
     const long long step = (long long)grid.x * kEmbThreads * kEmbUnroll, row_step = step / per_row;
     const unsigned at_step = (unsigned)(step % per_row);
@@ -578,9 +605,8 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
         fillers = (int)(want < most ? want : most);
         if (fillers > s.V) fillers = s.V;
     }
-    const int blocks = l.slabs + fillers, K = (l.slab + kSortThreads - 1) / kSortThreads;
-    cudaError_t err = K <= 2 ? launch_sort<2>(a, blocks, st) : K <= 4 ? launch_sort<4>(a, blocks, st) : K <= 8 ? launch_sort<8>(a, blocks, st)
-                                                                                                                : launch_sort<kSortMost>(a, blocks, st);
+    // (ids of up to 18 bits fit into a 32-bit word beside the place)
+    cudaError_t err = bits <= 32 - kPlaceBits ? launch_sort<uint32_t>(a, l.slabs + fillers, st) : launch_sort<uint64_t>(a, l.slabs + fillers, st);
     if (err == cudaSuccess && l.slabs > 1)
         err = launch_dependent(k_embed_merge, dim3((unsigned)((s.n + kEmbThreads - 1) / kEmbThreads)), kEmbThreads, 0, 1, st, (long long)s.n, l.slabs, l.slab,
                                (const int *)l.key, (const int *)l.pos, l.key2, l.pos2);
@@ -592,29 +618,26 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     b.part = l.part;
     b.runs = l.runs;
     b.list = l.list;
+    b.chunk = l.chunk;
     b.add = add;
-    const Layout L = layout_of(s);
+    const Layout L = s.d % 8 == 0 && s.ldy % 8 == 0 ? kEights : layout_of(s);  // (fp32 too: its loads meet in the L1 cache)
     int threads = 32;
     while (threads < kEmbThreads && threads * 8 < s.d) threads <<= 1;
     const dim3 grid((unsigned)l.chunks, (unsigned)((s.d + threads * 8 - 1) / (threads * 8)));
     const int tiles = (s.d + kJoinCols * 8 - 1) / (kJoinCols * 8);
-    const long long most_items = (long long)(s.n / kLong + 1) * tiles;
+    const long long most_items = (long long)(s.n / (2 * l.chunk) + 1) * tiles;
     const dim3 join((unsigned)(most_items < 2 * sms ? most_items : 2 * sms));
     err = with_type(s.table_dtype, [&](auto to) {
         using TO = typename decltype(to)::type;
         cudaError_t e = with_type(s.y_dtype, [&](auto ty) {
             using TY = typename decltype(ty)::type;
             auto go = [&](auto kernel) { return launch_dependent(kernel, grid, threads, 0, 1, st, b); };
-            if constexpr (sizeof(TY) + sizeof(TO) == 4) {
-                if (L == kEights) return go(k_embed_sum<TY, TO, kEights>);
-            }
+            if (L == kEights) return go(k_embed_sum<TY, TO, kEights>);
             return L == kOne ? go(k_embed_sum<TY, TO, kOne>) : go(k_embed_sum<TY, TO, kQuads>);
         });
-        if (e != cudaSuccess || s.n <= kLong) return e;  // (no run is long)
+        if (e != cudaSuccess || s.n <= 2 * l.chunk) return e;  // (no run is long)
         auto go = [&](auto kernel) { return launch_dependent(kernel, join, kJoin * kJoinCols, 0, 1, st, b, tiles); };
-        if constexpr (sizeof(TO) == 2) {
-            if (L == kEights) return go(k_embed_join<TO, kEights>);
-        }
+        if (L == kEights) return go(k_embed_join<TO, kEights>);
         return L == kOne ? go(k_embed_join<TO, kOne>) : go(k_embed_join<TO, kQuads>);
     });
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;

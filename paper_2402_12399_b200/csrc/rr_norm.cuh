@@ -21,8 +21,10 @@ struct NormArgs {
     int M, N;
     int group;       // threads of a row, a power of two
     int layer;       // mean taken off
-    int ahead;       // rows come through shared memory, the next set while the present one is worked on; else straight from global memory
+    int ahead;       // backward: buffers for rows in shared memory: 2, the next row comes while one is worked on; 1, then; 0, straight from global memory
     float eps, inv_n;
+    long long stride;                                   // rows from one set of a block to its next,
+    long long sx, sr, sh, sy, sdy, sdh, sdx;            // and as many pitches
     long long ldx, ldr, ldh, ldy, lddy, lddh, lddx;
     const void *x, *residual, *dy, *dh, *w, *b;
     void *h, *y, *dx;  // (backward: h is read only)
@@ -32,44 +34,25 @@ struct NormArgs {
     int add;         // dw, db: add to what is there
 };
 
-// Columns of slot s of a thread: first_column on, the eight of them as Layout says with steps of step_of.
+// A row is shared out over `group` threads (G of them; 0: fewer than 32, told at run time).  Thread t holds kSlots times eight columns: those
+// of slot s are first_column + 8 group s on, the eight of them as Layout says with steps of step_of.
 template <Layout L>
-__device__ __forceinline__ int first_column(int s, int t, int group)
-{
-    return L == kEights ? (s * group + t) * 8 : L == kQuads ? s * 8 * group + t * 4 : s * 8 * group + t;
-}
+__device__ __forceinline__ int first_column(int t) { return L == kEights ? t * 8 : L == kQuads ? t * 4 : t; }
 template <Layout L>
 __device__ __forceinline__ int step_of(int group) { return L == kQuads ? 4 * group : group; }
 // values behind the row set to zero
 template <Layout L>
-__device__ __forceinline__ void cut(f32x2 (&v)[4], int at, int step, int N)
+__device__ __forceinline__ void cut(f32x2 (&v)[4], int step, int left)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if constexpr (L == kOne) {
             float x, y;
             unpack2(v[j], x, y);
-            v[j] = pack2(at + 2 * j * step < N ? x : 0.f, at + (2 * j + 1) * step < N ? y : 0.f);
-        } else if (at + (L == kQuads && j >= 2 ? step : 0) >= N) {
+            v[j] = pack2(2 * j * step < left ? x : 0.f, (2 * j + 1) * step < left ? y : 0.f);
+        } else if ((L == kQuads && j >= 2 ? step : 0) >= left) {
             v[j] = pack2(0.f, 0.f);
         }
-    }
-}
-
-template <Layout L>
-__device__ __forceinline__ void parameter(const void *p, int f32, int at, int step, int left, float none, f32x2 (&v)[4])
-{
-    if (!p) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = pack2(none, none);
-    } else if (f32) {
-        Eight<float, L> e;
-        e.template load<kConst>(static_cast<const float *>(p) + at, step, left);
-        e.get(v);
-    } else {
-        Eight<bf16, L> e;
-        e.template load<kConst>(static_cast<const bf16 *>(p) + at, step, left);
-        e.get(v);
     }
 }
 
@@ -77,11 +60,16 @@ __device__ __forceinline__ void parameter(const void *p, int f32, int at, int st
 // kEights, kQuads: a thread copies its own pieces ahead of their use and reads back nothing but what it copied, so all it needs is its own
 // wait.  kOne: the threads of a row copy it in 16-byte pieces from the boundary before its start on, wherever that lies; a barrier later they read
 // elements.  Nothing behind the end of a row is read.
+__host__ __device__ constexpr int row_bytes(int size, int N) { return (N * size + 15) / 16 * 16 + 16; }
 __host__ __device__ constexpr int tensor_bytes(Layout L, int size, int slots, int threads, int rows, int N)
 {
-    return L == kOne ? rows * ((N * size + 15) / 16 * 16 + 16) : slots * 8 * size * threads;
+    return L == kOne ? rows * row_bytes(size, N) : slots * 8 * size * threads;
 }
-__device__ __forceinline__ void copy16(uint32_t to, const void *from, int bytes)
+__device__ __forceinline__ void copy16(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_some(uint32_t to, const void *from, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
@@ -89,43 +77,45 @@ __device__ __forceinline__ void copy8(uint32_t to, const void *from)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
+// `own`: the thread's first column in the row; `to`: its tensor's place in shared memory
 template <class T, Layout L, int kSlots, int kThreads>
-__device__ __forceinline__ void copy_row(char *to, const T *row, int t, int group, int N)
+__device__ __forceinline__ void copy_row(uint32_t to, const T *own, int t, int group, int N)
 {
     if constexpr (L == kOne) {
-        const uint32_t dst = smem_u32(to) + threadIdx.x / group * tensor_bytes(kOne, sizeof(T), 0, 0, 1, N);
+        const T *row = own - t;
+        const uint32_t dst = to + threadIdx.x / group * row_bytes(sizeof(T), N);
         const int lead = (int)(reinterpret_cast<uintptr_t>(row) & 15), bytes = lead + N * (int)sizeof(T);
         const char *src = reinterpret_cast<const char *>(row) - lead;
-        for (int g = t * 16; g < bytes; g += group * 16) copy16(dst + g, src + g, min(16, bytes - g));
+        for (int g = t * 16; g < bytes; g += group * 16) copy_some(dst + g, src + g, min(16, bytes - g));
     } else {
+        const int left = N - first_column<L>(t);
 #pragma unroll
         for (int s = 0; s < kSlots; ++s) {
-            const int at = first_column<L>(s, t, group), step = step_of<L>(group);
-            if (at >= N) break;
             if constexpr (L == kEights) {
-                copy16(smem_u32(to) + (s * kThreads + threadIdx.x) * 16, row + at, 16);
+                if (s * 8 * group < left) copy16(to + (s * kThreads + threadIdx.x) * 16, own + s * 8 * group);
             } else {
                 constexpr int kPiece = 4 * sizeof(T);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    if (at + q * step >= N) break;
-                    const uint32_t dst = smem_u32(to) + ((2 * s + q) * kThreads + threadIdx.x) * kPiece;
-                    if constexpr (kPiece == 16) copy16(dst, row + at + q * step, 16);
-                    else copy8(dst, row + at + q * step);
+                    const uint32_t dst = to + ((2 * s + q) * kThreads + threadIdx.x) * kPiece;
+                    const T *src = own + s * 8 * group + q * 4 * group;
+                    if (s * 8 * group + q * 4 * group >= left) continue;
+                    if constexpr (kPiece == 16) copy16(dst, src);
+                    else copy8(dst, src);
                 }
             }
         }
     }
 }
-// slot s of the thread out of a copied row (`row`: where it lies in global memory, which says where it lies in its buffer)
+// slot s of the thread out of a copied row (`own`: where it lies in global memory, which says where it lies in its buffer)
 template <class T, Layout L, int kThreads>
-__device__ __forceinline__ void take(const char *from, const T *row, int s, int t, int group, int N, Eight<T, L> &e)
+__device__ __forceinline__ void take(const char *from, const T *own, int s, int t, int group, int N, Eight<T, L> &e)
 {
-    const int at = first_column<L>(s, t, group), step = step_of<L>(group);
     if constexpr (L == kOne) {
-        const T *p = reinterpret_cast<const T *>(from + threadIdx.x / group * tensor_bytes(kOne, sizeof(T), 0, 0, 1, N) + (reinterpret_cast<uintptr_t>(row) & 15));
+        const int left = N - t - s * 8 * group;
+        const T *p = reinterpret_cast<const T *>(from + threadIdx.x / group * row_bytes(sizeof(T), N) + (reinterpret_cast<uintptr_t>(own - t) & 15)) + t + s * 8 * group;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e.e[j] = at + j * step < N ? p[at + j * step] : from_f32<T>(0.f);
+        for (int j = 0; j < 8; ++j) e.e[j] = j * group < left ? p[j * group] : from_f32<T>(0.f);
     } else if constexpr (L == kEights) {
         e.q[0] = *reinterpret_cast<const uint4 *>(from + (s * kThreads + threadIdx.x) * 16);
     } else {
@@ -133,16 +123,17 @@ __device__ __forceinline__ void take(const char *from, const T *row, int s, int 
         const Quad *p = reinterpret_cast<const Quad *>(from) + 2 * s * kThreads + threadIdx.x;
         e.a = p[0];
         e.b = Quad{};
-        if (at + step < N) e.b = p[kThreads];
+        if (s * 8 * group + 4 * group < N - 4 * t) e.b = p[kThreads];
     }
 }
 __device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kOpen>
 __device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(kOpen) : "memory"); }
 // the threads of a row meet
-__device__ __forceinline__ void row_barrier(int group)
+template <int G>
+__device__ __forceinline__ void row_barrier()
 {
-    if (group <= 32) __syncwarp();
+    if constexpr (G <= 32) __syncwarp();
     else __syncthreads();
 }
 
@@ -153,30 +144,36 @@ __device__ __forceinline__ float both(f32x2 v)
     return a + b;
 }
 
-// Sums of two values over the `group` threads of a row, the same in each of them, in a fixed order.  `turn` alternates between calls (a
+// Sums of one or two values over the threads of a row, the same in each of them, in a fixed order.  `turn` alternates between calls (a
 // buffer is written again only behind the barrier of the call between).
+template <int G, bool kTwo>
 __device__ __forceinline__ void row_sums(float &a, float &b, int group, float2 (*buf)[32], int &turn)
 {
-    const int in_warp = group < 32 ? group : 32;
-    for (int o = in_warp >> 1; o > 0; o >>= 1) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if ((G ? G : group) <= o) continue;
         a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
+        if (kTwo) b += __shfl_xor_sync(0xffffffffu, b, o);
     }
-    if (group <= 32) return;
-    const int warp = threadIdx.x >> 5, per_row = group >> 5;
-    if ((threadIdx.x & 31) == 0) buf[turn][warp] = make_float2(a, b);
-    __syncthreads();
-    const float2 *mine = &buf[turn][warp & ~(per_row - 1)];
-    a = b = 0.f;
-    for (int q = 0; q < per_row; ++q) {
-        a += mine[q].x;
-        b += mine[q].y;
+    if constexpr (G > 32) {
+        constexpr int kPerRow = G / 32;
+        const int warp = threadIdx.x >> 5;
+        if ((threadIdx.x & 31) == 0) buf[turn][warp] = make_float2(a, b);
+        __syncthreads();
+        const float2 *mine = &buf[turn][warp & ~(kPerRow - 1)];
+        a = mine[0].x;
+        b = mine[0].y;
+#pragma unroll
+        for (int q = 1; q < kPerRow; ++q) {
+            a += mine[q].x;
+            if (kTwo) b += mine[q].y;
+        }
+        turn ^= 1;
     }
-    turn ^= 1;
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
-// Threads of a row (a power of two), eights of columns that a thread holds, threads of a block and rows of it side by side.
+// Threads of a row (a power of two) that hold `slots` eights of columns each, threads of a block (`least` or more) and rows of it side by side.
 struct NormLayout {
     int group, threads, slots, rows;
 };
@@ -205,11 +202,11 @@ struct Access {
     Layout layout() const { return all_bf16 && eights ? kEights : quads ? kQuads : kOne; }
 };
 
-// calls f(layout, slots, threads) with its arguments as compile-time constants
-template <Layout L, int kSlots, int kThreads, class F>
+// calls f(layout, slots, threads, group) with its arguments as compile-time constants
+template <Layout L, int kSlots, int kThreads, int G, class F>
 cudaError_t call(F f)
 {
-    return f(std::integral_constant<Layout, L>{}, std::integral_constant<int, kSlots>{}, std::integral_constant<int, kThreads>{});
+    return f(std::integral_constant<Layout, L>{}, std::integral_constant<int, kSlots>{}, std::integral_constant<int, kThreads>{}, std::integral_constant<int, G>{});
 }
 template <class T>
 struct Type {
@@ -220,14 +217,7 @@ cudaError_t with_type(int dtype, F f) { return dtype == RR_F32 ? f(Type<float>{}
 
 constexpr int kMostShared = 226 << 10;  // for the rows (beside a little of the kernels' own)
 
-// `smem` bytes of dynamic shared memory for a kernel
-template <class K>
-cudaError_t allow(K kernel, size_t smem)
-{
-    return smem <= 40 << 10 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-}
-
-inline NormArgs norm_args(const rr_norm_shape &s, const NormLayout &l)
+inline NormArgs norm_args(const rr_norm_shape &s, const NormLayout &l, int blocks)
 {
     NormArgs a = {};
     a.M = s.M;
@@ -236,13 +226,14 @@ inline NormArgs norm_args(const rr_norm_shape &s, const NormLayout &l)
     a.layer = s.kind == RR_NORM_LAYER;
     a.eps = s.eps;
     a.inv_n = 1.0f / (float)s.N;
-    a.ldx = s.ldx;
-    a.ldr = s.ldr;
-    a.ldh = s.ldh;
-    a.ldy = s.ldy;
-    a.lddy = s.lddy;
-    a.lddh = s.lddh;
-    a.lddx = s.lddx;
+    a.stride = (long long)blocks * l.rows;
+    a.sx = a.stride * (a.ldx = s.ldx);
+    a.sr = a.stride * (a.ldr = s.ldr);
+    a.sh = a.stride * (a.ldh = s.ldh);
+    a.sy = a.stride * (a.ldy = s.ldy);
+    a.sdy = a.stride * (a.lddy = s.lddy);
+    a.sdh = a.stride * (a.lddh = s.lddh);
+    a.sdx = a.stride * (a.lddx = s.lddx);
     a.w_f32 = s.w_dtype == RR_F32;
     return a;
 }

@@ -9,66 +9,93 @@ constexpr int bwd_blocks(int threads) { return threads == 256 ? 2 : 1; }  // an 
 
 // A block takes every gridDim-th set of rows and keeps the sums of its columns over them in registers.  With four eights a thread there are no
 // registers left to keep a row's numbers: they are worked out a second time.  TD: type of dx and dh.
-template <class TY, class TH, class TD, Layout L, int kSlots, int kThreads>
+template <class TY, class TH, class TD, Layout L, int kSlots, int kThreads, int G>
 __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(const NormArgs a)
 {
     constexpr bool kHold = kSlots == 2;
     extern __shared__ __align__(16) char ring[];  // [2] dy, h, dh; afterwards the sums of the block's rows side by side
     __shared__ float2 buf[2][32];
     dependent_start();
-    const int t = threadIdx.x & (a.group - 1), step = step_of<L>(a.group), rows = kThreads / a.group;
-    const long long stride = (long long)gridDim.x * rows;
-    long long row = (long long)blockIdx.x * rows + threadIdx.x / a.group;
+    const int group = G ? G : a.group, rows = kThreads / group, t = threadIdx.x & (group - 1), step = step_of<L>(group), col = first_column<L>(t);
+    long long row = (long long)blockIdx.x * rows + threadIdx.x / group;
     const int h_at = tensor_bytes(L, sizeof(TY), kSlots, kThreads, rows, a.N), d_at = h_at + tensor_bytes(L, sizeof(TH), kSlots, kThreads, rows, a.N);
     const int stage_bytes = d_at + (a.dh ? tensor_bytes(L, sizeof(TD), kSlots, kThreads, rows, a.N) : 0);
-    auto request = [&](long long r, char *to) {
+    const uint32_t ring_at = smem_u32(ring);
+    // the thread's first column in the present rows
+    const TY *py = static_cast<const TY *>(a.dy) + row * a.lddy + col;
+    const TH *ph = static_cast<const TH *>(a.h) + row * a.ldh + col;
+    const TD *pd = static_cast<const TD *>(a.dh) + row * a.lddh + col;
+    TD *px = static_cast<TD *>(a.dx) + row * a.lddx + col;
+    auto request = [&](long long r, const TY *y, const TH *h, const TD *d, int stage) {
         if (r < a.M) {
-            copy_row<TY, L, kSlots, kThreads>(to, static_cast<const TY *>(a.dy) + r * a.lddy, t, a.group, a.N);
-            copy_row<TH, L, kSlots, kThreads>(to + h_at, static_cast<const TH *>(a.h) + r * a.ldh, t, a.group, a.N);
-            if (a.dh) copy_row<TD, L, kSlots, kThreads>(to + d_at, static_cast<const TD *>(a.dh) + r * a.lddh, t, a.group, a.N);
+            const uint32_t to = ring_at + stage * stage_bytes;
+            copy_row<TY, L, kSlots, kThreads>(to, y, t, group, a.N);
+            copy_row<TH, L, kSlots, kThreads>(to + h_at, h, t, group, a.N);
+            if (a.dh) copy_row<TD, L, kSlots, kThreads>(to + d_at, d, t, group, a.N);
         }
         copies_asked();
     };
-    if (a.ahead) request(row, ring);
+    if (a.ahead) request(row, py, ph, pd, 0);
+    float mean = 0.f, rstd = 0.f;
+    if (row < a.M) {
+        if (a.layer) mean = __ldg(a.mean + row);
+        rstd = __ldg(a.rstd + row);
+    }
     f32x2 aw[kSlots][4], ab[kSlots][4];
 #pragma unroll
     for (int s = 0; s < kSlots; ++s)
 #pragma unroll
         for (int j = 0; j < 4; ++j) aw[s][j] = ab[s][j] = pack2(0.f, 0.f);
     int turn = 0, stage = 0;
-    for (long long first = (long long)blockIdx.x * rows; first < a.M; first += stride, row += stride) {
+    for (long long first = (long long)blockIdx.x * rows; first < a.M; first += a.stride) {
         const bool in = row < a.M;
-        const float mean = in && a.layer ? __ldg(a.mean + row) : 0.f, rstd = in ? __ldg(a.rstd + row) : 0.f;
         const char *here = ring + stage * stage_bytes;
         if (a.ahead) {
-            stage ^= 1;
-            if (L == kOne) {  // (the rows of the other buffer have been read by all, these have come for all)
+            stage = a.ahead == 2 ? stage ^ 1 : 0;
+            if (L == kOne || a.ahead == 1) {
                 copies_arrived<0>();
-                row_barrier(a.group);
-                request(row + stride, ring + stage * stage_bytes);
-            } else {
-                request(row + stride, ring + stage * stage_bytes);
-                copies_arrived<1>();
+                if (L == kOne) row_barrier<G>();  // (the rows of the other buffer have been read by all, these have come for all)
             }
+            if (a.ahead == 2) request(row + a.stride, py + a.sdy, ph + a.sh, pd + a.sdh, stage);
+            if (L != kOne && a.ahead == 2) copies_arrived<1>();
         }
-        const TY *py = static_cast<const TY *>(a.dy) + row * a.lddy;
-        const TH *ph = static_cast<const TH *>(a.h) + row * a.ldh;
-        const TD *pd = static_cast<const TD *>(a.dh) + row * a.lddh;
         const f32x2 centre = pack2(-mean, -mean), factor = pack2(rstd, rstd);
-        // the numbers of slot s: dy, xh and the weight (behind the row: dy is 0, and so is all that is made of it)
-        auto numbers = [&](int s, int at, f32x2 (&y)[4], f32x2 (&x)[4], f32x2 (&w)[4]) {
+        mean = rstd = 0.f;
+        if (row + a.stride < a.M) {  // (of the next row)
+            if (a.layer) mean = __ldg(a.mean + row + a.stride);
+            rstd = __ldg(a.rstd + row + a.stride);
+        }
+        // the numbers of slot s: dy, xh and dy w (behind the row: dy is 0, and so is all that is made of it)
+        auto numbers = [&](int s, f32x2 (&y)[4], f32x2 (&x)[4], f32x2 (&g)[4]) {
+            const int left = a.N - col - s * 8 * group;
             Eight<TY, L> ey;
             Eight<TH, L> eh;
             if (a.ahead) {
-                take<TY, L, kThreads>(here, py, s, t, a.group, a.N, ey);
-                take<TH, L, kThreads>(here + h_at, ph, s, t, a.group, a.N, eh);
+                take<TY, L, kThreads>(here, py, s, t, group, a.N, ey);
+                take<TH, L, kThreads>(here + h_at, ph, s, t, group, a.N, eh);
             } else {
-                ey.load(py + at, step, a.N - at);
-                eh.load(ph + at, step, a.N - at);
+                ey.load(py + s * 8 * group, step, left);
+                eh.load(ph + s * 8 * group, step, left);
             }
-            parameter<L>(a.w, a.w_f32, at, step, a.N - at, 1.f, w);
             ey.get(y);
             eh.get(x);
+            if (!a.w) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[j] = y[j];
+            } else {
+                f32x2 w[4];
+                if (a.w_f32) {
+                    Eight<float, L> e;
+                    e.template load<kConst>(static_cast<const float *>(a.w) + col + s * 8 * group, step, left);
+                    e.get(w);
+                } else {
+                    Eight<bf16, L> e;
+                    e.template load<kConst>(static_cast<const bf16 *>(a.w) + col + s * 8 * group, step, left);
+                    e.get(w);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[j] = mul2(y[j], w[j]);
+            }
             if (a.layer) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = add2(x[j], centre);
@@ -80,55 +107,76 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
         if (in) {
 #pragma unroll
             for (int s = 0; s < kSlots; ++s) {
-                const int at = first_column<L>(s, t, a.group), k = kHold ? s : 0;
-                if (at >= a.N) break;
-                f32x2 w[4];
-                numbers(s, at, g[k], xh[k], w);
+                const int k = kHold ? s : 0;
+                if (col + s * 8 * group >= a.N) continue;
+                f32x2 y[4];
+                numbers(s, y, xh[k], g[k]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    aw[s][j] = fma2(g[k][j], xh[k][j], aw[s][j]);
-                    if (a.db) ab[s][j] = add2(ab[s][j], g[k][j]);
-                    g[k][j] = mul2(g[k][j], w[j]);
-                    if (a.layer) p1 = add2(p1, g[k][j]);
+                    aw[s][j] = fma2(y[j], xh[k][j], aw[s][j]);
                     p2 = fma2(g[k][j], xh[k][j], p2);
+                }
+                if (a.layer) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p1 = add2(p1, g[k][j]);
+                }
+                if (a.db) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ab[s][j] = add2(ab[s][j], y[j]);
                 }
             }
         }
-        if (!a.dx) continue;  // (not wanted)
-        float s1 = both(p1), s2 = both(p2);
-        row_sums(s1, s2, a.group, buf, turn);
-        if (!in) continue;
-        const f32x2 c1 = pack2(-s1 * a.inv_n, -s1 * a.inv_n), c2 = pack2(-s2 * a.inv_n, -s2 * a.inv_n);
+        if (a.dx) {
+            float s1 = both(p1), s2 = both(p2);
+            if (a.layer) row_sums<G, true>(s2, s1, group, buf, turn);
+            else row_sums<G, false>(s2, s1, group, buf, turn);
+            const f32x2 c1 = pack2(-s1 * a.inv_n, -s1 * a.inv_n), c2 = pack2(-s2 * a.inv_n, -s2 * a.inv_n);
+            if (in) {
 #pragma unroll
-        for (int s = 0; s < kSlots; ++s) {
-            const int at = first_column<L>(s, t, a.group), k = kHold ? s : 0;
-            if (at >= a.N) break;
-            if constexpr (!kHold) {
-                f32x2 w[4];
-                numbers(s, at, g[0], xh[0], w);
+                for (int s = 0; s < kSlots; ++s) {
+                    const int k = kHold ? s : 0, left = a.N - col - s * 8 * group;
+                    if (left <= 0) continue;
+                    if constexpr (!kHold) {
+                        f32x2 y[4];
+                        numbers(s, y, xh[0], g[0]);
+                    }
+                    Eight<TD, L> e;
+                    f32x2 d[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], w[j]);
-            }
-            Eight<TD, L> e;
-            f32x2 o[4];
-            if (a.dh) {
-                if (a.ahead) take<TD, L, kThreads>(here + d_at, pd, s, t, a.group, a.N, e);
-                else e.load(pd + at, step, a.N - at);
-                e.get(o);
-            }
+                    for (int j = 0; j < 4; ++j) d[j] = fma2(xh[k][j], c2, g[k][j]);
+                    if (a.layer) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f32x2 d = fma2(xh[k][j], c2, g[k][j]);
-                if (a.layer) d = add2(d, c1);
-                o[j] = a.dh ? fma2(d, factor, o[j]) : mul2(d, factor);
+                        for (int j = 0; j < 4; ++j) d[j] = add2(d[j], c1);
+                    }
+                    if (a.dh) {
+                        f32x2 o[4];
+                        if (a.ahead) take<TD, L, kThreads>(here + d_at, pd, s, t, group, a.N, e);
+                        else e.load(pd + s * 8 * group, step, left);
+                        e.get(o);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) d[j] = fma2(d[j], factor, o[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) d[j] = mul2(d[j], factor);
+                    }
+                    e.set(d);
+                    e.store(px + s * 8 * group, step, left);
+                }
             }
-            e.set(o);
-            e.store(static_cast<TD *>(a.dx) + row * a.lddx + at, step, a.N - at);
         }
+        if (a.ahead == 1) {  // one buffer: the next row comes when this one has been read
+            if (L == kOne) row_barrier<G>();
+            request(row + a.stride, py + a.sdy, ph + a.sh, pd + a.sdh, 0);
+        }
+        row += a.stride;
+        py += a.sdy;
+        ph += a.sh;
+        pd += a.sdh;
+        px += a.sdx;
     }
     if (!a.dw && !a.db) return;
     // The sums of the rows side by side: of a warp by exchange (every lane adds the same pairs in the same order), of the block through shared memory
-    for (int o = a.group; o < 32; o <<= 1) {
+    for (int o = group; o < 32; o <<= 1) {
 #pragma unroll
         for (int s = 0; s < kSlots; ++s)
 #pragma unroll
@@ -138,12 +186,12 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
             }
     }
     const size_t part = (size_t)blockIdx.x * a.N;
-    const int sets = kThreads / (a.group < 32 ? 32 : a.group);
+    const int sets = kThreads / (group < 32 ? 32 : group);
     if (sets == 1) {
 #pragma unroll
         for (int s = 0; s < kSlots; ++s) {
-            const int at = first_column<L>(s, t, a.group);
-            if (at >= a.N) break;
+            const int at = col + s * 8 * group;
+            if (at >= a.N) continue;
             float *const out[2] = {a.dw, a.db};
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -168,12 +216,12 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
     copies_arrived<0>();
     __syncthreads();  // (nobody reads rows any more)
     float *const sums = reinterpret_cast<float *>(ring);  // [sets][2][N]
-    const int set = threadIdx.x / (a.group < 32 ? 32 : a.group);
-    if ((threadIdx.x & 31) < a.group) {
+    const int set = threadIdx.x / (group < 32 ? 32 : group);
+    if (group >= 32 || (int)(threadIdx.x & 31) < group) {
 #pragma unroll
         for (int s = 0; s < kSlots; ++s) {
-            const int at = first_column<L>(s, t, a.group);
-            if (at >= a.N) break;
+            const int at = col + s * 8 * group;
+            if (at >= a.N) continue;
             Eight<float, kOne> e;  // (element by element: a row of sums starts anywhere)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -199,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
 }
 
 // out[c] (+)= sum of the blocks' parts of column c, in a fixed order: a thread adds up every kLanes-th part, then the lanes are added in turn
-constexpr int kFoldLanes = 16;
+constexpr int kFoldLanes = 32;
 __global__ void __launch_bounds__(32 * kFoldLanes) k_norm_fold(int blocks, int N, const float *pw, const float *pb, float *dw, float *db, int add)
 {
     __shared__ float red[kFoldLanes][33];
@@ -236,9 +284,15 @@ int bwd_parts(int M, int N)
 template <Layout L, class F>
 cudaError_t with_layout(const NormLayout &l, F f)
 {
-    if (l.threads == 256) return call<L, 2, 256>(f);
-    if (l.threads == 1024) return call<L, 4, 1024>(f);
-    return l.slots == 2 ? call<L, 2, 512>(f) : call<L, 4, 512>(f);
+    switch (l.group) {
+    case 32: return call<L, 2, 256, 32>(f);
+    case 64: return call<L, 2, 256, 64>(f);
+    case 128: return call<L, 2, 256, 128>(f);
+    case 256: return call<L, 2, 256, 256>(f);
+    case 512: return l.slots == 2 ? call<L, 2, 512, 512>(f) : call<L, 4, 512, 512>(f);
+    case 1024: return call<L, 4, 1024, 1024>(f);
+    default: return call<L, 2, 256, 0>(f);
+    }
 }
 
 }  // namespace
@@ -256,7 +310,8 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
     if (!dh && !dx) access.all_bf16 = access.all_bf16 && s.dx_dtype == RR_BF16;  // (its kernels are of that type all the same)
     const Layout L = access.layout();
     const NormLayout l = bwd_layout(s.N);
-    NormArgs a = norm_args(s, l);
+    const int parts = bwd_parts(s.M, s.N), add = (s.flags & RR_ADD_DW) != 0;
+    NormArgs a = norm_args(s, l, parts);
     a.dy = dy;
     a.h = const_cast<void *>(h);
     a.w = w;
@@ -264,7 +319,6 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
     a.rstd = const_cast<float *>(rstd);
     a.dh = dh;
     a.dx = dx;
-    const int parts = bwd_parts(s.M, s.N), add = (s.flags & RR_ADD_DW) != 0;
     const bool fold = parts > 1 && (dw || db);
     Carver c(workspace);
     c.take<Header>(1);
@@ -273,9 +327,10 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
     a.db = db ? (fold ? pb : db) : nullptr;
     a.add = fold ? 0 : add;
     auto bytes = [&](int dtype) { return tensor_bytes(L, dtype == RR_F32 ? 4 : 2, l.slots, l.threads, l.rows, s.N); };
-    int smem = 2 * (bytes(s.y_dtype) + bytes(s.h_dtype) + (dh ? bytes(s.dx_dtype) : 0));
-    a.ahead = (long long)s.M > (long long)parts * l.rows && smem <= kMostShared / bwd_blocks(l.threads);  // (a block with one set of rows has nothing to fetch ahead)
-    if (!a.ahead) smem = 0;
+    const int row = bytes(s.y_dtype) + bytes(s.h_dtype) + (dh ? bytes(s.dx_dtype) : 0), room = kMostShared / bwd_blocks(l.threads);
+    // (a block with one set of rows has nothing to fetch ahead)
+    a.ahead = (long long)s.M <= (long long)parts * l.rows ? 0 : 2 * row <= room ? 2 : row <= room ? 1 : 0;
+    int smem = a.ahead * row;
     const int sets = l.threads / (l.group < 32 ? 32 : l.group), sums = sets > 1 ? sets * 2 * s.N * 4 : 0;  // (32 KB at most)
     if (smem < sums) smem = sums;
     cudaError_t err = with_type(s.y_dtype, [&](auto ty) {
@@ -284,9 +339,10 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
                 using TY = typename decltype(ty)::type;
                 using TH = typename decltype(th)::type;
                 using TD = typename decltype(td)::type;
-                auto go = [&](auto layout, auto slots, auto threads) {
-                    auto kernel = k_norm_bwd<TY, TH, TD, layout(), slots(), threads()>;
-                    const cudaError_t e = allow(kernel, smem);
+                auto go = [&](auto layout, auto slots, auto threads, auto group) {
+                    auto kernel = k_norm_bwd<TY, TH, TD, layout(), slots(), threads(), group()>;
+                    static SharedAllowance allowance;
+                    const cudaError_t e = allowance.ask(kernel, smem);
                     return e != cudaSuccess ? e : launch_dependent(kernel, dim3(parts), threads(), (size_t)smem, 1, st, a);
                 };
                 if constexpr (sizeof(TY) + sizeof(TH) + sizeof(TD) == 6) {

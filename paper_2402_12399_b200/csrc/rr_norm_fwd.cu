@@ -5,63 +5,58 @@ namespace rr {
 
 namespace {
 
-constexpr int fwd_blocks(int threads) { return threads == 128 ? 6 : threads == 256 ? 3 : threads == 512 ? 2 : 1; }  // an SM
+constexpr int fwd_blocks(int threads, int slots) { return (slots == 2 || threads > 256 ? 1024 : 768) / threads; }  // an SM
+
+// v w + b of eight columns from `at` on (w and b come from the L1 cache: a block meets the same columns in every row)
+template <class TW, Layout L>
+__device__ __forceinline__ void apply(const NormArgs &a, int at, int step, f32x2 (&v)[4])
+{
+    Eight<TW, L> e;
+    f32x2 p[4];
+    if (a.w) {
+        e.template load<kConst>(static_cast<const TW *>(a.w) + at, step, a.N - at);
+        e.get(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], p[j]);
+    }
+    if (a.b) {
+        e.template load<kConst>(static_cast<const TW *>(a.b) + at, step, a.N - at);
+        e.get(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = add2(v[j], p[j]);
+    }
+}
 
 // TH: type of the residual stream, void without one
-template <class TX, class TH, class TY, Layout L, int kSlots, int kThreads>
-__global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads)) k_norm_fwd(const NormArgs a)
+template <class TX, class TH, class TY, Layout L, int kSlots, int kThreads, int G>
+__global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm_fwd(const NormArgs a)
 {
     constexpr bool kRes = !std::is_same<TH, void>::value;
     using TR = std::conditional_t<kRes, TH, float>;
-    extern __shared__ __align__(16) char ring[];  // [2] x, then residual
     __shared__ float2 buf[2][32];
     dependent_start();
-    const int t = threadIdx.x & (a.group - 1), step = step_of<L>(a.group), rows = kThreads / a.group;
-    const long long stride = (long long)gridDim.x * rows;
-    long long row = (long long)blockIdx.x * rows + threadIdx.x / a.group;
-    const int residual_at = tensor_bytes(L, sizeof(TX), kSlots, kThreads, rows, a.N);
-    const int stage_bytes = residual_at + (kRes ? tensor_bytes(L, sizeof(TR), kSlots, kThreads, rows, a.N) : 0);
-    auto request = [&](long long r, char *to) {
-        if (r < a.M) {
-            copy_row<TX, L, kSlots, kThreads>(to, static_cast<const TX *>(a.x) + r * a.ldx, t, a.group, a.N);
-            if (kRes) copy_row<TR, L, kSlots, kThreads>(to + residual_at, static_cast<const TR *>(a.residual) + r * a.ldr, t, a.group, a.N);
-        }
-        copies_asked();
-    };
-    if (a.ahead) request(row, ring);
-    int turn = 0, stage = 0;
-    for (long long first = (long long)blockIdx.x * rows; first < a.M; first += stride, row += stride) {
+    const int group = G ? G : a.group, rows = kThreads / group, t = threadIdx.x & (group - 1), step = step_of<L>(group), col = first_column<L>(t);
+    long long row = (long long)blockIdx.x * rows + threadIdx.x / group;
+    const TX *px = static_cast<const TX *>(a.x) + row * a.ldx + col;
+    const TR *pr = static_cast<const TR *>(a.residual) + row * a.ldr + col;
+    TR *ph = static_cast<TR *>(a.h) + row * a.ldh + col;
+    TY *py = static_cast<TY *>(a.y) + row * a.ldy + col;
+    int turn = 0;
+    for (long long first = (long long)blockIdx.x * rows; first < a.M; first += a.stride) {
         const bool in = row < a.M;
         f32x2 v[kSlots][4];
         {
             Eight<TX, L> ex[kSlots];
             Eight<TR, L> er[kSlots];
-            const char *here = ring + stage * stage_bytes;
-            if (a.ahead) {
-                stage ^= 1;
-                if (L == kOne) {  // (the rows of the other buffer have been read by all, these have come for all)
-                    copies_arrived<0>();
-                    row_barrier(a.group);
-                    request(row + stride, ring + stage * stage_bytes);
-                } else {
-                    request(row + stride, ring + stage * stage_bytes);
-                    copies_arrived<1>();
-                }
-            }
-            const TX *px = static_cast<const TX *>(a.x) + row * a.ldx;
-            const TR *pr = static_cast<const TR *>(a.residual) + row * a.ldr;
 #pragma unroll
             for (int s = 0; s < kSlots; ++s) {
-                const int at = first_column<L>(s, t, a.group);
-                if (!in || at >= a.N) {
+                const int left = a.N - col - s * 8 * group;
+                if (!in || left <= 0) {
                     ex[s].zero();
                     if (kRes) er[s].zero();
-                } else if (a.ahead) {
-                    take<TX, L, kThreads>(here, px, s, t, a.group, a.N, ex[s]);
-                    if (kRes) take<TR, L, kThreads>(here + residual_at, pr, s, t, a.group, a.N, er[s]);
                 } else {
-                    ex[s].load(px + at, step, a.N - at);
-                    if (kRes) er[s].load(pr + at, step, a.N - at);
+                    ex[s].load(px + s * 8 * group, step, left);
+                    if (kRes) er[s].load(pr + s * 8 * group, step, left);
                 }
             }
 #pragma unroll
@@ -74,8 +69,8 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads)) k_norm_fwd(con
                     for (int j = 0; j < 4; ++j) v[s][j] = add2(v[s][j], r[j]);
                     er[s].set(v[s]);
                     er[s].get(v[s]);  // the norm is that of the stream as it is stored
-                    const int at = first_column<L>(s, t, a.group);
-                    if (a.h && in && at < a.N) er[s].store(static_cast<TR *>(a.h) + row * a.ldh + at, step, a.N - at);
+                    const int left = a.N - col - s * 8 * group;
+                    if (a.h && in && left > 0) er[s].store(ph + s * 8 * group, step, left);
                 }
             }
         }
@@ -87,7 +82,7 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads)) k_norm_fwd(con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum = add2(sum, v[s][j]);
             m = both(sum);
-            row_sums(m, d1, a.group, buf, turn);
+            row_sums<G, false>(m, d1, group, buf, turn);
             m *= a.inv_n;
             sum = pack2(0.f, 0.f);
             const f32x2 centre = pack2(-m, -m);
@@ -95,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads)) k_norm_fwd(con
             for (int s = 0; s < kSlots; ++s) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[s][j] = add2(v[s][j], centre);
-                cut<L>(v[s], first_column<L>(s, t, a.group), step, a.N);
+                cut<L>(v[s], step, a.N - col - s * 8 * group);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum = add2(sum, v[s][j]);
             }
@@ -107,47 +102,81 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads)) k_norm_fwd(con
 #pragma unroll
             for (int j = 0; j < 4; ++j) square = fma2(v[s][j], v[s][j], square);
         d2 = both(square);
-        row_sums(d1, d2, a.group, buf, turn);
+        if (a.layer) row_sums<G, true>(d2, d1, group, buf, turn);
+        else row_sums<G, false>(d2, d1, group, buf, turn);
         // what rounding left of the mean is in d1 (a row far from zero against its spread)
-        const float rest = d1 * a.inv_n;
+        const float rest = a.layer ? d1 * a.inv_n : 0.f;
         const float rstd = __frsqrt_rn(fmaxf(fmaf(d2, a.inv_n, -rest * rest), 0.f) + a.eps);
-        if (!in) continue;
-        if (t == 0) {
-            if (a.mean) a.mean[row] = m + rest;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        const f32x2 factor = pack2(rstd, rstd), shift = pack2(-rest * rstd, -rest * rstd);
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) {
-            const int at = first_column<L>(s, t, a.group);
-            if (at >= a.N) break;
-            f32x2 w[4];
-            parameter<L>(a.w, a.w_f32, at, step, a.N - at, 1.f, w);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[s][j] = mul2(fma2(v[s][j], factor, shift), w[j]);
-            if (a.b) {
-                parameter<L>(a.b, a.w_f32, at, step, a.N - at, 0.f, w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[s][j] = add2(v[s][j], w[j]);
+        if (in) {
+            if (t == 0) {
+                if (a.mean) a.mean[row] = m + rest;
+                if (a.rstd) a.rstd[row] = rstd;
             }
-            Eight<TY, L> e;
-            e.set(v[s]);
-            e.store(static_cast<TY *>(a.y) + row * a.ldy + at, step, a.N - at);
+            const f32x2 factor = pack2(rstd, rstd), shift = pack2(-rest * rstd, -rest * rstd);
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) {
+                const int at = col + s * 8 * group;
+                if (at >= a.N) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[s][j] = fma2(v[s][j], factor, shift);
+                if (a.w_f32) apply<float, L>(a, at, step, v[s]);
+                else apply<bf16, L>(a, at, step, v[s]);
+                Eight<TY, L> e;
+                e.set(v[s]);
+                e.store(py + s * 8 * group, step, a.N - at);
+            }
+        }
+        row += a.stride;
+        px += a.sx;
+        py += a.sy;
+        if (kRes) {
+            pr += a.sr;
+            ph += a.sh;
         }
     }
 }
 
-// Four eights a thread, which has its registers for one row; two where elements go one by one, if that is enough.
-NormLayout fwd_layout(int N, Layout L) { return norm_layout(N, L == kOne && N <= 16384 ? 2 : 4, 128); }
+// Two eights a thread, or four: one matrix to read and rows enough to fill the SMs want more of it in flight (65536 x 1024 in bf16 48 us instead of 52), and a
+// row beyond 4096 columns fewer threads that meet (8192 x 8192 52 us instead of 67).
+NormLayout fwd_layout(int M, int N, Layout L, bool residual, int sms)
+{
+    NormLayout l = norm_layout(N, 2, 128);
+    const bool fills = (long long)M > (long long)sms * fwd_blocks(l.threads, 2) * l.rows;
+    if (N > 16384 || (L != kOne && N > 4096) || (L == kEights && !residual && fills)) l = norm_layout(N, 4, 128);
+    return l;
+}
 
 template <Layout L, class F>
 cudaError_t with_layout(const NormLayout &l, F f)
 {
-    constexpr int kSlots = L == kOne ? 2 : 4;
-    if (l.threads == 128) return call<L, kSlots, 128>(f);
-    if (l.threads == 256) return call<L, kSlots, 256>(f);
-    if (l.threads == 512) return call<L, kSlots, 512>(f);
-    return l.slots == 4 ? call<L, 4, 1024>(f) : call<L, kSlots, 1024>(f);
+    if (l.slots == 2) {
+        switch (l.group) {
+        case 32: return call<L, 2, 128, 32>(f);
+        case 64: return call<L, 2, 128, 64>(f);
+        case 128: return call<L, 2, 128, 128>(f);
+        case 256: return call<L, 2, 256, 256>(f);
+        default:
+            if constexpr (L == kOne) {
+                if (l.group == 512) return call<L, 2, 512, 512>(f);
+                if (l.group == 1024) return call<L, 2, 1024, 1024>(f);
+            }
+            return call<L, 2, 128, 0>(f);
+        }
+    }
+    if constexpr (L != kOne) {
+        if (l.group == 256) return call<L, 4, 256, 256>(f);
+        if (l.group == 512) return call<L, 4, 512, 512>(f);
+    }
+    if constexpr (L == kEights) {
+        switch (l.group) {
+        case 32: return call<L, 4, 128, 32>(f);
+        case 64: return call<L, 4, 128, 64>(f);
+        case 128: return call<L, 4, 128, 128>(f);
+        default:
+            if (l.group < 32) return call<L, 4, 128, 0>(f);
+        }
+    }
+    return call<L, 4, 1024, 1024>(f);
 }
 
 }  // namespace
@@ -161,8 +190,15 @@ rr_status launch_norm_fwd(const rr_norm_shape &s, const void *x, const void *res
     access.matrix(h, s.h_dtype, s.ldh);
     access.matrix(y, s.y_dtype, s.ldy);
     const Layout L = access.layout();
-    const NormLayout l = fwd_layout(s.N, L);
-    NormArgs a = norm_args(s, l);
+    const int sms = device_sm_count();
+    if (sms < 1) return RR_ERR_CUDA;
+    const NormLayout l = fwd_layout(s.M, s.N, L, residual != nullptr, sms);
+    const long long sets = ((long long)s.M + l.rows - 1) / l.rows;
+    // Blocks far beyond those resident: each is short, so that they drift apart and reads and writes mix, and the last ones leave few SMs idle
+    // (16384 x 4096, fp32 + bf16 residual: 111 us with the resident ones, 99 so).
+    const long long most = (long long)sms * 32;
+    const dim3 grid((unsigned)(sets < most ? sets : most));
+    NormArgs a = norm_args(s, l, grid.x);
     a.x = x;
     a.residual = residual;
     a.w = w;
@@ -171,24 +207,12 @@ rr_status launch_norm_fwd(const rr_norm_shape &s, const void *x, const void *res
     a.y = y;
     a.mean = a.layer ? mean : nullptr;
     a.rstd = rstd;
-    const int sms = device_sm_count();
-    if (sms < 1) return RR_ERR_CUDA;
-    const long long sets = ((long long)s.M + l.rows - 1) / l.rows;
-    int smem = 2 * (tensor_bytes(L, s.x_dtype == RR_F32 ? 4 : 2, l.slots, l.threads, l.rows, s.N) +
-                    (residual ? tensor_bytes(L, s.h_dtype == RR_F32 ? 4 : 2, l.slots, l.threads, l.rows, s.N) : 0));
-    int per_sm = fwd_blocks(l.threads);
-    a.ahead = sets > (long long)sms * per_sm && smem <= kMostShared;  // (a block with one set of rows has nothing to fetch ahead)
-    if (!a.ahead) smem = 0;
-    while (per_sm > 1 && per_sm * (smem + 1024) > kMostShared) --per_sm;
-    const dim3 grid((unsigned)(sets < (long long)sms * per_sm ? sets : (long long)sms * per_sm));
     auto types = [&](auto tx, auto th, auto ty) {
         using TX = typename decltype(tx)::type;
         using TH = typename decltype(th)::type;
         using TY = typename decltype(ty)::type;
-        auto go = [&](auto layout, auto slots, auto threads) {
-            auto kernel = k_norm_fwd<TX, TH, TY, layout(), slots(), threads()>;
-            const cudaError_t err = allow(kernel, smem);
-            return err != cudaSuccess ? err : launch_dependent(kernel, grid, threads(), (size_t)smem, 1, st, a);
+        auto go = [&](auto layout, auto slots, auto threads, auto group) {
+            return launch_dependent(k_norm_fwd<TX, TH, TY, layout(), slots(), threads(), group()>, grid, threads(), 0, 1, st, a);
         };
         if constexpr (sizeof(TX) + sizeof(TY) == 4 && !std::is_same<TH, float>::value) {
             if (L == kEights) return with_layout<kEights>(l, go);
