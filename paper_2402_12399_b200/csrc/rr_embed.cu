@@ -6,6 +6,7 @@
 // kernel adds up in order: a frequent id costs no more than any other.  Rows that no token names are zeroed by blocks that run beside the
 // sort and learn of the named rows from a bitmap of their own.  Sums are fp32.
 #include <type_traits>
+#include <utility>
 
 #include "rr_ffn.cuh"
 #include "rr_vec.cuh"
@@ -53,11 +54,53 @@ __device__ __forceinline__ void token_ids(const EmbArgs &a, const long long (&to
     if (bad) latch_status(a.status, RR_ERR_INVALID_ARG);
 }
 
-// A block takes tiles of kTile units of the result (kN elements each), whatever the width of a row; row and place of a unit come from a
-// product, and those of the next tile from those of the last.
+// `units` units of kN elements, kStep units apart, at most kEmbUnroll of them: all read before the first is written.  live: y is a row of the table
+// and not of zeros.
 constexpr int kEmbUnroll = 4;
+template <class TX, class TY, int kN, int kStep>
+__device__ __forceinline__ void copy_units(const TX *from, TY *to, int units, bool live, float scale)
+{
+    Unit<TX, kN> e[kEmbUnroll];
+#pragma unroll
+    for (int u = 0; u < kEmbUnroll; ++u) {
+        e[u].raw = {};
+        if (live && u < units) e[u].template load<kKeep>(from + u * kStep * kN);
+    }
+#pragma unroll
+    for (int u = 0; u < kEmbUnroll; ++u) {
+        if (u >= units) break;
+        Unit<TY, kN> o;
+        if constexpr (std::is_same<TX, TY>::value) o.raw = e[u].raw;
+        if (scale != 1.0f || !std::is_same<TX, TY>::value) scaled<kN>(e[u], o, scale);
+        if (!live) o.raw = {};  // (not -0)
+        o.template store<kStream>(to + u * kStep * kN);
+    }
+}
+
+// Wide rows: a warp takes pieces of a row, 32 kEmbUnroll units each.  One look at the id and one division for four units a lane: the kernel
+// below, which divides for every unit, is bound by instructions (65536 x 1024 in bf16 30.5 us).
 template <class TX, class TY, int kN>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int per_row, unsigned long long magic, long long row_step, unsigned at_step)
+__global__ void __launch_bounds__(kEmbThreads) k_embed_rows(const EmbArgs a, int per_row, int pieces, unsigned long long magic)
+{
+    constexpr int kPiece = 32 * kEmbUnroll;
+    dependent_start();
+    const int lane = threadIdx.x & 31;
+    const long long items = a.n * pieces, step = (long long)gridDim.x * (kEmbThreads / 32);
+    for (long long item = (long long)blockIdx.x * (kEmbThreads / 32) + (threadIdx.x >> 5); item < items; item += step) {
+        const long long row = magic ? (long long)__umul64hi((unsigned long long)item, magic) : item;  // item / pieces (the host says why)
+        const int first = (int)(item - row * pieces) * kPiece + lane;
+        const long long token[1] = {row};
+        int id[1];
+        token_ids(a, token, a.n, id);
+        copy_units<TX, TY, kN, 32>(static_cast<const TX *>(a.in) + (long long)max(id[0], 0) * a.d + (long long)first * kN, static_cast<TY *>(a.out) + row * a.ld + (long long)first * kN,
+                                   (per_row - first + 31) / 32, id[0] >= 0, a.scale);
+    }
+}
+
+// Narrow rows: a block takes tiles of units, whatever the width of a row; row and place of a unit come from a product, and those of the next
+// tile from those of the last.
+template <class TX, class TY, int kN>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_units(const EmbArgs a, int per_row, unsigned long long magic, long long row_step, unsigned at_step)
 {
     constexpr int kTile = kEmbThreads * kEmbUnroll;
     dependent_start();
@@ -71,7 +114,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_fwd(const EmbArgs a, int 
 #pragma unroll
         for (int u = 0; u < kEmbUnroll; ++u) {
             const unsigned l = u * kEmbThreads + threadIdx.x, w = at0 + l;
-            const unsigned q = magic ? (unsigned)__umul64hi(w, magic) : w;  // w / per_row (the host says why)
+            const unsigned q = magic ? (unsigned)__umul64hi(w, magic) : w;  // w / per_row
             row[u] = row0 + q;
             at[u] = w - q * per_row;
         }
@@ -104,7 +147,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigitBits = 5, kDigits = 1 << kDigitBits; // at most
 constexpr int kSortMost = 16;                            // tokens a thread of a sorting block holds
-constexpr int kSlab = kSortThreads * kSortMost;          // tokens of a sorting block
+constexpr int kSlab = kSortThreads * kSortMost;          // tokens of a sorting block (20 us; four of 4096 and their merge take as long)
 constexpr int kPlaceBits = 14;                           // a token's place in its slab
 static_assert(kSlab <= 1 << kPlaceBits && kSortMost <= 16, "a place fits into its bits, a thread's count of a digit into four");
 constexpr int kTableWords = kDigits * (kSortThreads / 2 / 16 * 17);
@@ -253,40 +296,40 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
     }
 }
 
-// Sorted slabs into one order: a token's place is the number of tokens in front of it in every slab (equal ids: earlier slabs only).
-// Four slabs are searched side by side.
-__global__ void __launch_bounds__(kEmbThreads) k_embed_merge(long long n, int slabs, int slab, const int *__restrict__ key, const int *__restrict__ pos, int *out_key,
-                                                             int *out_pos)
+// Every kSide sorted slabs into one: a token's place is the number of tokens in front of it in each of them (equal ids: earlier slabs only).  The
+// slabs are searched side by side, all of a step's loads in flight together.
+template <int kSide>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_merge(int n, int slab, const int *__restrict__ key, const int *__restrict__ pos, int *out_key, int *out_pos)
 {
-    constexpr int kSide = 4;
     dependent_start();
-    const long long i = (long long)blockIdx.x * kEmbThreads + threadIdx.x;
+    const int i = blockIdx.x * kEmbThreads + threadIdx.x;
     if (i >= n) return;
-    const int mine = (int)(i / slab), id = __ldg(key + i);
-    const int token = __ldg(pos + i);
-    long long to = i - (long long)mine * slab;
-    int steps = 1;
+    const int mine = i / slab, first = mine / kSide * kSide, id = __ldg(key + i), token = __ldg(pos + i);
+    int to = i - (mine - first) * slab;  // (places are below 2^30)
+    int lo[kSide], hi[kSide], start[kSide], steps = 1;
     while (1 << steps <= slab) ++steps;
-    for (int s0 = 0; s0 < slabs; s0 += kSide) {
-        int lo[kSide], hi[kSide];
 #pragma unroll
-        for (int u = 0; u < kSide; ++u) {
-            const int s = s0 + u;
-            lo[u] = 0;
-            hi[u] = s < slabs && s != mine ? (int)min((long long)slab, n - (long long)s * slab) : 0;
-        }
-        for (int step = 0; step < steps; ++step) {
-#pragma unroll
-            for (int u = 0; u < kSide; ++u) {  // tokens of slab s below id, or in earlier slabs not above it
-                if (lo[u] >= hi[u]) continue;
-                const int mid = (lo[u] + hi[u]) >> 1, k = __ldg(key + (long long)(s0 + u) * slab + mid);
-                if (k < id || (k == id && s0 + u < mine)) lo[u] = mid + 1;
-                else hi[u] = mid;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kSide; ++u) to += lo[u];
+    for (int u = 0; u < kSide; ++u) {
+        const long long at = (long long)(first + u) * slab;
+        const bool other = at < n && first + u != mine;
+        start[u] = other ? (int)at : 0;
+        lo[u] = 0;
+        hi[u] = other ? (int)min((long long)slab, n - at) : 0;
     }
+    for (int step = 0; step < steps; ++step) {
+        int k[kSide];
+#pragma unroll
+        for (int u = 0; u < kSide; ++u) k[u] = __ldg(key + start[u] + min((lo[u] + hi[u]) >> 1, max(hi[u] - 1, 0)));
+#pragma unroll
+        for (int u = 0; u < kSide; ++u) {  // tokens of that slab below id, or in earlier slabs not above it
+            const int mid = (lo[u] + hi[u]) >> 1;
+            const bool before = k[u] < id || (k[u] == id && first + u < mine), open = lo[u] < hi[u];
+            if (open && before) lo[u] = mid + 1;
+            if (open && !before) hi[u] = mid;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) to += lo[u];
     out_key[to] = id;
     out_pos[to] = token;
 }
@@ -482,7 +525,7 @@ struct BwdLayout {
     int *key, *pos, *key2, *pos2, *runs, *list;
     float *part;
     long long chunks;
-    int slabs, slab, chunk;
+    int chunk;
 };
 size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
 {
@@ -492,14 +535,12 @@ size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
     l.chunk = kMostChunk;
     while (l.chunk > kLeastChunk && n * warps < 16384ll * l.chunk) l.chunk >>= 1;
     l.chunks = (n + l.chunk - 1) / l.chunk;
-    l.slabs = (int)((n + kSlab - 1) / kSlab);
-    l.slab = l.slabs ? (int)((n + l.slabs - 1) / l.slabs) : 0;
     Carver c(ws);
     l.hdr = c.take<Header>(1);
     l.key = c.take<int>(n);
     l.pos = c.take<int>(n);
-    l.key2 = l.slabs > 1 ? c.take<int>(n) : l.key;
-    l.pos2 = l.slabs > 1 ? c.take<int>(n) : l.pos;
+    l.key2 = n > kSlab ? c.take<int>(n) : l.key;
+    l.pos2 = n > kSlab ? c.take<int>(n) : l.pos;
     l.runs = c.take<int>(1);
     l.list = c.take<int>(n / (2 * l.chunk) + 1);
     l.part = c.take<float>(n > 2 * l.chunk ? (size_t)l.chunks * 2 * d : 0);
@@ -558,22 +599,32 @@ rr_status launch_embed_fwd(const rr_embed_shape &s, const void *ids, const void 
     const Layout L = layout_of(s);
     const int per_row = L == kEights ? s.d / 8 : L == kQuads ? s.d / 4 : s.d, sms = device_sm_count();
     if (sms < 1) return RR_ERR_CUDA;
-    // w / per_row is the high word of w * magic, magic = ceil(2^64 / per_row): what the rounding up adds to the quotient is below
-    // w / 2^64 < 2^-32, less than the 1 / per_row that would be missing to the next whole number.  (A divisor of one has no such factor.)
-    const unsigned long long magic = per_row == 1 ? 0 : ~0ull / (unsigned)per_row + 1;
-    const long long tiles = ((long long)s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll), most = (long long)sms * 16;
-    const dim3 grid((unsigned)(tiles < most ? tiles : most));
+    // i / q is the high word of i * magic, magic = ceil(2^64 / q), for i < 2^40 and q < 2^23 (there is no memory for more): what the rounding up adds to the quotient is below
+    // i / 2^64 < 2^-24, less than the 1 / q that would be missing to the next whole number.  (For i < 2^32: q < 2^31.)  A divisor of one has no such
+    // factor.
+    auto factor = [](int q) { return q == 1 ? 0 : ~0ull / (unsigned)q + 1; };
+    constexpr int kPiece = 32 * kEmbUnroll;
+    const int pieces = (per_row + kPiece - 1) / kPiece;
+    const bool wide = (long long)pieces * kPiece * 3 <= (long long)per_row * 4;  // (at most a quarter of a row's last piece is idle)
+    const long long blocks = wide ? ((long long)s.n * pieces + kEmbThreads / 32 - 1) / (kEmbThreads / 32)
+                                  : ((long long)s.n * per_row + kEmbThreads * kEmbUnroll - 1) / (kEmbThreads * kEmbUnroll);
+    const long long most = (long long)sms * 16;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
     const long long step = (long long)grid.x * kEmbThreads * kEmbUnroll, row_step = step / per_row;
     const unsigned at_step = (unsigned)(step % per_row);
     const cudaError_t err = with_type(s.table_dtype, [&](auto tx) {
         return with_type(s.y_dtype, [&](auto ty) {
             using TX = typename decltype(tx)::type;
             using TY = typename decltype(ty)::type;
-            auto go = [&](auto kernel) { return launch_dependent(kernel, grid, kEmbThreads, 0, 1, st, a, per_row, magic, row_step, at_step); };
+            auto go = [&](auto n) {
+                constexpr int kN = n();
+                return wide ? launch_dependent(k_embed_rows<TX, TY, kN>, grid, kEmbThreads, 0, 1, st, a, per_row, pieces, factor(pieces))
+                            : launch_dependent(k_embed_units<TX, TY, kN>, grid, kEmbThreads, 0, 1, st, a, per_row, factor(per_row), row_step, at_step);
+            };
             if constexpr (sizeof(TX) + sizeof(TY) == 4) {
-                if (L == kEights) return go(k_embed_fwd<TX, TY, 8>);
+                if (L == kEights) return go(std::integral_constant<int, 8>{});
             }
-            return L == kOne ? go(k_embed_fwd<TX, TY, 1>) : go(k_embed_fwd<TX, TY, 4>);
+            return L == kOne ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 4>{});
         });
     });
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
@@ -588,8 +639,8 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     const bool add = (s.flags & RR_ADD_DW) != 0;
     SortArgs a;
     a.e = emb_args(s, ids, dy, dtable, ws);
-    a.slabs = l.slabs;
-    a.slab = l.slab;
+    a.slabs = (s.n + kSlab - 1) / kSlab;
+    a.slab = (s.n + a.slabs - 1) / a.slabs;
     int bits = 1;
     while (bits < 31 && s.V >> bits) ++bits;  // (V itself is a key)
     a.passes = (bits + kDigitBits - 1) / kDigitBits;
@@ -600,21 +651,28 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     a.out_f32 = s.table_dtype == RR_F32;
     int fillers = 0;
     if (!add) {  // zeroing blocks: one an SM, but none with less than 64 KB
-        const long long bytes = (long long)s.V * s.d * (a.out_f32 ? 4 : 2), want = (bytes + 65535) / 65536;
-        const int most = sms - l.slabs > sms / 4 ? sms - l.slabs : sms / 4;  // (one block an SM: all at once)
+        const long long want = ((long long)s.V * s.d * (a.out_f32 ? 4 : 2) + 65535) / 65536;
+        const int most = sms - a.slabs > sms / 4 ? sms - a.slabs : sms / 4;  // (one block an SM: all at once)
         fillers = (int)(want < most ? want : most);
         if (fillers > s.V) fillers = s.V;
     }
     // (ids of up to 18 bits fit into a 32-bit word beside the place)
-    cudaError_t err = bits <= 32 - kPlaceBits ? launch_sort<uint32_t>(a, l.slabs + fillers, st) : launch_sort<uint64_t>(a, l.slabs + fillers, st);
-    if (err == cudaSuccess && l.slabs > 1)
-        err = launch_dependent(k_embed_merge, dim3((unsigned)((s.n + kEmbThreads - 1) / kEmbThreads)), kEmbThreads, 0, 1, st, (long long)s.n, l.slabs, l.slab,
-                               (const int *)l.key, (const int *)l.pos, l.key2, l.pos2);
+    cudaError_t err = bits <= 32 - kPlaceBits ? launch_sort<uint32_t>(a, a.slabs + fillers, st) : launch_sort<uint64_t>(a, a.slabs + fillers, st);
+    int *key = l.key, *pos = l.pos, *key2 = l.key2, *pos2 = l.pos2;
+    long long sorted = a.slab;
+    while (err == cudaSuccess && sorted < s.n) {
+        const bool few = sorted * 4 >= s.n;
+        err = launch_dependent(few ? k_embed_merge<4> : k_embed_merge<8>, dim3((unsigned)((s.n + kEmbThreads - 1) / kEmbThreads)), kEmbThreads, 0, 1, st, (int)s.n,
+                               (int)sorted, (const int *)key, (const int *)pos, key2, pos2);
+        std::swap(key, key2);
+        std::swap(pos, pos2);
+        sorted *= few ? 4 : 8;
+    }
     if (err != cudaSuccess) return RR_ERR_CUDA;
     SumArgs b;
     b.e = a.e;
-    b.key = l.key2;
-    b.pos = l.pos2;
+    b.key = key;
+    b.pos = pos;
     b.part = l.part;
     b.runs = l.runs;
     b.list = l.list;

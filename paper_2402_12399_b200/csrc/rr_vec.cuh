@@ -94,8 +94,13 @@ __device__ __forceinline__ void scaled(const Unit<A, kN> &from, Unit<B, kN> &to,
 {
     float v[kN];
     from.get(v);
+    if constexpr (kN == 1) {
+        v[0] *= f;
+    } else {
+        const f32x2 two = tc::pack2(f, f);
 #pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] *= f;
+        for (int j = 0; j < kN; j += 2) tc::unpack2(tc::mul2(tc::pack2(v[j], v[j + 1]), two), v[j], v[j + 1]);
+    }
     to.set(v);
 }
 
