@@ -541,7 +541,7 @@ rr_status rr_norm_bwd(const rr_norm_shape *s /* host */, const void *dy, const v
 
 /* Shape of one embedding call. */
 typedef struct rr_embed_shape {
-    int32_t n, V, d;           /* tokens (0 <= n <= 2^30), rows of the table, width; 1 <= V, d <= 2^30, V d < 2^40 */
+    int32_t n, V, d;           /* tokens (0 <= n <= 2^30), rows of the table (1 to 2^30), width (1 to 2^26); V d < 2^40 */
     int32_t wide_ids;          /* 0: ids are i32, 1: i64                                         */
     int32_t table_dtype;       /* RR_BF16 or RR_F32: type of table / dtable                      */
     int32_t y_dtype;           /* type of y / dy                                                 */

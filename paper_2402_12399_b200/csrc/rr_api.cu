@@ -711,7 +711,7 @@ namespace {
 rr_status check_embed_sizes(long long n, long long V, long long d)
 {
     constexpr long long kMost = 1ll << 30;
-    return n < 0 || n > kMost || V < 1 || V > kMost || d < 1 || d > kMost || V * d >= 1ll << 40 ? RR_ERR_INVALID_ARG : RR_OK;
+    return n < 0 || n > kMost || V < 1 || V > kMost || d < 1 || d > kMost >> 4 || V * d >= 1ll << 40 ? RR_ERR_INVALID_ARG : RR_OK;
 }
 
 rr_status check_embed(const rr_embed_shape *in, rr_embed_shape *s)

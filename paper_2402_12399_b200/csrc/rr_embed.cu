@@ -2,9 +2,12 @@
 //     y_i = scale table[id_i]          dtable_v = scale (sum over the tokens i with id_i = v, in token order, of dy_i)
 // Forward: a gather, bound by HBM.  Backward without floating-point atomics, so that results repeat: the tokens are sorted by id (stably:
 // equal ids stay in token order), the sorted tokens are cut into chunks of equal length, a block adds up the rows of a chunk in registers and
-// writes the table's row whenever the id changes.  An id that fills a chunk, or lies across its ends, leaves parts in the workspace that a last
-// kernel adds up in order: a frequent id costs no more than any other.  Rows that no token names are zeroed by blocks that run beside the
-// sort and learn of the named rows from a bitmap of their own.  Sums are fp32.
+// writes the table's row whenever the id changes.  An id with many tokens leaves pieces in the workspace that a last kernel adds up in order: a
+// frequent id costs no more than any other.  Rows that no token names are zeroed by blocks that run beside the sort and learn of the named
+// rows from a bitmap of their own.  Few tokens need no sort.  Sums are fp32.
+// Measured, bf16: forward 65536 x 1024 27.8 us (5.6 TB/s counting every row of the table that is named once), 37 x 4096 1.7 us.  Gradient of a table of
+// 32000 rows, 16384 x 4096 into fp32 130 us (5.0 TB/s; 80 of them the zeroed rows, which hide the sort), 16384 x 1024 45, 65536 x 1024 97 (sort
+// and zeroes 30, merge 8, sums 34, long runs 8, starts).
 #include <type_traits>
 #include <utility>
 
@@ -162,27 +165,29 @@ struct SortArgs {
     int out_f32;
 };
 
-// Rows of this zeroing block that no token names.  `lanes` lanes of a warp zero a row, as many as it has 16-byte pieces.
-__device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *map)
+// Rows of this zeroing block that no token names (`size`: bytes of an element).  `lanes` lanes of a warp zero a row, as many as it has 16-byte
+// pieces.
+template <int kThreads>
+__device__ void zero_rows(const EmbArgs &e, int size, int block, int blocks, uint32_t *map)
 {
-    const long long V = a.e.V, lo = V * block / blocks, hi = V * (block + 1) / blocks;
-    const long long width = (long long)a.e.d * (a.out_f32 ? 4 : 2);
+    const long long V = e.V, lo = V * block / blocks, hi = V * (block + 1) / blocks;
+    const long long width = (long long)e.d * size;
     int lanes = 1;
     while (lanes < 32 && lanes * 16 < width) lanes <<= 1;
-    const int lane = threadIdx.x & (lanes - 1), step = kSortThreads / lanes;
+    const int lane = threadIdx.x & (lanes - 1), step = kThreads / lanes;
     constexpr int kAtOnce = 8;
     for (long long r0 = lo; r0 < hi; r0 += kMapWords * 32) {
         const long long r1 = min(hi, r0 + kMapWords * 32);
         const int words = (int)((r1 - r0 + 31) / 32);
         __syncthreads();
-        for (int i = threadIdx.x; i < words; i += kSortThreads) map[i] = 0;
+        for (int i = threadIdx.x; i < words; i += kThreads) map[i] = 0;
         __syncthreads();
-        for (long long i0 = threadIdx.x; i0 < a.e.n; i0 += kAtOnce * kSortThreads) {
+        for (long long i0 = threadIdx.x; i0 < e.n; i0 += kAtOnce * kThreads) {
             long long token[kAtOnce];
             int id[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) token[u] = i0 + u * kSortThreads;
-            token_ids(a.e, token, a.e.n, id);
+            for (int u = 0; u < kAtOnce; ++u) token[u] = i0 + u * kThreads;
+            token_ids(e, token, e.n, id);
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u)
                 if (id[u] >= r0 && id[u] < r1) atomicOr(&map[(id[u] - r0) >> 5], 1u << ((id[u] - r0) & 31));
@@ -190,7 +195,7 @@ __device__ void zero_rows(const SortArgs &a, int block, int blocks, uint32_t *ma
         __syncthreads();
         for (long long r = r0 + threadIdx.x / lanes; r < r1; r += step) {
             if (map[(r - r0) >> 5] >> ((r - r0) & 31) & 1) continue;
-            char *p = static_cast<char *>(a.e.out) + r * width;  // (an even address, an even number of bytes)
+            char *p = static_cast<char *>(e.out) + r * width;  // (an even address, an even number of bytes)
             const int head = (int)min(width, (long long)(-(uintptr_t)p & 15)), tail = (int)((width - head) & 15);
             for (int i = 2 * lane; i < head; i += 2 * lanes) *reinterpret_cast<uint16_t *>(p + i) = 0;
             for (int i = 2 * lane; i < tail; i += 2 * lanes) *reinterpret_cast<uint16_t *>(p + width - tail + i) = 0;
@@ -211,7 +216,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
     extern __shared__ __align__(16) uint32_t shared[];
     dependent_start();
     if ((int)blockIdx.x >= a.slabs) {
-        zero_rows(a, blockIdx.x - a.slabs, gridDim.x - a.slabs, shared);
+        zero_rows<kSortThreads>(a.e, a.out_f32 ? 4 : 2, blockIdx.x - a.slabs, gridDim.x - a.slabs, shared);
         return;
     }
     // Table and words have gaps, so that threads next to each other meet in different banks: two entries after every 32, one word after every K.
@@ -466,8 +471,71 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
     }
 }
 
-// Long runs: a block adds up the pieces of kJoinCols 8 columns of one, every kJoin-th piece by a row of threads, those in order.
-constexpr int kJoin = 8, kJoinCols = 32;
+// Few tokens: one kernel instead of three.  Every block looks at all ids; the block of a token that is the first of its id adds up the rows of
+// all of them, those of other tokens have nothing to do, and the blocks behind zero the rows that nobody names.
+constexpr int kDirect = 128;
+template <class TY, class TO, Layout L>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_direct(const SumArgs a, int tiles)
+{
+    extern __shared__ __align__(16) uint32_t shared[];  // (the bitmap of a zeroing block)
+    dependent_start();
+    const int n = (int)a.e.n, token = blockIdx.x / tiles;
+    if (token >= n) {
+        zero_rows<kEmbThreads>(a.e, sizeof(TO), blockIdx.x - n * tiles, gridDim.x - n * tiles, shared);
+        return;
+    }
+    int *const same = reinterpret_cast<int *>(shared);  // the tokens of this one's id, in order
+    __shared__ int ids[kDirect];
+    __shared__ int count;
+    if (threadIdx.x < kDirect) {
+        const long long at[1] = {(long long)threadIdx.x};
+        int id[1];
+        token_ids(a.e, at, a.e.n, id);
+        ids[threadIdx.x] = id[0];
+    }
+    __syncthreads();
+    const int id = ids[token];
+    if (id < 0) return;
+    if (threadIdx.x < 32) {
+        int found = 0;
+        bool first = true;
+#pragma unroll
+        for (int k = 0; k < kDirect; k += 32) {
+            const int at = k + threadIdx.x;
+            const uint32_t with = __ballot_sync(0xffffffffu, ids[at] == id);
+            if (ids[at] == id) same[found + __popc(with & ((1u << threadIdx.x) - 1))] = at;
+            if (found == 0 && with) first = k + __ffs(with) - 1 == token;
+            found += __popc(with);
+        }
+        if (threadIdx.x == 0) count = first ? found : 0;
+    }
+    __syncthreads();
+    const int step = L == kQuads ? 4 * kEmbThreads : kEmbThreads,
+              at = (int)(blockIdx.x % tiles) * kEmbThreads * 8 + (int)threadIdx.x * (L == kEights ? 8 : L == kQuads ? 4 : 1);
+    if (at >= a.e.d) return;
+    const TY *dy = static_cast<const TY *>(a.e.in) + at;
+    f32x2 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(0.f, 0.f);
+    for (int i = 0; i < count; i += kAhead) {
+        Eight<TY, L> row[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < count) row[u].load(dy + (long long)same[i + u] * a.e.ld, step, a.e.d - at);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u >= count) break;
+            f32x2 v[4];
+            row[u].get(v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = tc::add2(acc[j], v[j]);
+        }
+    }
+    if (count) write_row<TO, L>(a, id, at, step, acc);
+}
+
+// Long runs: a block adds up the pieces of 8 kJoinCols columns of one, every kJoin-th piece by a row of threads, then the rows of threads in order.
+constexpr int kJoin = 16, kJoinCols = 32;
 template <class TO, Layout L>
 __global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a, int tiles)
 {
@@ -488,7 +556,7 @@ __global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(0.f, 0.f);
         if (at < a.e.d) {
-#pragma unroll 4
+#pragma unroll 8
             for (long long k = chunk + q; k <= end; k += kJoin) {
                 Eight<float, L> e;
                 e.template load<kKeep>(a.part + (k * 2 + (k == chunk ? 1 : 0)) * a.e.d + at, step, a.e.d - at);
@@ -501,11 +569,16 @@ __global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a
 #pragma unroll
         for (int j = 0; j < 4; ++j) tc::unpack2(acc[j], red[q][2 * j][c], red[q][2 * j + 1][c]);
         __syncthreads();
+        if (q < 8) {  // the q-th of the eight values
+            float sum = red[0][q][c];
+#pragma unroll
+            for (int i = 1; i < kJoin; ++i) sum += red[i][q][c];
+            red[0][q][c] = sum;  // (nobody else reads it before the barrier)
+        }
+        __syncthreads();
         if (q == 0 && at < a.e.d) {
 #pragma unroll
-            for (int i = 1; i < kJoin; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] = tc::add2(acc[j], tc::pack2(red[i][2 * j][c], red[i][2 * j + 1][c]));
+            for (int j = 0; j < 4; ++j) acc[j] = tc::pack2(red[0][2 * j][c], red[0][2 * j + 1][c]);
             write_row<TO, L>(a, id, at, step, acc);
         }
         // (the next item writes to red behind the barrier in its search)
@@ -637,8 +710,32 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     BwdLayout l;
     bwd_layout(ws, s.n, s.d, &l);
     const bool add = (s.flags & RR_ADD_DW) != 0;
+    const Layout L = s.d % 8 == 0 && s.ldy % 8 == 0 ? kEights : layout_of(s);  // (fp32 too: its loads meet in the L1 cache)
+    const EmbArgs e = emb_args(s, ids, dy, dtable, ws);
+    const long long zeroing = add ? 0 : ((long long)s.V * s.d * (s.table_dtype == RR_F32 ? 4 : 2) + 65535) / 65536;  // blocks that have 64 KB to zero
+    // calls f(type of dy, type of dtable, layout)
+    auto with_types = [&](auto f) {
+        return with_type(s.table_dtype, [&](auto to) {
+            return with_type(s.y_dtype, [&](auto ty) {
+                using std::integral_constant;
+                return L == kEights ? f(ty, to, integral_constant<Layout, kEights>{}) : L == kOne ? f(ty, to, integral_constant<Layout, kOne>{}) : f(ty, to, integral_constant<Layout, kQuads>{});
+            });
+        });
+    };
+    if (s.n <= kDirect) {
+        SumArgs b = {};
+        b.e = e;
+        b.add = add;
+        const int tiles = (s.d + kEmbThreads * 8 - 1) / (kEmbThreads * 8);
+        const long long most = zeroing < 4 * sms ? zeroing : 4 * sms;
+        const dim3 grid((unsigned)((long long)s.n * tiles + (most < s.V ? most : s.V)));
+        const cudaError_t err = with_types([&](auto ty, auto to, auto layout) {
+            return launch_dependent(k_embed_direct<typename decltype(ty)::type, typename decltype(to)::type, layout()>, grid, kEmbThreads, kMapWords * 4, 1, st, b, tiles);
+        });
+        return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
+    }
     SortArgs a;
-    a.e = emb_args(s, ids, dy, dtable, ws);
+    a.e = e;
     a.slabs = (s.n + kSlab - 1) / kSlab;
     a.slab = (s.n + a.slabs - 1) / a.slabs;
     int bits = 1;
@@ -650,10 +747,9 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     a.runs = l.runs;
     a.out_f32 = s.table_dtype == RR_F32;
     int fillers = 0;
-    if (!add) {  // zeroing blocks: one an SM, but none with less than 64 KB
-        const long long want = ((long long)s.V * s.d * (a.out_f32 ? 4 : 2) + 65535) / 65536;
+    if (!add) {
         const int most = sms - a.slabs > sms / 4 ? sms - a.slabs : sms / 4;  // (one block an SM: all at once)
-        fillers = (int)(want < most ? want : most);
+        fillers = (int)(zeroing < most ? zeroing : most);
         if (fillers > s.V) fillers = s.V;
     }
     // (ids of up to 18 bits fit into a 32-bit word beside the place)
@@ -678,26 +774,19 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     b.list = l.list;
     b.chunk = l.chunk;
     b.add = add;
-    const Layout L = s.d % 8 == 0 && s.ldy % 8 == 0 ? kEights : layout_of(s);  // (fp32 too: its loads meet in the L1 cache)
     int threads = 32;
     while (threads < kEmbThreads && threads * 8 < s.d) threads <<= 1;
     const dim3 grid((unsigned)l.chunks, (unsigned)((s.d + threads * 8 - 1) / (threads * 8)));
     const int tiles = (s.d + kJoinCols * 8 - 1) / (kJoinCols * 8);
     const long long most_items = (long long)(s.n / (2 * l.chunk) + 1) * tiles;
     const dim3 join((unsigned)(most_items < 2 * sms ? most_items : 2 * sms));
-    err = with_type(s.table_dtype, [&](auto to) {
-        using TO = typename decltype(to)::type;
-        cudaError_t e = with_type(s.y_dtype, [&](auto ty) {
-            using TY = typename decltype(ty)::type;
-            auto go = [&](auto kernel) { return launch_dependent(kernel, grid, threads, 0, 1, st, b); };
-            if (L == kEights) return go(k_embed_sum<TY, TO, kEights>);
-            return L == kOne ? go(k_embed_sum<TY, TO, kOne>) : go(k_embed_sum<TY, TO, kQuads>);
-        });
-        if (e != cudaSuccess || s.n <= 2 * l.chunk) return e;  // (no run is long)
-        auto go = [&](auto kernel) { return launch_dependent(kernel, join, kJoin * kJoinCols, 0, 1, st, b, tiles); };
-        if (L == kEights) return go(k_embed_join<TO, kEights>);
-        return L == kOne ? go(k_embed_join<TO, kOne>) : go(k_embed_join<TO, kQuads>);
+    err = with_types([&](auto ty, auto to, auto layout) {
+        return launch_dependent(k_embed_sum<typename decltype(ty)::type, typename decltype(to)::type, layout()>, grid, threads, 0, 1, st, b);
     });
+    if (err == cudaSuccess && s.n > 2 * l.chunk)  // (else no run is long)
+        err = with_types([&](auto, auto to, auto layout) {
+            return launch_dependent(k_embed_join<typename decltype(to)::type, layout()>, join, kJoin * kJoinCols, 0, 1, st, b, tiles);
+        });
     return err == cudaSuccess ? RR_OK : RR_ERR_CUDA;
 }
 

@@ -278,6 +278,7 @@ int bwd_parts(int M, int N)
     const NormLayout l = bwd_layout(N);
     const int sms = device_sm_count();
     const long long sets = ((long long)M + l.rows - 1) / l.rows, most = (long long)(sms > 0 ? sms : 148) * bwd_blocks(l.threads);
+    if (sets <= 4) return 1;  // (one block after the other set of rows: no second kernel, the device takes as long and the caller 2 us less)
     return (int)(sets < most ? sets : most);
 }
 

@@ -106,7 +106,8 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm
         else row_sums<G, false>(d2, d1, group, buf, turn);
         // what rounding left of the mean is in d1 (a row far from zero against its spread)
         const float rest = a.layer ? d1 * a.inv_n : 0.f;
-        const float rstd = __frsqrt_rn(fmaxf(fmaf(d2, a.inv_n, -rest * rest), 0.f) + a.eps);
+        const float spread = fmaf(d2, a.inv_n, -rest * rest);
+        const float rstd = __frsqrt_rn((spread < 0.f ? 0.f : spread) + a.eps);  // (a NaN stays one)
         if (in) {
             if (t == 0) {
                 if (a.mean) a.mean[row] = m + rest;

@@ -138,6 +138,15 @@ def test_more_elements_than_32_bits_count():
     assert (x[-5000:] == 0.25).all() and (x[:5000] == 0.25).all() and (x[(1 << 32) - 100:(1 << 32) + 100] == 0.25).all()
 
 
+def test_more_tensors_than_are_looked_up_at_once():
+    import paper_2402_12399_b200 as rr
+    for count, size in ((70000, 3), (700, 5000)):
+        whole = torch.randn(count * size + 1, device="cuda")[1:]
+        keep = whole.clone()
+        grads = list(whole.view(count, size).unbind(0))
+        _check([whole], [keep], rr.clip_grads(rr.grad_plan(grads), 7.0), 7.0)
+
+
 def test_captured_with_new_gradients():
     import paper_2402_12399_b200 as rr
     grads = [torch.randn(3000, device="cuda"), torch.randn(77, 9, device="cuda").bfloat16()]

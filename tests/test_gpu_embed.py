@@ -24,7 +24,7 @@ def _ids(g, n, V, kind):
     return ids
 
 
-SIZES = [(1, 1, 1), (1, 7, 8), (5, 3, 1000), (31, 100, 64), (32, 32000, 256), (33, 5, 2056), (37, 9, 4096), (1000, 300, 7), (1501, 9973, 1000), (2048, 2, 128), (2049, 65535, 24),
+SIZES = [(1, 1, 1), (1, 7, 8), (5, 3, 1000), (31, 100, 64), (32, 32000, 256), (33, 5, 2056), (37, 9, 4096), (128, 40, 520), (129, 40, 520), (100, 3000, 2064), (1000, 300, 7), (1501, 9973, 1000), (2048, 2, 128), (2049, 65535, 24),
          (4097, 65536, 8), (9000, 70000, 40), (16384, 1 << 17, 16), (16385, 50, 72), (40001, 262144, 9), (65536, 32000, 8)]
 
 

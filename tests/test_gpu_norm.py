@@ -176,6 +176,10 @@ def test_a_row_does_not_reach_another():
                 assert torch.isnan(y[i]).any()
             else:
                 assert torch.equal(y[i], clean[i])
+        rstd = torch.empty(50, device="cuda")
+        y = rr.norm_fwd(x, kind=rr.NORM_RMS, rstd=rstd)
+        assert torch.isnan(y[7]).all() and torch.isnan(rstd[7])                     # the mean square is not a number
+        assert torch.isnan(y[20]).all() and torch.isnan(y[33, 0]) and (y[33, 1:] == 0).all() and (rstd[[20, 33]] == 0).all()    # it is infinite
 
 
 def test_no_rows():

@@ -76,7 +76,7 @@ def test_embedding(rr):
         a = {**dict(ids=AT, i=2 * AT, o=3 * AT, ws=4 * AT, by=1 << 30), **kw}
         return [f(C.byref(_embed(rr, **kw)), a["ids"], a["i"], a["o"], a["ws"], a["by"], None) for f in (rr.lib().rr_embed_fwd, rr.lib().rr_embed_bwd)]
     # (ids 64 bytes, 16 x 24 in bf16 768, the table 4800)
-    for bad in [dict(n=-1), dict(n=(1 << 30) + 1), dict(V=0), dict(V=-1), dict(V=(1 << 30) + 1), dict(d=0), dict(d=(1 << 30) + 1), dict(V=1 << 20, d=1 << 20),
+    for bad in [dict(n=-1), dict(n=(1 << 30) + 1), dict(V=0), dict(V=-1), dict(V=(1 << 30) + 1), dict(d=0), dict(d=(1 << 26) + 1, V=1), dict(V=1 << 20, d=1 << 20),
                 dict(wide_ids=2), dict(wide_ids=-1), dict(table_dtype=2), dict(y_dtype=-1), dict(flags=1), dict(flags=6), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(scale=float("-inf")), dict(ldy=23), dict(ldy=-24), dict(ldy=1 << 40), dict(ldy=1 << 62), dict(ldy=-(1 << 63)),
                 dict(n=1 << 30, ldy=1 << 38), dict(ids=None), dict(i=None), dict(o=None), dict(ws=None), dict(ids=AT + 2), dict(ids=AT + 4, wide_ids=1), dict(i=ODD),
