@@ -246,7 +246,8 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
     }
 }
 
-// out[c] (+)= sum of the blocks' parts of column c, in a fixed order: a thread adds up every kLanes-th part, then the lanes are added in turn
+// out[c] (+)= sum of the blocks' parts of column c, in a fixed order: thread (q, lane) adds up every kFoldLanes-th part of column `lane`, then a warp
+// adds up the kFoldLanes sums of a column in pairs
 constexpr int kFoldLanes = 32;
 __global__ void __launch_bounds__(32 * kFoldLanes) k_norm_fold(int blocks, int N, const float *pw, const float *pb, float *dw, float *db, int add)
 {
@@ -263,11 +264,11 @@ __global__ void __launch_bounds__(32 * kFoldLanes) k_norm_fold(int blocks, int N
     }
     red[q][lane] = sum;
     __syncthreads();
-    if (q || c >= N) return;
-    sum = red[0][lane];
+    sum = red[lane][q];
 #pragma unroll
-    for (int i = 1; i < kFoldLanes; ++i) sum += red[i][lane];
-    out[c] = add ? out[c] + sum : sum;
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const int column = blockIdx.x * 32 + q;
+    if (lane == 0 && column < N) out[column] = add ? out[column] + sum : sum;
 }
 
 // Two eights a thread beside the sums of as many columns; four from 8192 columns on, where two would take a block of 1024.

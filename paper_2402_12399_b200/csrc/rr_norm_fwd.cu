@@ -76,11 +76,9 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm
         }
         float m = 0.f, d1 = 0.f, d2 = 0.f;
         if (a.layer) {
-            f32x2 sum = pack2(0.f, 0.f);
+            f32x2 sum = pack2(0.f, 0.f);  // (in pairs: a mean is often small against its terms)
 #pragma unroll
-            for (int s = 0; s < kSlots; ++s)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum = add2(sum, v[s][j]);
+            for (int s = 0; s < kSlots; ++s) sum = add2(sum, add2(add2(v[s][0], v[s][1]), add2(v[s][2], v[s][3])));
             m = both(sum);
             row_sums<G, false>(m, d1, group, buf, turn);
             m *= a.inv_n;
@@ -91,8 +89,7 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[s][j] = add2(v[s][j], centre);
                 cut<L>(v[s], step, a.N - col - s * 8 * group);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum = add2(sum, v[s][j]);
+                sum = add2(sum, add2(add2(v[s][0], v[s][1]), add2(v[s][2], v[s][3])));
             }
             d1 = both(sum);
         }
@@ -110,7 +107,8 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm
         const float rstd = __frsqrt_rn((spread < 0.f ? 0.f : spread) + a.eps);  // (a NaN stays one)
         if (in) {
             if (t == 0) {
-                if (a.mean) a.mean[row] = m + rest;
+                // (`rest` is the mean of rounded differences: below a few of their half steps it says more about them than about m)
+                if (a.mean) a.mean[row] = fabsf(rest) * rstd > 0x1p-22f ? m + rest : m;
                 if (a.rstd) a.rstd[row] = rstd;
             }
             const f32x2 factor = pack2(rstd, rstd), shift = pack2(-rest * rstd, -rest * rstd);
