@@ -779,7 +779,7 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     const dim3 grid((unsigned)l.chunks, (unsigned)((s.d + threads * 8 - 1) / (threads * 8)));
     const int tiles = (s.d + kJoinCols * 8 - 1) / (kJoinCols * 8);
     const long long most_items = (long long)(s.n / (2 * l.chunk) + 1) * tiles;
-    const dim3 join((unsigned)(most_items < 2 * sms ? most_items : 2 * sms));
+    const dim3 join((unsigned)(most_items < 4 * sms ? most_items : 4 * sms));
     err = with_types([&](auto ty, auto to, auto layout) {
         return launch_dependent(k_embed_sum<typename decltype(ty)::type, typename decltype(to)::type, layout()>, grid, threads, 0, 1, st, b);
     });
