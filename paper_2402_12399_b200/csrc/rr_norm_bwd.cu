@@ -7,19 +7,51 @@ namespace {
 
 constexpr int bwd_blocks(int threads) { return threads == 256 ? 2 : 1; }  // an SM
 
+__host__ __device__ constexpr int weight_bytes(int slots, int threads) { return slots * 8 * 4 * threads; }
+
+// weights of eight columns from `at` on (1 where there are none)
+template <Layout L>
+__device__ __forceinline__ void weight(const NormArgs &a, int at, int step, f32x2 (&w)[4])
+{
+    if (!a.w || at >= a.N) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack2(1.f, 1.f);
+    } else if (a.w_f32) {
+        Eight<float, L> e;
+        e.template load<kConst>(static_cast<const float *>(a.w) + at, step, a.N - at);
+        e.get(w);
+    } else {
+        Eight<bf16, L> e;
+        e.template load<kConst>(static_cast<const bf16 *>(a.w) + at, step, a.N - at);
+        e.get(w);
+    }
+}
+
 // A block takes every gridDim-th set of rows and keeps the sums of its columns over them in registers.  With four eights a thread there are no
 // registers left to keep a row's numbers: they are worked out a second time.  TD: type of dx and dh.
 template <class TY, class TH, class TD, Layout L, int kSlots, int kThreads, int G>
 __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(const NormArgs a)
 {
     constexpr bool kHold = kSlots == 2;
-    extern __shared__ __align__(16) char ring[];  // [2] dy, h, dh; afterwards the sums of the block's rows side by side
+    extern __shared__ __align__(16) char shared[];  // weights (kHold), then [2] dy, h, dh; afterwards the sums of the block's rows side by side
     __shared__ float2 buf[2][32];
     dependent_start();
     const int group = G ? G : a.group, rows = kThreads / group, t = threadIdx.x & (group - 1), step = step_of<L>(group), col = first_column<L>(t);
     long long row = (long long)blockIdx.x * rows + threadIdx.x / group;
     const int h_at = tensor_bytes(L, sizeof(TY), kSlots, kThreads, rows, a.N), d_at = h_at + tensor_bytes(L, sizeof(TH), kSlots, kThreads, rows, a.N);
     const int stage_bytes = d_at + (a.dh ? tensor_bytes(L, sizeof(TD), kSlots, kThreads, rows, a.N) : 0);
+    // A thread's weights are the same in every row: they lie in shared memory as the numbers they are, each thread's its own.
+    float4 *const weights = reinterpret_cast<float4 *>(shared) + threadIdx.x;
+    char *const ring = shared + (kHold ? weight_bytes(kSlots, kThreads) : 0);
+    if constexpr (kHold) {
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            f32x2 w[4];
+            weight<L>(a, col + s * 8 * group, step, w);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) quad_from(weights[(2 * s + q) * kThreads], w[2 * q], w[2 * q + 1]);
+        }
+    }
     const uint32_t ring_at = smem_u32(ring);
     // the thread's first column in the present rows
     const TY *py = static_cast<const TY *>(a.dy) + row * a.lddy + col;
@@ -79,23 +111,15 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
             }
             ey.get(y);
             eh.get(x);
-            if (!a.w) {
+            f32x2 w[4];
+            if constexpr (kHold) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] = y[j];
+                for (int q = 0; q < 2; ++q) quad_of(weights[(2 * s + q) * kThreads], w[2 * q], w[2 * q + 1]);
             } else {
-                f32x2 w[4];
-                if (a.w_f32) {
-                    Eight<float, L> e;
-                    e.template load<kConst>(static_cast<const float *>(a.w) + col + s * 8 * group, step, left);
-                    e.get(w);
-                } else {
-                    Eight<bf16, L> e;
-                    e.template load<kConst>(static_cast<const bf16 *>(a.w) + col + s * 8 * group, step, left);
-                    e.get(w);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] = mul2(y[j], w[j]);
+                weight<L>(a, col + s * 8 * group, step, w);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = mul2(y[j], w[j]);
             if (a.layer) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = add2(x[j], centre);
@@ -329,12 +353,13 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
     a.db = db ? (fold ? pb : db) : nullptr;
     a.add = fold ? 0 : add;
     auto bytes = [&](int dtype) { return tensor_bytes(L, dtype == RR_F32 ? 4 : 2, l.slots, l.threads, l.rows, s.N); };
-    const int row = bytes(s.y_dtype) + bytes(s.h_dtype) + (dh ? bytes(s.dx_dtype) : 0), room = kMostShared / bwd_blocks(l.threads);
+    const int weights = l.slots == 2 ? weight_bytes(2, l.threads) : 0;
+    const int row = bytes(s.y_dtype) + bytes(s.h_dtype) + (dh ? bytes(s.dx_dtype) : 0), room = kMostShared / bwd_blocks(l.threads) - weights;
     // (a block with one set of rows has nothing to fetch ahead)
     a.ahead = (long long)s.M <= (long long)parts * l.rows ? 0 : 2 * row <= room ? 2 : row <= room ? 1 : 0;
-    int smem = a.ahead * row;
+    int smem = weights + a.ahead * row;
     const int sets = l.threads / (l.group < 32 ? 32 : l.group), sums = sets > 1 ? sets * 2 * s.N * 4 : 0;  // (32 KB at most)
-    if (smem < sums) smem = sums;
+    if (smem < weights + sums) smem = weights + sums;
     cudaError_t err = with_type(s.y_dtype, [&](auto ty) {
         return with_type(s.h_dtype, [&](auto th) {
             return with_type(s.dx_dtype, [&](auto td) {
