@@ -767,16 +767,9 @@ def _vector(t, n: int, dtype, what: str):
     return t.data_ptr()
 
 
-def _matrix(t, shape, what: str):
-    """(address, pitch, type) of a matrix whose rows may lie apart; zeros when it is not given."""
-    if t is None:
-        return None, 0, 0
-    code = _TYPE_CODE.get(t.dtype)
-    if code is None:
-        _code(t, what)
-    if t.shape == shape and t.is_contiguous():
-        return t.data_ptr(), 0, code
-    return t.data_ptr(), _pitch(t, shape[0], shape[1], what), code
+def _type_and_pitch(t, shape, what: str):
+    """What is said about a matrix that is not simply packed, or not of a type that is known."""
+    return _code(t, what), _pitch(t, shape[0], shape[1], what)
 
 
 def _parameters(weight, bias) -> int:
@@ -800,18 +793,27 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Te
         out = torch.empty(shape, dtype=out_dtype or (x if residual is None else residual).dtype, device=x.device)
     here = _here()
     _elsewhere(here, x, weight, bias, residual, h, out, mean, rstd)
-    px, ldx, xt = _matrix(x, shape, "x")
-    pr, ldr, ht = _matrix(residual, shape, "residual")
-    ph, ldh, t = _matrix(h, shape, "h")
-    py, ldy, yt = _matrix(out, shape, "out")
+    ldx = ldr = ldh = ldy = ht = 0
+    xt, yt = _TYPE_CODE.get(x.dtype), _TYPE_CODE.get(out.dtype)
+    if xt is None or not x.is_contiguous():
+        xt, ldx = _type_and_pitch(x, shape, "x")
+    if yt is None or out.shape != shape or not out.is_contiguous():
+        yt, ldy = _type_and_pitch(out, shape, "out")
+    if residual is not None:
+        ht = _TYPE_CODE.get(residual.dtype)
+        if ht is None or residual.shape != shape or not residual.is_contiguous():
+            ht, ldr = _type_and_pitch(residual, shape, "residual")
     if h is not None:
         if residual is None:
             raise ValueError("h is residual + x: it needs a residual")
-        if t != ht:
+        if h.dtype != residual.dtype:
             raise TypeError(f"residual is {residual.dtype}, h {h.dtype}")
+        if h.shape != shape or not h.is_contiguous():
+            ldh = _pitch(h, M, N, "h")
     s = _CNorm(M, N, kind, xt, ht, _parameters(weight, bias), yt, 0, 0, eps, ldx, ldr, ldh, ldy)
-    code = (_lib or lib()).rr_norm_fwd(C.byref(s), px, pr, _vector(weight, N, None, "weight"), _vector(bias, N, None, "bias"), ph, py,
-                                       _vector(mean, M, _F32, "mean"), _vector(rstd, M, _F32, "rstd"), _stream_of(here))
+    code = (_lib or lib()).rr_norm_fwd(C.byref(s), x.data_ptr(), None if residual is None else residual.data_ptr(), _vector(weight, N, None, "weight"),
+                                       _vector(bias, N, None, "bias"), None if h is None else h.data_ptr(), out.data_ptr(), _vector(mean, M, _F32, "mean"),
+                                       _vector(rstd, M, _F32, "rstd"), _stream_of(here))
     if code:
         raise RRError(code, "rr_norm_fwd")
     return out
@@ -829,23 +831,28 @@ def norm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mea
         workspace = alloc_workspace(norm_workspace_bytes(M, N), dy.device)
     here = _here()
     _elsewhere(here, dy, h, weight, mean, rstd, dh, dx, dw, dbias, workspace)
-    py, lddy, yt = _matrix(dy, shape, "dy")
-    ph, ldh, ht = _matrix(h, shape, "h")
-    pd, lddh, dt = _matrix(dh, shape, "dh")
-    px, lddx, t = _matrix(dx, shape, "dx")
+    lddy = ldh = lddh = lddx = dt = 0
+    yt, ht = _TYPE_CODE.get(dy.dtype), _TYPE_CODE.get(h.dtype)
+    if yt is None or not dy.is_contiguous():
+        yt, lddy = _type_and_pitch(dy, shape, "dy")
+    if ht is None or h.shape != shape or not h.is_contiguous():
+        ht, ldh = _type_and_pitch(h, shape, "h")
     if dx is not None:
-        if dh is not None and dt != t:
+        dt = _TYPE_CODE.get(dx.dtype)
+        if dt is None or dx.shape != shape or not dx.is_contiguous():
+            dt, lddx = _type_and_pitch(dx, shape, "dx")
+    if dh is not None:
+        if dx is not None and dh.dtype != dx.dtype:
             raise TypeError(f"dh is {dh.dtype}, dx {dx.dtype}")
-        dt = t
+        dt = _TYPE_CODE.get(dh.dtype)
+        if dt is None or dh.shape != shape or not dh.is_contiguous():
+            dt, lddh = _type_and_pitch(dh, shape, "dh")
     s = _CNorm(M, N, kind, 0, ht, _parameters(weight, None), yt, dt, ADD_DW if add_dw else 0, 0.0, 0, 0, ldh, 0, lddy, lddh, lddx)
-    code = (_lib or lib()).rr_norm_bwd(C.byref(s), py, ph, _vector(weight, N, None, "weight"), _vector(mean, M, _F32, "mean"), _vector(rstd, M, _F32, "rstd"),
-                                       pd, px, _vector(dw, N, _F32, "dw"), _vector(dbias, N, _F32, "dbias"), workspace.data_ptr(), workspace.numel(),
-                                       _stream_of(here))
+    code = (_lib or lib()).rr_norm_bwd(C.byref(s), dy.data_ptr(), h.data_ptr(), _vector(weight, N, None, "weight"), _vector(mean, M, _F32, "mean"),
+                                       _vector(rstd, M, _F32, "rstd"), None if dh is None else dh.data_ptr(), None if dx is None else dx.data_ptr(),
+                                       _vector(dw, N, _F32, "dw"), _vector(dbias, N, _F32, "dbias"), workspace.data_ptr(), workspace.numel(), _stream_of(here))
     if code:
         raise RRError(code, "rr_norm_bwd")
-    for t in (dx, dw, dbias):
-        if t is not None:
-            t._workspace = workspace
     return dx, dw, dbias
 
 
@@ -877,9 +884,11 @@ def embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: t
     _elsewhere(here, ids, table, out, workspace)
     if not table.is_contiguous():
         raise ValueError("table must be contiguous")
-    py, ldy, yt = _matrix(out, (n, d), "out")
+    yt, ldy = _TYPE_CODE.get(out.dtype), 0
+    if yt is None or out.shape != (n, d) or not out.is_contiguous():
+        yt, ldy = _type_and_pitch(out, (n, d), "out")
     s = _CEmbed(n, V, d, _token_ids(ids), _code(table, "table"), yt, 0, scale, ldy)
-    code = (_lib or lib()).rr_embed_fwd(C.byref(s), ids.data_ptr(), table.data_ptr(), py, workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    code = (_lib or lib()).rr_embed_fwd(C.byref(s), ids.data_ptr(), table.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
     if code:
         raise RRError(code, "rr_embed_fwd")
     out._workspace = workspace
@@ -898,9 +907,11 @@ def embed_bwd(ids: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, scale: 
     _elsewhere(here, ids, dy, dtable, workspace)
     if not dtable.is_contiguous():
         raise ValueError("dtable must be contiguous")
-    py, ldy, yt = _matrix(dy, (n, d), "dy")
+    yt, ldy = _TYPE_CODE.get(dy.dtype), 0
+    if yt is None or dy.shape != (n, d) or not dy.is_contiguous():
+        yt, ldy = _type_and_pitch(dy, (n, d), "dy")
     s = _CEmbed(n, V, d, _token_ids(ids), _code(dtable, "dtable"), yt, ADD_DW if accumulate else 0, scale, ldy)
-    code = (_lib or lib()).rr_embed_bwd(C.byref(s), ids.data_ptr(), py, dtable.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
+    code = (_lib or lib()).rr_embed_bwd(C.byref(s), ids.data_ptr(), dy.data_ptr(), dtable.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(here))
     if code:
         raise RRError(code, "rr_embed_bwd")
     dtable._workspace = workspace
