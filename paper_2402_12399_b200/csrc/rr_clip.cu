@@ -48,7 +48,7 @@ __device__ __forceinline__ GradEntry entry(const GradEntry *plan, int i)
     const longlong2 *p = reinterpret_cast<const longlong2 *>(plan + i);
     longlong2 *q = reinterpret_cast<longlong2 *>(&e);
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(GradEntry) / 16; ++j) q[j] = __ldg(p + j);
+    for (int j = 0; j < (int)sizeof(GradEntry) / 16; ++j) q[j] = p[j];
     return e;
 }
 static_assert(sizeof(GradEntry) == 48, "read in pieces of 16 bytes");
@@ -64,12 +64,12 @@ __device__ __forceinline__ void seek(Place &p, const GradEntry *plan, int tensor
     int lo = 0, len = tensors;  // the last tensor whose first chunk is not behind this one (those without a chunk lie before one with)
     while (len > 1) {
         const int stride = (len + kClipThreads - 1) / kClipThreads, at = (int)threadIdx.x * stride;
-        const int count = __syncthreads_count(at < len && __ldg(&plan[lo + at].first) <= chunk) - 1;  // (the first of the range always is)
+        const int count = __syncthreads_count(at < len && plan[lo + at].first <= chunk) - 1;  // (the first of the range always is)
         lo += count * stride;
         len = min(stride, len - count * stride);
     }
     p.e = entry(plan, lo);
-    p.end = __ldg(&plan[lo + 1].first);
+    p.end = plan[lo + 1].first;
 }
 
 // Range of chunk `c` of a tensor: elements [lo, hi), of which [body, body + 8 eights) lie at 16-byte boundaries.
@@ -140,7 +140,7 @@ __device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
     for (; i + (kAtOnce - 1) * kClipThreads < units; i += kAtOnce * kClipThreads) {
         Unit<T, kN> e[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) e[u].template load<kConst>(p + (long long)(i + u * kClipThreads) * kN);
+        for (int u = 0; u < kAtOnce; ++u) e[u].template load<kKeep>(p + (long long)(i + u * kClipThreads) * kN);
 #pragma unroll
         for (int u = 0; u < kAtOnce; u += 8 / kN) {  // eight values at a time
             float v[8];
@@ -151,7 +151,7 @@ __device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
     }
     for (; i < units; i += kClipThreads) {
         Unit<T, kN> e;
-        e.template load<kConst>(p + (long long)i * kN);
+        e.template load<kKeep>(p + (long long)i * kN);
         float v[kN];
         e.get(v);
         sum += squares<kN>(v);
@@ -220,7 +220,7 @@ k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, co
     if (c >= 0) seek(p, plan, tensors, c);  // (the plan is older than the sums: see above)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0;
-    for (int i = threadIdx.x; i < parts; i += kClipThreads) sum += __ldg(part + i);
+    for (int i = threadIdx.x; i < parts; i += kClipThreads) sum += __ldcg(part + i);
     sum = block_sum(sum, buf);
     const double root = sqrt(sum);
     const bool finite = isfinite(sum);

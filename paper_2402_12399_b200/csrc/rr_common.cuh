@@ -81,10 +81,11 @@ inline int device_sm_count()
     return n;
 }
 
-// The shared memory that a kernel may be launched with, beyond the 48 KB of every kernel: asked for once per device and size that is larger than
-// before (the question costs a launch half a microsecond).  One static object per kernel.
+// Shared memory beyond the 48 KB of every kernel: the most there is is asked for, once per device (the question costs a launch half a microsecond,
+// and a number that changed from call to call would be a race between threads).  One static object per kernel.
 struct SharedAllowance {
-    std::atomic<int> known[64] = {};
+    static constexpr int kMost = 226 << 10;  // (beside a little of the kernel's own)
+    std::atomic<bool> asked[64] = {};
     template <class K>
     cudaError_t ask(K kernel, int bytes)
     {
@@ -93,9 +94,9 @@ struct SharedAllowance {
         cudaError_t err = cudaGetDevice(&dev);
         if (err != cudaSuccess) return err;
         const bool keep = dev >= 0 && dev < 64;
-        if (keep && known[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
-        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (err == cudaSuccess && keep) known[dev].store(bytes, std::memory_order_relaxed);
+        if (keep && asked[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (err == cudaSuccess && keep) asked[dev].store(true, std::memory_order_relaxed);
         return err;
     }
 };

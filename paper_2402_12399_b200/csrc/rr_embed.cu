@@ -5,9 +5,9 @@
 // writes the table's row whenever the id changes.  An id with many tokens leaves pieces in the workspace that a last kernel adds up in order: a
 // frequent id costs no more than any other.  Rows that no token names are zeroed by blocks that run beside the sort and learn of the named
 // rows from a bitmap of their own.  Few tokens need no sort.  Sums are fp32.
-// Measured, bf16: forward 65536 x 1024 27.8 us (5.6 TB/s counting every row of the table that is named once), 37 x 4096 1.7 us.  Gradient of a table of
-// 32000 rows, 16384 x 4096 into fp32 130 us (5.0 TB/s; 80 of them the zeroed rows, which hide the sort), 16384 x 1024 45, 65536 x 1024 97 (sort
-// and zeroes 30, merge 8, sums 34, long runs 8, starts).
+// Measured, bf16: forward 65536 x 1024 27.7 us (5.7 TB/s counting every row of the table that is named once), 37 x 4096 1.7 us.  Gradient of a table of
+// 32000 rows, 16384 x 4096 into fp32 129 us (5.1 TB/s; 80 of them the zeroed rows, which hide the sort), 16384 x 1024 42, 65536 x 1024 86 (sort
+// beside rows to zero 28, merge 8, sums 33, long runs 8, starts).
 #include <type_traits>
 #include <utility>
 
@@ -44,8 +44,8 @@ __device__ __forceinline__ void token_ids(const EmbArgs &a, const long long (&to
     for (int k = 0; k < kN; ++k) {
         raw[k] = -1;
         if (token[k] >= end) continue;
-        if (a.wide) raw[k] = __ldg(static_cast<const long long *>(a.ids) + token[k]);
-        else raw[k] = __ldg(static_cast<const int *>(a.ids) + token[k]);
+        if (a.wide) raw[k] = static_cast<const long long *>(a.ids)[token[k]];
+        else raw[k] = static_cast<const int *>(a.ids)[token[k]];
     }
     bool bad = false;
 #pragma unroll
@@ -304,12 +304,12 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const SortArgs a)
 // Every kSide sorted slabs into one: a token's place is the number of tokens in front of it in each of them (equal ids: earlier slabs only).  The
 // slabs are searched side by side, all of a step's loads in flight together.
 template <int kSide>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_merge(int n, int slab, const int *__restrict__ key, const int *__restrict__ pos, int *out_key, int *out_pos)
+__global__ void __launch_bounds__(kEmbThreads) k_embed_merge(int n, int slab, const int *key, const int *pos, int *out_key, int *out_pos)
 {
     dependent_start();
     const int i = blockIdx.x * kEmbThreads + threadIdx.x;
     if (i >= n) return;
-    const int mine = i / slab, first = mine / kSide * kSide, id = __ldg(key + i), token = __ldg(pos + i);
+    const int mine = i / slab, first = mine / kSide * kSide, id = key[i], token = pos[i];
     int to = i - (mine - first) * slab;  // (places are below 2^30)
     int lo[kSide], hi[kSide], start[kSide], steps = 1;
     while (1 << steps <= slab) ++steps;
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_merge(int n, int slab, co
     for (int step = 0; step < steps; ++step) {
         int k[kSide];
 #pragma unroll
-        for (int u = 0; u < kSide; ++u) k[u] = __ldg(key + start[u] + min((lo[u] + hi[u]) >> 1, max(hi[u] - 1, 0)));
+        for (int u = 0; u < kSide; ++u) k[u] = key[start[u] + min((lo[u] + hi[u]) >> 1, max(hi[u] - 1, 0))];
 #pragma unroll
         for (int u = 0; u < kSide; ++u) {  // tokens of that slab below id, or in earlier slabs not above it
             const int mid = (lo[u] + hi[u]) >> 1;
@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const SumArgs a)
         k[u] = -1;
         p[u] = 0;
         if (i >= kBefore + kReach || at < 0 || at >= a.e.n) continue;
-        k[u] = __ldg(a.key + at);
-        if (i >= kBefore) p[u] = __ldg(a.pos + at);
+        k[u] = a.key[at];
+        if (i >= kBefore) p[u] = a.pos[at];
     }
 #pragma unroll
     for (int u = 0; u < kLooks; ++u) {
@@ -543,12 +543,12 @@ __global__ void __launch_bounds__(kJoin *kJoinCols) k_embed_join(const SumArgs a
     dependent_start();
     const long long items = (long long)*a.runs * tiles;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long chunk = __ldg(a.list + item / tiles);
-        const int id = __ldg(a.key + (chunk + 1) * a.chunk - 1);
+        const long long chunk = a.list[item / tiles];
+        const int id = a.key[(chunk + 1) * a.chunk - 1];
         long long end = chunk;  // its last chunk: those behind the first that begin with it
         for (int more = kJoin * kJoinCols; more == kJoin * kJoinCols; end += more) {
             const long long at = (end + 1 + threadIdx.x) * a.chunk;
-            more = __syncthreads_count(at < a.e.n && __ldg(a.key + at) == id);
+            more = __syncthreads_count(at < a.e.n && a.key[at] == id);
         }
         const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols, step = L == kQuads ? 4 * kJoinCols : kJoinCols;
         const int at = (int)(item % tiles) * kJoinCols * 8 + c * (L == kEights ? 8 : L == kQuads ? 4 : 1);
@@ -648,7 +648,7 @@ template <int K, class T>
 cudaError_t launch_sort(const SortArgs &a, int blocks, cudaStream_t st)
 {
     constexpr size_t smem = (size_t)kTableWords * 4 + (size_t)kSortThreads * (K + 1) * sizeof(T);
-    static_assert(smem >= kMapWords * 4 && smem <= 227 << 10, "a zeroing block's bitmap lies in the same memory");
+    static_assert(smem >= kMapWords * 4 && smem <= SharedAllowance::kMost, "a zeroing block's bitmap lies in the same memory");
     static SharedAllowance allowance;
     const cudaError_t err = allowance.ask(k_embed_sort<K, T>, (int)smem);
     if (err != cudaSuccess) return err;

@@ -18,11 +18,11 @@ __device__ __forceinline__ void weight(const NormArgs &a, int at, int step, f32x
         for (int j = 0; j < 4; ++j) w[j] = pack2(1.f, 1.f);
     } else if (a.w_f32) {
         Eight<float, L> e;
-        e.template load<kConst>(static_cast<const float *>(a.w) + at, step, a.N - at);
+        e.template load<kKeep>(static_cast<const float *>(a.w) + at, step, a.N - at);
         e.get(w);
     } else {
         Eight<bf16, L> e;
-        e.template load<kConst>(static_cast<const bf16 *>(a.w) + at, step, a.N - at);
+        e.template load<kKeep>(static_cast<const bf16 *>(a.w) + at, step, a.N - at);
         e.get(w);
     }
 }
@@ -70,8 +70,8 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
     if (a.ahead) request(row, py, ph, pd, 0);
     float mean = 0.f, rstd = 0.f;
     if (row < a.M) {
-        if (a.layer) mean = __ldg(a.mean + row);
-        rstd = __ldg(a.rstd + row);
+        if (a.layer) mean = a.mean[row];
+        rstd = a.rstd[row];
     }
     f32x2 aw[kSlots][4], ab[kSlots][4];
 #pragma unroll
@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(kThreads, bwd_blocks(kThreads)) k_norm_bwd(con
         const f32x2 centre = pack2(-mean, -mean), factor = pack2(rstd, rstd);
         mean = rstd = 0.f;
         if (row + a.stride < a.M) {  // (of the next row)
-            if (a.layer) mean = __ldg(a.mean + row + a.stride);
-            rstd = __ldg(a.rstd + row + a.stride);
+            if (a.layer) mean = a.mean[row + a.stride];
+            rstd = a.rstd[row + a.stride];
         }
         // the numbers of slot s: dy, xh and dy w (behind the row: dy is 0, and so is all that is made of it)
         auto numbers = [&](int s, f32x2 (&y)[4], f32x2 (&x)[4], f32x2 (&g)[4]) {
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(32 * kFoldLanes) k_norm_fold(int blocks, int N
     float sum = 0.f;
     if (c < N) {
 #pragma unroll 8
-        for (int b = q; b < blocks; b += kFoldLanes) sum += __ldg(p + (size_t)b * N + c);
+        for (int b = q; b < blocks; b += kFoldLanes) sum += __ldcs(p + (size_t)b * N + c);
     }
     red[q][lane] = sum;
     __syncthreads();

@@ -14,13 +14,13 @@ __device__ __forceinline__ void apply(const NormArgs &a, int at, int step, f32x2
     Eight<TW, L> e;
     f32x2 p[4];
     if (a.w) {
-        e.template load<kConst>(static_cast<const TW *>(a.w) + at, step, a.N - at);
+        e.template load<kKeep>(static_cast<const TW *>(a.w) + at, step, a.N - at);
         e.get(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], p[j]);
     }
     if (a.b) {
-        e.template load<kConst>(static_cast<const TW *>(a.b) + at, step, a.N - at);
+        e.template load<kKeep>(static_cast<const TW *>(a.b) + at, step, a.N - at);
         e.get(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = add2(v[j], p[j]);

@@ -19,9 +19,9 @@ __device__ __forceinline__ T from_f32(float v)
     else return __float2bfloat16_rn(v);
 }
 
-// How a load or store treats the caches: kStream for what is touched once, kKeep for what comes again, kConst for what comes again and
-// what nothing in the launch writes to.
-enum Cache { kKeep, kStream, kConst };
+// How a load or store treats the caches: kStream for what is touched once, kKeep for what comes again.  (No loads past the coherent path: a kernel
+// that is made ready while the one in front of it still writes must not promise that what it reads stays as it is while it runs.)
+enum Cache { kKeep, kStream };
 // A single bf16 goes as the 16-bit word it is: cuda_bf16.h states its cached loads as pure functions of the address, which the compiler may then
 // make before the condition that guards them (a missing vector was read from address zero) or move across a store to the same place.
 template <Cache C, class V>
@@ -29,8 +29,7 @@ __device__ __forceinline__ V fetch(const V *p)
 {
     if constexpr (std::is_same<V, __nv_bfloat16>::value) return __ushort_as_bfloat16(fetch<C>(reinterpret_cast<const unsigned short *>(p)));
     else if constexpr (C == kStream) return __ldcs(p);
-    else if constexpr (C == kConst) return __ldg(p);
-    else return *p;
+    else return __ldca(p);  // (which, as __ldcs, stays where it is written: loads asked for together are asked for together)
 }
 template <Cache C, class V>
 __device__ __forceinline__ void place(V *p, V v)

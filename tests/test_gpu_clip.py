@@ -147,6 +147,20 @@ def test_more_tensors_than_are_looked_up_at_once():
         _check([whole], [keep], rr.clip_grads(rr.grad_plan(grads), 7.0), 7.0)
 
 
+def test_plans_one_after_the_other_at_one_address():
+    """A plan that takes the place of the last one at once: nothing of the old list is seen."""
+    import paper_2402_12399_b200 as rr
+    grads = [[torch.randn(257 * (i + 1) + 31 * j, device="cuda") for j in range(1 + i % 7)] for i in range(30)]
+    keep = [[t.clone() for t in g] for g in grads]
+    norms = torch.empty(30, 2, device="cuda")
+    ws = rr.alloc_workspace(rr.clip_workspace_bytes())
+    torch.cuda.synchronize()
+    for i, g in enumerate(grads):
+        norms[i] = rr.clip_grads(rr.grad_plan(g), 1.0, workspace=ws)     # (the plan's buffer goes back to the allocator, which hands it out again)
+    for i, g in enumerate(grads):
+        _check(g, keep[i], norms[i], 1.0)
+
+
 def test_captured_with_new_gradients():
     import paper_2402_12399_b200 as rr
     grads = [torch.randn(3000, device="cuda"), torch.randn(77, 9, device="cuda").bfloat16()]
