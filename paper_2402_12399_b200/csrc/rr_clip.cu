@@ -7,7 +7,7 @@
 // length nor the order costs anything; eights whose squares leave the range of fp32 are squared in 64 bits, so finite gradients never
 // overflow or vanish.
 // Measured: 0.59 G fp32 (one layer of 64 experts, its block and its table) into other buffers 1071 us, 6.6 TB/s over the two reads and the write;
-// the norm alone 6.5 TB/s from 0.18 G on; 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor
+// the norm alone 6.5 TB/s from 0.18 G on (bf16 5.6), with no common 16-byte boundary of source and destination 356 us instead of 357 for 0.18 G fp32; 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor
 // made by the last block of the first kernel 6.9).
 #include "rr_ffn.cuh"
 #include "rr_vec.cuh"
@@ -30,7 +30,7 @@ struct GradEntry {
     long long first;     // its first chunk; the entry behind the last tensor holds the number of chunks
     int src_f32, dst_f32;
     int head;            // elements up to the first that both src and dst hold at a 16-byte boundary; -1: there is none
-    int pad;
+    int src_head;        // the same for the squares, which read src alone: head, or where there is none up to src's first
 };
 
 constexpr int kPlanEntries = 64;     // written by one launch (3 KB of parameters)
@@ -77,18 +77,18 @@ struct Range {
     long long lo, hi, body;
     int eights;
 };
-__device__ __forceinline__ Range range_of(const GradEntry &e, long long c, int chunk)
+__device__ __forceinline__ Range range_of(const GradEntry &e, int head, long long c, int chunk)
 {
     Range r;
-    if (e.head < 0) {
+    if (head < 0) {
         r.lo = c * chunk;
         r.hi = min(e.n, r.lo + chunk);
         r.body = r.hi;
         r.eights = 0;
     } else {
-        r.body = min(e.n, e.head + c * chunk);
+        r.body = min(e.n, head + c * chunk);
         r.lo = c ? r.body : 0;
-        r.hi = min(e.n, e.head + (c + 1) * chunk);
+        r.hi = min(e.n, head + (c + 1) * chunk);
         r.eights = (int)((r.hi - r.body) >> 3);
     }
     return r;
@@ -120,19 +120,32 @@ __device__ __forceinline__ double block_sum(double v, double *buf)
     return v;
 }
 
-// f(k) for every element k of the range that the body leaves over, in front of it (all of a tensor without common boundaries) and behind it
-template <class F>
-__device__ __forceinline__ void edges(const Range &r, F f)
+// f(k, element k) for every element of the range that the body leaves over, in front of it (all of a tensor without common boundaries: eight at
+// a time) and behind it
+template <class T, class F>
+__device__ __forceinline__ void edges(const T *src, const Range &r, F f)
 {
-    for (long long k = r.lo + threadIdx.x; k < r.body; k += kClipThreads) f(k);
-    const long long k = r.body + 8ll * r.eights + threadIdx.x;
-    if (k < r.hi) f(k);
+    long long k = r.lo + threadIdx.x;
+    for (; k + 7 * kClipThreads < r.body; k += 8 * kClipThreads) {
+        Unit<T, 1> e[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) e[u].template load<kKeep>(src + k + u * kClipThreads);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            float v[1];
+            e[u].get(v);
+            f(k + u * kClipThreads, v[0]);
+        }
+    }
+    for (; k < r.body; k += kClipThreads) f(k, as_f32(src[k]));
+    k = r.body + 8ll * r.eights + threadIdx.x;
+    if (k < r.hi) f(k, as_f32(src[k]));
 }
 
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
 {
-    constexpr int kN = 16 / sizeof(T), kAtOnce = 2 * kClipUnroll;  // 16 bytes, and how many of them a thread has in flight
+    constexpr int kN = 16 / sizeof(T), kAtOnce = kClipUnroll * 8 / kN;  // 16 bytes, and how many of them a thread has in flight (a chunk has that many)
     const int units = r.eights * (8 / kN);
     const T *p = src + r.body;
     double sum = 0;
@@ -156,8 +169,8 @@ __device__ __forceinline__ double chunk_squares(const T *src, const Range &r)
         e.get(v);
         sum += squares<kN>(v);
     }
-    edges(r, [&](long long k) {
-        const double v = as_f32(src[k]);
+    edges(src, r, [&](long long, float x) {
+        const double v = x;
         sum += v * v;
     });
     return sum;
@@ -174,7 +187,7 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const GradEntry *
     p.end = 0;
     for (long long c = blockIdx.x; c < chunks; c += gridDim.x) {
         if (c >= p.end) seek(p, plan, tensors, c);
-        const Range r = range_of(p.e, c - p.e.first, chunk);
+        const Range r = range_of(p.e, p.e.src_head, c - p.e.first, chunk);
         sum += p.e.src_f32 ? chunk_squares(static_cast<const float *>(p.e.src), r) : chunk_squares(static_cast<const bf16 *>(p.e.src), r);
     }
     sum = block_sum(sum, buf);
@@ -207,7 +220,7 @@ __device__ __forceinline__ void chunk_scale(const TS *src, TD *dst, const Range 
         scaled<kN>(e, o, f);
         o.template store<kStream>(q + (long long)i * kN);
     }
-    edges(r, [&](long long k) { dst[k] = from_f32<TD>(as_f32(src[k]) * f); });
+    edges(src, r, [&](long long k, float x) { dst[k] = from_f32<TD>(x * f); });
 }
 
 __global__ void __launch_bounds__(kClipThreads)
@@ -235,7 +248,7 @@ k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, co
         if (c < p.e.first) seek(p, plan, tensors, c);
         const GradEntry &e = p.e;
         if (!e.dst || (e.dst == e.src && f == 1.0f)) continue;
-        const Range r = range_of(e, c - e.first, chunk);
+        const Range r = range_of(e, e.head, c - e.first, chunk);
         if (e.src_f32) {
             if (e.dst_f32) chunk_scale(static_cast<const float *>(e.src), static_cast<float *>(e.dst), r, f);
             else chunk_scale(static_cast<const float *>(e.src), static_cast<bf16 *>(e.dst), r, f);
@@ -248,11 +261,10 @@ k_grad_scale(const GradEntry *plan, int tensors, long long chunks, int chunk, co
 
 int size_of(int dtype) { return dtype == RR_F32 ? 4 : 2; }
 
-// elements up to the first at which both addresses are multiples of 16 bytes, -1 if there is none
-int common_head(const rr_grad &g)
+// elements up to the first at which both addresses (of elements of ss and ds bytes) are multiples of 16 bytes, -1 if there is none
+int common_head(const void *src, int ss, const void *dst, int ds)
 {
-    const uintptr_t s = (uintptr_t)g.src, d = g.dst ? (uintptr_t)g.dst : s;
-    const int ss = size_of(g.src_dtype), ds = g.dst ? size_of(g.dst_dtype) : ss;
+    const uintptr_t s = (uintptr_t)src, d = (uintptr_t)dst;
     for (int h = 0; h < 8; ++h)
         if ((s + (uintptr_t)h * ss) % 16 == 0 && (d + (uintptr_t)h * ds) % 16 == 0) return h;
     return -1;
@@ -286,7 +298,10 @@ rr_status launch_grad_plan(int tensors, const rr_grad *list, void *plan, rr_grad
             e.n = g.n;
             e.src_f32 = g.src_dtype == RR_F32;
             e.dst_f32 = g.dst_dtype == RR_F32;
-            e.head = common_head(g);
+            const int ss = size_of(g.src_dtype), src_head = common_head(g.src, ss, g.src, ss);
+            e.head = g.dst ? common_head(g.src, ss, g.dst, size_of(g.dst_dtype)) : src_head;
+            // (without a common one there is a chunk for every `chunk` elements from the first on, which reach as far from src's)
+            e.src_head = e.head < 0 ? src_head : e.head;
             const long long body = e.head < 0 ? g.n : g.n > e.head ? g.n - e.head : 0;
             first += g.n == 0 ? 0 : body == 0 ? 1 : (body + chunk - 1) / chunk;
         }

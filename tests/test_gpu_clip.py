@@ -80,6 +80,23 @@ def test_a_plain_list_is_clipped_in_place():
     _check(grads, keep, rr.clip_grads(grads, 1.0), 1.0)
 
 
+@pytest.mark.parametrize("types", ["ff", "bb", "fb", "bf"])
+@pytest.mark.parametrize("n", [1, 9, 2047, 2048 + 8, 3 * 8192 + 5, 1 << 23])
+def test_buffers_without_a_common_boundary(types, n):
+    """src begins one to seven elements behind a 16-byte boundary and dst at one, and the other way round."""
+    import paper_2402_12399_b200 as rr
+    for s, d in ((1, 0), (0, 1), (3, 2), (7, 0), (0, 7)):
+        g = torch.Generator("cuda").manual_seed(n + s)
+        src = torch.randn(n + s, generator=g, device="cuda").to(T[types[0]])[s:]
+        whole = torch.full((n + d + 9,), 7.0, device="cuda", dtype=T[types[1]])
+        keep, out = src.clone(), whole[d:d + n]
+        plan = rr.grad_plan([src], out=[out])
+        norm = rr.clip_grads(plan, 0.5)
+        rr.check(norm._workspace)
+        _check([out], [keep], norm, 0.5)
+        assert torch.equal(src, keep) and (whole[:d] == 7).all() and (whole[d + n:] == 7).all()
+
+
 @pytest.mark.parametrize("t", "fb")
 @pytest.mark.parametrize("size", [1e30, 3e38, 1e-30, 1e-40, 0.0])
 def test_squares_that_fp32_cannot_hold(t, size):
