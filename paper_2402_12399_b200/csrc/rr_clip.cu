@@ -7,8 +7,9 @@
 // length nor the order costs anything; eights whose squares leave the range of fp32 are squared in 64 bits, so finite gradients never
 // overflow or vanish.
 // Measured: 0.59 G fp32 (one layer of 64 experts, its block and its table) into other buffers 1071 us, 6.6 TB/s over the two reads and the write;
-// the norm alone 6.5 TB/s from 0.18 G on (bf16 5.6), with no common 16-byte boundary of source and destination 356 us instead of 357 for 0.18 G fp32; 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor
-// made by the last block of the first kernel 6.9).
+// 0.18 G fp32 357 us, with no common 16-byte boundary 356 (an element at a time and one load after the other 2340); the norm alone 6.5 TB/s from
+// 0.18 G on (bf16 5.6); 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor made by the last block of
+// the first kernel 6.9).
 #include "rr_ffn.cuh"
 #include "rr_vec.cuh"
 
