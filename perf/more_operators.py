@@ -99,7 +99,7 @@ def draw(rng):
             if n * d <= 65536 * 1024 and V * d <= 32000 * 4096:
                 return _embed("", op, n, V, d, two(), two(), rng.choice([1.0, 1.0, 0.5, 32.0]), rng.choice([0.0, 0.1, 0.3]), rng.random() < 0.5)
     while True:
-        E, d, f, V, blocks = rng.choice([0, _log(rng, 1, 64)]), _log(rng, 8, 4096), _log(rng, 8, 8192), rng.choice([0, _log(rng, 8, 64000)]), _log(rng, 1, 5)  # (at most 52 outputs)
+        E, d, f, V, blocks = rng.choice([0, _log(rng, 1, 64)]), _log(rng, 8, 4096), _log(rng, 8, 8192), rng.choice([0, _log(rng, 8, 64000)]), _log(rng, 1, 16)
         if blocks * (3 * E * d * f + E * d + 4 * d * d) + V * d <= MOST_CLIP:
             active = rng.random() < 0.7
             return _clip("", blocks, E, d, f, V, two(), two(), two(), rng.random() < 0.4, active)
