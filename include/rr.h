@@ -531,7 +531,8 @@ typedef struct rr_norm_shape {
  * differences, and all sums have a fixed order: results repeat bit for bit.  Matrices are read 16 bytes at a time where N is a multiple of 8 and
  * pitches are multiples of 16 bytes, and element by element otherwise; any pitch of at least N is taken.  M == 0 does nothing
  * forward and sets dw and db to zero backward (or leaves them under RR_ADD_DW).  An output that overlaps what the call reads, or another
- * output, in any other way than named is refused, as for rr_linear_*.  Calls that share a workspace must not overlap on the GPU.
+ * output, in any other way than named is refused, as for rr_linear_*.  Calls that share a workspace must not overlap on the GPU; what
+ * rr_norm_workspace_bytes says of M and N is enough for every smaller M and N.
  */
 rr_status rr_norm_workspace_bytes(int M, int N, size_t *bwd_bytes);
 rr_status rr_norm_fwd(const rr_norm_shape *s /* host */, const void *x, const void *residual, const void *w, const void *b, void *h, void *y,
@@ -560,7 +561,7 @@ typedef struct rr_embed_shape {
  * fp32 arithmetic, one rounding to the result's type (under RR_ADD_DW of the sum with what was there).  The gradient's sums follow the order
  * of the tokens, in pieces that depend on n, d and the ids alone: results repeat bit for bit.  n == 0 does nothing forward; backward
  * it sets dtable to zero, or leaves it under RR_ADD_DW.  An output that overlaps what the call reads is refused.  Calls that share a
- * workspace must not overlap on the GPU.
+ * workspace must not overlap on the GPU; what rr_embed_workspace_bytes says of n and d is enough for every smaller n and d.
  */
 rr_status rr_embed_workspace_bytes(int n, int V, int d, size_t *fwd_bytes, size_t *bwd_bytes);
 rr_status rr_embed_fwd(const rr_embed_shape *s /* host */, const void *ids, const void *table, void *y, void *workspace,

@@ -593,6 +593,16 @@ struct Type {
 template <class F>
 cudaError_t with_type(int dtype, F f) { return dtype == RR_F32 ? f(Type<float>{}) : f(Type<bf16>{}); }
 
+// Floats of the pieces of `n` tokens, and of any fewer or narrower ones, so that the workspace of a program's largest batch serves every other:
+// two rows a chunk.  Chunks are shorter where tokens are few, and then a row of each makes at most 2^23 + d floats in all: chunks of 8 (16) are taken
+// below n ceil(d / 256) = 2^18 (2^19), so that n d / 8 (n d / 16) stays below 2^26 / 8 (2^27 / 16), and the last chunk adds a row.
+size_t piece_floats(long long n, int d)
+{
+    const size_t least = (size_t)((n + kMostChunk - 1) / kMostChunk) * d, most = (size_t)((n + kLeastChunk - 1) / kLeastChunk) * d, cap = (1ull << 23) + d;
+    const size_t few = most < cap ? most : cap;
+    return 2 * (least > few ? least : few);
+}
+
 struct BwdLayout {
     Header *hdr;
     int *key, *pos, *key2, *pos2, *runs, *list;
@@ -615,8 +625,8 @@ size_t bwd_layout(void *ws, long long n, int d, BwdLayout *out)
     l.key2 = n > kSlab ? c.take<int>(n) : l.key;
     l.pos2 = n > kSlab ? c.take<int>(n) : l.pos;
     l.runs = c.take<int>(1);
-    l.list = c.take<int>(n / (2 * l.chunk) + 1);
-    l.part = c.take<float>(n > 2 * l.chunk ? (size_t)l.chunks * 2 * d : 0);
+    l.list = c.take<int>(n / (2 * kLeastChunk) + 1);
+    l.part = c.take<float>(n > kDirect ? piece_floats(n, d) : 0);  // (fewer tokens are not sorted)
     if (out) *out = l;
     return align_up(c.off, 256);
 }
@@ -783,7 +793,7 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     err = with_types([&](auto ty, auto to, auto layout) {
         return launch_dependent(k_embed_sum<typename decltype(ty)::type, typename decltype(to)::type, layout()>, grid, threads, 0, 1, st, b);
     });
-    if (err == cudaSuccess && s.n > 2 * l.chunk)  // (else no run is long)
+    if (err == cudaSuccess)
         err = with_types([&](auto, auto to, auto layout) {
             return launch_dependent(k_embed_join<typename decltype(to)::type, layout()>, join, kJoin * kJoinCols, 0, 1, st, b, tiles);
         });

@@ -323,7 +323,14 @@ cudaError_t with_layout(const NormLayout &l, F f)
 
 }  // namespace
 
-size_t norm_workspace(int M, int N) { return kHeaderBytes + align_up((size_t)bwd_parts(M, N) * N * 4, 256) * 2; }
+// (enough for narrower rows too, so that the workspace of a program's largest norm serves every other: up to 4096 columns there are two blocks an
+// SM that leave a part, beyond that one)
+size_t norm_workspace(int M, int N)
+{
+    const int narrow = N < 4096 ? N : 4096;
+    const size_t own = (size_t)bwd_parts(M, N) * N, less = (size_t)bwd_parts(M, narrow) * narrow;
+    return kHeaderBytes + align_up((own > less ? own : less) * 4, 256) * 2;
+}
 
 rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h, const void *w, const float *mean, const float *rstd, const void *dh,
                           void *dx, float *dw, float *db, void *workspace, cudaStream_t st)
