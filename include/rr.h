@@ -7,8 +7,8 @@
  *    pointers are ordinary host memory.  All dev pointers must be 16-byte
  *    aligned; hidden / weight / dout tensors must be 128-byte aligned (they are
  *    read through TMA).  Everything is row-major and densely packed (rr_linear_*, rr_norm_* and
- *    rr_embed_* ask for 16 bytes and take pitches; ids and the gradients of a clip need only the
- *    alignment of their type).
+ *    rr_embed_* ask for 16 bytes and take pitches; ids, the gradients of a clip, and the gradients of
+ *    the norm's weight and bias and of the embedding's table need only the alignment of their type).
  *  - The caller owns and allocates every buffer, including the workspace.  The
  *    library allocates no device memory and keeps no state between calls other
  *    than lazily resolved driver entry points.
@@ -524,7 +524,7 @@ typedef struct rr_norm_shape {
  *     dw = sum over the rows of dy xh,   db = sum over the rows of dy
  *   h, w, mean, rstd as in the forward pass (h is x where that had no residual)
  *   dh [M,N] or NULL: gradient that reaches h along the residual stream, type dx_dtype
- *   dx [M,N]: the gradient of h, which is that of x and of residual;  dw [N], db [N] fp32.  Each of the three may be NULL.
+ *   dx [M,N]: the gradient of h, which is that of x and of residual;  dw [N], db [N] fp32, aligned to 4 bytes.  Each of the three may be NULL.
  *   dx may be the same buffer as dy, h or dh (same type and pitch)
  *   workspace dev, >= rr_norm_workspace_bytes, 256-byte aligned
  * The arithmetic is fp32 with one rounding to the type of each result; a row is held on the chip, so the variance is a mean of squared
@@ -556,7 +556,7 @@ typedef struct rr_embed_shape {
  * rr_embed_bwd:  dtable_v = scale (sum over the tokens i with id_i = v of dy_i), rows without a token 0; under RR_ADD_DW added to what
  *                dtable holds (rows without a token are not touched).  What dy holds for id -1 does not matter.
  *   ids [n] dev, i32 or i64, aligned to their size;  an id outside -1..V-1 counts as -1 and latches RR_ERR_INVALID_ARG in the workspace header
- *   table, dtable [V,d] dev, 16-byte aligned, dense;  y, dy [n,d] dev, 16-byte aligned
+ *   table [V,d] dev, 16-byte aligned, dense;  dtable [V,d] dev, aligned to its element, dense;  y, dy [n,d] dev, 16-byte aligned
  *   workspace dev, >= fwd_bytes / bwd_bytes, 256-byte aligned; its first 256 bytes are zero when first used (the status word)
  * fp32 arithmetic, one rounding to the result's type (under RR_ADD_DW of the sum with what was there).  The gradient's sums follow the order
  * of the tokens, in pieces that depend on n, d and the ids alone: results repeat bit for bit.  n == 0 does nothing forward; backward

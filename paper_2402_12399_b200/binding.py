@@ -824,7 +824,8 @@ def norm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mea
              add_dw: bool = False, workspace: torch.Tensor | None = None):
     """rr_norm_bwd; writes the gradients whose buffers are given -- dx [M,N] (bf16 or fp32; the gradient of h, so that of x and of the
     residual), dw [N] and dbias [N] fp32 -- and returns (dx, dw, dbias).  `h` is what the norm was taken of (x where there was no residual);
-    `dh`, of dx's type, is the gradient that reaches it along the residual stream.  With add_dw, dw and dbias are added to."""
+    `dh`, of dx's type, is the gradient that reaches it along the residual stream.  With add_dw, dw and dbias are added to; they may lie
+    anywhere in a flat buffer."""
     shape = dy.shape
     M, N = shape
     if workspace is None:
@@ -897,8 +898,8 @@ def embed_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: t
 
 def embed_bwd(ids: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
               workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """rr_embed_bwd; writes (or, with accumulate, adds to) the gradient of the table [V,d], bf16 or fp32, and returns it.  dy [n,d] may be a
-    view whose rows lie apart."""
+    """rr_embed_bwd; writes (or, with accumulate, adds to) the gradient of the table [V,d], bf16 or fp32, and returns it; it may lie anywhere
+    in a flat buffer.  dy [n,d] may be a view whose rows lie apart."""
     V, d = dtable.shape
     n = ids.numel()
     if workspace is None:

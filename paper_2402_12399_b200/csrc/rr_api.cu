@@ -678,7 +678,7 @@ rr_status rr_norm_bwd(const rr_norm_shape *shape, const void *dy, const void *h,
     rr_norm_shape s;
     rr_status rc = check_norm(shape, &s);
     if (rc) return rc;
-    if (!aligned(dx, 16) || !aligned(dw, 16) || !aligned(db, 16)) return RR_ERR_INVALID_ARG;
+    if (!aligned(dx, 16) || !aligned(dw, 4) || !aligned(db, 4)) return RR_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (s.M == 0) {  // no rows: the gradients of the parameters are zero
         if (!(s.flags & RR_ADD_DW) && ((dw && cudaMemsetAsync(dw, 0, (size_t)s.N * 4, st) != cudaSuccess) ||
@@ -728,7 +728,7 @@ rr_status check_embed(const rr_embed_shape *in, rr_embed_shape *s)
 rr_status check_embed_call(const rr_embed_shape &s, const void *ids, const void *in, const void *out, const void *workspace, bool back)
 {
     if (!ids || !in || !out || !workspace) return RR_ERR_INVALID_ARG;
-    if (!aligned(ids, s.wide_ids ? 8 : 4) || !aligned(in, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
+    if (!aligned(ids, s.wide_ids ? 8 : 4) || !aligned(in, 16) || !aligned(out, back ? bytes_of(s.table_dtype) : 16) || !aligned(workspace, 256)) return RR_ERR_INVALID_ARG;
     const Region rows = matrix(back ? in : out, s.n, s.d, s.ldy, bytes_of(s.y_dtype)), tab = matrix(back ? out : in, 1, (long long)s.V * s.d, (long long)s.V * s.d, bytes_of(s.table_dtype)),
                  rid = matrix(ids, 1, s.n, s.n, s.wide_ids ? 8 : 4);
     return overlap(rows, tab) || overlap(back ? tab : rows, rid) ? RR_ERR_INVALID_ARG : RR_OK;
@@ -764,7 +764,7 @@ rr_status rr_embed_bwd(const rr_embed_shape *shape, const void *ids, const void 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (s.n == 0) {  // no tokens: the gradient is zero
         if (s.flags & RR_ADD_DW) return RR_OK;
-        if (!dtable || !aligned(dtable, 16)) return RR_ERR_INVALID_ARG;
+        if (!dtable || !aligned(dtable, bytes_of(s.table_dtype))) return RR_ERR_INVALID_ARG;
         return cudaMemsetAsync(dtable, 0, (size_t)s.V * s.d * bytes_of(s.table_dtype), st) == cudaSuccess ? RR_OK : RR_ERR_CUDA;
     }
     rc = check_embed_call(s, ids, dy, dtable, workspace, true);

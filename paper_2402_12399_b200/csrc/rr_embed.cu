@@ -720,7 +720,9 @@ rr_status launch_embed_bwd(const rr_embed_shape &s, const void *ids, const void 
     BwdLayout l;
     bwd_layout(ws, s.n, s.d, &l);
     const bool add = (s.flags & RR_ADD_DW) != 0;
-    const Layout L = s.d % 8 == 0 && s.ldy % 8 == 0 ? kEights : layout_of(s);  // (fp32 too: its loads meet in the L1 cache)
+    // (eights in fp32 too: its loads meet in the L1 cache; a table that starts anywhere, in a flat buffer, goes one by one: 65536 x 1024 into fp32
+    // 119 us instead of 85)
+    const Layout L = (uintptr_t)dtable % 16 != 0 ? kOne : s.d % 8 == 0 && s.ldy % 8 == 0 ? kEights : layout_of(s);
     const EmbArgs e = emb_args(s, ids, dy, dtable, ws);
     const long long zeroing = add ? 0 : ((long long)s.V * s.d * (s.table_dtype == RR_F32 ? 4 : 2) + 65535) / 65536;  // blocks that have 64 KB to zero
     // calls f(type of dy, type of dtable, layout)

@@ -352,7 +352,8 @@ rr_status launch_norm_bwd(const rr_norm_shape &s, const void *dy, const void *h,
     a.rstd = const_cast<float *>(rstd);
     a.dh = dh;
     a.dx = dx;
-    const bool fold = parts > 1 && (dw || db);
+    // (gradients that start anywhere, in a flat buffer, are written one by one: the second kernel does; one row 4.8 us instead of 3.1)
+    const bool fold = (dw || db) && (parts > 1 || ((uintptr_t)dw | (uintptr_t)db) % 16 != 0);
     Carver c(workspace);
     c.take<Header>(1);
     float *pw = c.take<float>((size_t)parts * s.N), *pb = c.take<float>((size_t)parts * s.N);
