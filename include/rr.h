@@ -528,8 +528,9 @@ typedef struct rr_norm_shape {
  *   dx may be the same buffer as dy, h or dh (same type and pitch)
  *   workspace dev, >= rr_norm_workspace_bytes, 256-byte aligned
  * The arithmetic is fp32 with one rounding to the type of each result; a row is held on the chip, so the variance is a mean of squared
- * differences, and all sums have a fixed order: results repeat bit for bit.  Matrices are read 16 bytes at a time where N is a multiple of 8 and
- * pitches are multiples of 16 bytes, and element by element otherwise; any pitch of at least N is taken.  M == 0 does nothing
+ * differences, and all sums have a fixed order: results repeat bit for bit.  A thread reads eight
+ * elements at once where all matrices are bf16 and N and all pitches are multiples of 8, four where N and all pitches are multiples of 4,
+ * and single elements otherwise (backward their rows come to the chip in pieces of 16 bytes); any pitch of at least N is taken.  M == 0 does nothing
  * forward and sets dw and db to zero backward (or leaves them under RR_ADD_DW).  An output that overlaps what the call reads, or another
  * output, in any other way than named is refused, as for rr_linear_*.  Calls that share a workspace must not overlap on the GPU; what
  * rr_norm_workspace_bytes says of M and N is enough for every smaller M and N.
@@ -606,7 +607,8 @@ rr_status rr_clip_grads(const rr_grad_set *set /* host */, float bound, float *n
 
 /*
  * rr_check -- synchronise `stream`, then return the status word latched in `workspace`
- * (RR_OK, RR_ERR_NONFINITE, RR_ERR_TIMEOUT) or RR_ERR_CUDA if the stream reports an error.
+ * (RR_OK, RR_ERR_NONFINITE, RR_ERR_TIMEOUT, RR_ERR_INVALID_ARG of an id outside the table) or RR_ERR_CUDA if the stream
+ * reports an error.
  * The first error latched since the last rr_check is kept; rr_check clears it after reporting.
  */
 rr_status rr_check(const void *workspace /* dev */, void *stream);
