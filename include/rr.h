@@ -607,7 +607,7 @@ rr_status rr_clip_grads(const rr_grad_set *set /* host */, float bound, float *n
 
 /*
  * rr_check -- synchronise `stream`, then return the status word latched in `workspace`
- * (RR_OK, RR_ERR_NONFINITE, RR_ERR_TIMEOUT, RR_ERR_INVALID_ARG of an id outside the table) or RR_ERR_CUDA if the stream
+ * (RR_OK, RR_ERR_NONFINITE, RR_ERR_TIMEOUT, RR_ERR_INVALID_ARG of an id or an expert that there is none of) or RR_ERR_CUDA if the stream
  * reports an error.
  * The first error latched since the last rr_check is kept; rr_check clears it after reporting.
  */

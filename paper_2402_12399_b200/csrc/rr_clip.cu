@@ -8,7 +8,8 @@
 // overflow or vanish.
 // Measured: 0.59 G fp32 (one layer of 64 experts, its block and its table) into other buffers 1071 us, 6.6 TB/s over the two reads and the write;
 // 0.18 G fp32 357 us, with no common 16-byte boundary 356 (an element at a time and one load after the other 2340); the norm alone 6.5 TB/s from
-// 0.18 G on (bf16 5.6); 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor made by the last block of
+// 0.18 G on (bf16 5.6), and in tensors of about a million elements each, where every chunk of a block lies in another one and has to be looked up, 5.4 to 5.7
+// (bf16 3.6 to 4.0: 576 tensors, 0.82 G, 609 and 458 us); 0.5 M in 12 tensors 5.4 us (the latencies of two kernels that depend on each other; with the factor made by the last block of
 // the first kernel 6.9).
 #include "rr_ffn.cuh"
 #include "rr_vec.cuh"

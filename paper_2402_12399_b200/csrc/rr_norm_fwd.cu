@@ -135,8 +135,8 @@ __global__ void __launch_bounds__(kThreads, fwd_blocks(kThreads, kSlots)) k_norm
     }
 }
 
-// Two eights a thread, or four: one matrix to read and rows enough to fill the SMs want more of it in flight (65536 x 1024 in bf16 48 us instead of 52), and a
-// row beyond 4096 columns fewer threads that meet (8192 x 8192 52 us instead of 67).
+// Two eights a thread, or four: one matrix to read and rows enough to fill the SMs want more of it in flight (65536 x 1024 in bf16 44 us instead of 53), and a
+// row beyond 4096 columns fewer threads that meet (8192 x 8192 52 us instead of 71).
 NormLayout fwd_layout(int M, int N, Layout L, bool residual, int sms)
 {
     NormLayout l = norm_layout(N, 2, 128);
