@@ -750,6 +750,17 @@ def balance_bwd(logits: torch.Tensor, count: torch.Tensor, n_live: torch.Tensor,
 
 # ---- the rest of a training step around the layer ------------------------------------------------------
 
+def _own_workspace(nbytes: int, device) -> torch.Tensor:
+    """A workspace for one call, of which only the header has to be zero: a large one is not filled behind it (the embedding's gradient of 65536 x
+    1024 81 us instead of 99), a small one takes one call (the norm's of 2048 x 1024, 2.4 MB,
+    18.9 us instead of 20.1)."""
+    if nbytes <= 8 << 20:
+        return alloc_workspace(nbytes, device)
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    workspace[:256].zero_()
+    return workspace
+
+
 def norm_workspace_bytes(M: int, N: int) -> int:
     """Workspace bytes of norm_bwd."""
     a = C.c_size_t(0)
@@ -829,7 +840,7 @@ def norm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mea
     shape = dy.shape
     M, N = shape
     if workspace is None:
-        workspace = alloc_workspace(norm_workspace_bytes(M, N), dy.device)
+        workspace = _own_workspace(norm_workspace_bytes(M, N), dy.device)
     here = _here()
     _elsewhere(here, dy, h, weight, mean, rstd, dh, dx, dw, dbias, workspace)
     lddy = ldh = lddh = lddx = dt = 0
@@ -903,7 +914,7 @@ def embed_bwd(ids: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, scale: 
     V, d = dtable.shape
     n = ids.numel()
     if workspace is None:
-        workspace = alloc_workspace(embed_workspace_bytes(n, V, d)[1], dtable.device)
+        workspace = _own_workspace(embed_workspace_bytes(n, V, d)[1], dtable.device)
     here = _here()
     _elsewhere(here, ids, dy, dtable, workspace)
     if not dtable.is_contiguous():

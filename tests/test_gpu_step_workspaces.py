@@ -49,3 +49,30 @@ def test_norm_gradients(large, small):
     # sums of M terms of either sign in at most 300 + M / 148 steps, each 2^-24 of the magnitudes
     want, size = dy.double().sum(0), dy.double().abs().sum(0)
     assert ((got[2].double() - want).abs() <= (300 + M / 148) * 2.0 ** -24 * size).all()
+
+
+def test_calls_without_a_workspace_of_their_own():
+    """The binding's own workspace has a header of zeros whatever its memory held before; what it holds behind does not matter."""
+    import paper_2402_12399_b200 as rr
+    n, V, d = 3000, 50, 4096
+    g = torch.Generator("cuda").manual_seed(1)
+    ids, dy = torch.randint(0, V, (n,), generator=g, device="cuda"), torch.randint(-3, 4, (n, d), generator=g, device="cuda").bfloat16()
+    want = torch.zeros(V, d, device="cuda").index_add_(0, ids, dy.float())
+    out, dw, rstd = torch.empty(V, d, device="cuda"), torch.empty(d, device="cuda"), torch.ones(n, device="cuda")
+    for nbytes in (rr.embed_workspace_bytes(n, V, d)[1], rr.norm_workspace_bytes(n, d)):
+        assert nbytes > 8 << 20
+    sums = None
+    for fill in (0, 0xff, 0x5a):
+        for nbytes in (rr.embed_workspace_bytes(n, V, d)[1], rr.norm_workspace_bytes(n, d)):
+            torch.full((nbytes,), fill, dtype=torch.uint8, device="cuda")      # goes back to the allocator, which hands it out again
+        rr.embed_bwd(ids, dy, out)
+        rr.check(out._workspace)
+        assert torch.equal(out, want)
+        rr.norm_bwd(dy, dy, None, None, rstd, kind=rr.NORM_RMS, dw=dw)
+        sums = dw.clone() if sums is None else sums
+        assert torch.equal(dw, sums)
+    # an id outside the table is reported once, by the workspace that saw it
+    ids[0] = V
+    rr.embed_bwd(ids, dy, out)
+    with pytest.raises(rr.RRError):
+        rr.check(out._workspace)
