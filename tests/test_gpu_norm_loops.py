@@ -1,5 +1,5 @@
 """The norm where every block goes round its loop over the rows several times: forward from 32 sets of rows an SM on, backward from one or two on; rows
-wider than 4096 columns backward; offsets beyond 2^32 elements; the stored mean of rows far from zero.  Tolerances as in the tests of single rounds:
+wider than 4096 columns backward; offsets beyond 2^32 elements; the stored mean of rows far from zero.  Tolerances as where every block takes one set of rows:
 u = 2^-24, half a step of the result's type, 120 u (1 + |xh|) |w| for y, 160 u of the magnitudes for dx, at most 300 + M / 148 steps for dw and db."""
 import itertools
 
